@@ -206,6 +206,55 @@ int director_expert_ffn_combine(director_ctx* ctx, int32_t T, const void* xp, co
 int director_combine(director_ctx* ctx, int32_t T, const void* yp, const int32_t* inv_row,
                      const float* topk_w, const void* y_shared, void* y, void* stream);
 
+/* ---- The backward pass of the layer (fine-tuning; the paper serves and does not train) ----
+ * With the forward calls director_route, director_dispatch, director_expert_ffn_checkpoint and director_combine, and
+ * the gradient dy of y, the gradients of x, of the logits and of all weights come from
+ *   director_combine_backward  -> director_expert_ffn_backward -> director_dispatch_backward,  director_route_backward.
+ * Accumulation is in fp32 throughout, in a fixed order: a call repeated on the same inputs gives the same bits. */
+
+/* Gradient of director_combine:  dyp[inv_row[t,s],:] = bf16( topk_w[t,s] * dy[t,:] ),
+ *   dtopk_w[t,s] = sum_h dy[t,h] * yp[inv_row[t,s],h].
+ * (The gradient of y_shared is dy itself.)  dy: dev bf16 [T,H].  yp: dev bf16 [T*K,H], the forward's expert outputs.
+ * inv_row: dev int32 [T,K].  topk_w: dev fp32 [T,K].  dyp: dev bf16 [T*K,H].  dtopk_w: dev fp32 [T,K].
+ * An assignment with inv_row < 0 gets dtopk_w = 0; a row >= T*K is skipped the same way and reported as
+ * DIRECTOR_ERR_BAD_INDEX. */
+int director_combine_backward(director_ctx* ctx, int32_t T, const void* dy, const void* yp, const int32_t* inv_row,
+                              const float* topk_w, void* dyp, float* dtopk_w, void* stream);
+
+/* Gradient of director_dispatch's row copies:  dx[t,:] = bf16( sum_s dxp[inv_row[t,s],:] (+ dx_shared[t,:]) ), summed in
+ * slot order.  dxp: dev bf16 [T*K,H].  inv_row: dev int32 [T,K].  dx_shared: dev bf16 [T,H], the shared experts' (or any
+ * other branch's) gradient of x, or NULL.  dx: dev bf16 [T,H]. */
+int director_dispatch_backward(director_ctx* ctx, int32_t T, const void* dxp, const int32_t* inv_row,
+                               const void* dx_shared, void* dx, void* stream);
+
+/* Gradient of director_route (the choice of experts is piecewise constant; the weights are the softmax of the chosen
+ * logits):  dlogits[t,topk_idx[t,s]] = topk_w[t,s] * (dtopk_w[t,s] - sum_j topk_w[t,j] * dtopk_w[t,j]), all other
+ * entries 0.  topk_idx: dev int32 [T,K].  topk_w, dtopk_w: dev fp32 [T,K].  dlogits: dev fp32 [T,E], written whole.
+ * An index outside [0,E) is skipped and reported as DIRECTOR_ERR_BAD_INDEX. */
+int director_route_backward(director_ctx* ctx, int32_t T, const int32_t* topk_idx, const float* topk_w,
+                            const float* dtopk_w, float* dlogits, void* stream);
+
+/* director_expert_ffn for training: the same outputs (the bits that the tensor-core kernels give, at every batch size),
+ * and the gate and up values g = xp . w_gate[e]^T, u = xp . w_up[e]^T kept in 8 bits for director_expert_ffn_backward.
+ * Sixteen consecutive features of a row share a power of two, gate and up one each:
+ *   e = max(biased exponent of the largest magnitude - 6, 1),  code = clamp(rint(v * 2^(127-e)), -127, 127),
+ *   and the value kept is code * 2^(e-127); a block with a NaN or an infinity has e = 255 and reads as NaN.
+ * codes: dev int8 [T*K,F,2], (gate, up) pairs.  exps: dev uint8 [F/16,T*K,2].  Rows that belong to no segment are not
+ * written.  Shared experts (S > 0 and x != NULL): codes_shared int8 [T,S*F,2], exps_shared uint8 [S*F/16,T,2].
+ * Other arguments as for director_expert_ffn.  Needs the default tile scheme (director_set_ffn_variant 2 or 6) and
+ * distinct w_gate and w_up arrays less than 2^40 bytes apart, otherwise DIRECTOR_ERR_UNSUPPORTED. */
+int director_expert_ffn_checkpoint(director_ctx* ctx, int32_t T, const void* xp, const int32_t* seg_offsets,
+                                   const void* w_gate, const void* w_up, const void* w_down, int8_t* codes,
+                                   uint8_t* exps, void* yp, const void* x, const void* ws_gate, const void* ws_up,
+                                   const void* ws_down, int8_t* codes_shared, uint8_t* exps_shared, void* y_shared,
+                                   void* stream);
+
+/* The values that a checkpoint stands for, as numbers: gate[r,f], up[r,f] = code * 2^(e-127), exact in bf16.
+ * codes: dev int8 [rows,F,2].  exps: dev uint8 [F/16,rows,2].  gate, up: dev bf16 [rows,F].  rows >= 1, F % 16 == 0,
+ * rows * F / 16 < 2^31. */
+int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const int8_t* codes, const uint8_t* exps,
+                               void* gate, void* up, void* stream);
+
 /* (a5) Placement cost (Section VI-A): workload matrix W, per-rank load of Eq. 1 and dispatch
  * volume of Eq. 3 for the current placement, counted per executed assignment.
  * topk_idx: dev int32 [T,K].  token_src_rank: dev int32 [T] home rank of each token, or NULL for

@@ -28,6 +28,8 @@ EXPORTED = (
     "director_dedup_dispatch_tokens", "director_route_dispatch_cost", "director_layer_forward",
     "director_reserve_placements", "director_select_placement", "director_set_profiling_filter",
     "director_selftest_bounded_wait", "director_gemm_sm_mhz", "director_gemm_counters",
+    "director_combine_backward", "director_dispatch_backward", "director_route_backward",
+    "director_expert_ffn_checkpoint", "director_checkpoint_decode",
 )
 
 REPLICA_ROUND_ROBIN, REPLICA_LOCAL_FIRST = 0, 1
@@ -88,6 +90,11 @@ def load_library(rebuild_if_stale: bool = True) -> ctypes.CDLL:
     lib.director_gemm_sm_mhz.argtypes = [vp, c_int32, POINTER(c_double)]
     lib.director_gemm_sm_mhz.restype = c_double
     lib.director_gemm_counters.argtypes = [vp, c_int32, POINTER(c_int64)]
+    lib.director_combine_backward.argtypes = [vp, c_int32] + [vp] * 7
+    lib.director_dispatch_backward.argtypes = [vp, c_int32] + [vp] * 5
+    lib.director_route_backward.argtypes = [vp, c_int32] + [vp] * 5
+    lib.director_expert_ffn_checkpoint.argtypes = [vp, c_int32] + [vp] * 16
+    lib.director_checkpoint_decode.argtypes = [vp, c_int32, c_int32] + [vp] * 5
     lib.director_kernel_time.argtypes = [vp, c_char_p, POINTER(c_int64)]
     lib.director_kernel_time.restype = c_double
     lib.director_status_string.argtypes = [c_int]
@@ -106,6 +113,21 @@ def _ptr(t):
     if hasattr(t, "data_ptr"):
         return t.data_ptr()
     return t.ctypes.data
+
+
+def _need(where: str, **tensors):
+    """Checks the tensors of a training call: name = (tensor, dtype name, elements).  The C entry points see bare addresses; a
+    tensor of another type, a strided view or one too short would be read as something else."""
+    for name, (t, dtype, numel) in tensors.items():
+        if str(t.dtype) != dtype:
+            raise TypeError(f"{where}: {name} is {t.dtype}, {dtype} is needed")
+        if not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{where}: {name} has to be a contiguous CUDA tensor")
+        if t.numel() < numel:
+            raise ValueError(f"{where}: {name} has {t.numel()} elements, {numel} are needed")
+
+
+_BF16, _F32, _I32, _I8, _U8 = "torch.bfloat16", "torch.float32", "torch.int32", "torch.int8", "torch.uint8"
 
 
 def _stream():
@@ -206,6 +228,59 @@ class Director:
     def combine(self, T, yp, inv_row, topk_w, y_shared, y):
         _check(self.lib.director_combine(self._ctx, T, _ptr(yp), _ptr(inv_row), _ptr(topk_w), _ptr(y_shared),
                                          _ptr(y), _stream()), "director_combine")
+
+    # -- backward pass -------------------------------------------------------------------------
+    def combine_backward(self, T, dy, yp, inv_row, topk_w, dyp, dtopk_w):
+        """Gradient of combine: dyp = each row's weight times its token's dy, dtopk_w = the dot products of dy and yp."""
+        TK, H = T * self.shape.K, self.shape.H
+        _need("combine_backward", dy=(dy, _BF16, T * H), yp=(yp, _BF16, TK * H), inv_row=(inv_row, _I32, TK),
+              topk_w=(topk_w, _F32, TK), dyp=(dyp, _BF16, TK * H), dtopk_w=(dtopk_w, _F32, TK))
+        _check(self.lib.director_combine_backward(self._ctx, T, _ptr(dy), _ptr(yp), _ptr(inv_row), _ptr(topk_w), _ptr(dyp),
+                                                  _ptr(dtopk_w), _stream()), "director_combine_backward")
+
+    def dispatch_backward(self, T, dxp, inv_row, dx_shared, dx):
+        """Gradient of dispatch's row copies: dx = the sum of a token's rows of dxp (+ dx_shared, which may be None)."""
+        TK, H = T * self.shape.K, self.shape.H
+        _need("dispatch_backward", dxp=(dxp, _BF16, TK * H), inv_row=(inv_row, _I32, TK), dx=(dx, _BF16, T * H),
+              **({} if dx_shared is None else {"dx_shared": (dx_shared, _BF16, T * H)}))
+        _check(self.lib.director_dispatch_backward(self._ctx, T, _ptr(dxp), _ptr(inv_row), _ptr(dx_shared), _ptr(dx),
+                                                   _stream()), "director_dispatch_backward")
+
+    def route_backward(self, T, topk_idx, topk_w, dtopk_w, dlogits):
+        """Gradient of route: dlogits [T,E], zero where an expert was not chosen."""
+        TK = T * self.shape.K
+        _need("route_backward", topk_idx=(topk_idx, _I32, TK), topk_w=(topk_w, _F32, TK), dtopk_w=(dtopk_w, _F32, TK),
+              dlogits=(dlogits, _F32, T * self.shape.E))
+        _check(self.lib.director_route_backward(self._ctx, T, _ptr(topk_idx), _ptr(topk_w), _ptr(dtopk_w), _ptr(dlogits),
+                                                _stream()), "director_route_backward")
+
+    def expert_ffn_checkpoint(self, T, xp, seg_offsets, w_gate, w_up, w_down, codes, exps, yp, x=None, ws_gate=None,
+                              ws_up=None, ws_down=None, codes_shared=None, exps_shared=None, y_shared=None):
+        """expert_ffn for training: also keeps the gate and up values in 8 bits (codes int8 [T*K,F,2], exps uint8
+        [F/16,T*K,2]; the shared experts' likewise) for expert_ffn_backward."""
+        s = self.shape
+        TK = T * s.K
+        need = dict(xp=(xp, _BF16, TK * s.H), seg_offsets=(seg_offsets, _I32, s.R * s.C_max + 1),
+                    w_gate=(w_gate, _BF16, s.E * s.F * s.H), w_up=(w_up, _BF16, s.E * s.F * s.H),
+                    w_down=(w_down, _BF16, s.E * s.F * s.H), codes=(codes, _I8, 2 * TK * s.F),
+                    exps=(exps, _U8, TK * s.F // 8), yp=(yp, _BF16, TK * s.H))
+        if s.S > 0 and x is not None:
+            SF = s.S * s.F
+            need.update(x=(x, _BF16, T * s.H), ws_gate=(ws_gate, _BF16, SF * s.H), ws_up=(ws_up, _BF16, SF * s.H),
+                        ws_down=(ws_down, _BF16, SF * s.H), codes_shared=(codes_shared, _I8, 2 * T * SF),
+                        exps_shared=(exps_shared, _U8, T * SF // 8), y_shared=(y_shared, _BF16, T * s.H))
+        _need("expert_ffn_checkpoint", **need)
+        _check(self.lib.director_expert_ffn_checkpoint(
+            self._ctx, T, _ptr(xp), _ptr(seg_offsets), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(codes), _ptr(exps), _ptr(yp),
+            _ptr(x), _ptr(ws_gate), _ptr(ws_up), _ptr(ws_down), _ptr(codes_shared), _ptr(exps_shared), _ptr(y_shared),
+            _stream()), "director_expert_ffn_checkpoint")
+
+    def checkpoint_decode(self, rows, F, codes, exps, gate, up):
+        """The values that a checkpoint of `rows` rows of F features stands for, into gate and up (bf16 [rows,F])."""
+        _need("checkpoint_decode", codes=(codes, _I8, 2 * rows * F), exps=(exps, _U8, rows * F // 8), gate=(gate, _BF16, rows * F),
+              up=(up, _BF16, rows * F))
+        _check(self.lib.director_checkpoint_decode(self._ctx, rows, F, _ptr(codes), _ptr(exps), _ptr(gate), _ptr(up), _stream()),
+               "director_checkpoint_decode")
 
     def placement_cost(self, T, topk_idx, token_src_rank, workload, rank_load, dispatch_tokens, dispatch_bytes):
         _check(self.lib.director_placement_cost(self._ctx, T, _ptr(topk_idx), _ptr(token_src_rank), _ptr(workload),

@@ -455,6 +455,85 @@ int director_combine(director_ctx* ctx, int32_t T, const void* yp, const int32_t
     return launch_combine(ctx, T, yp, inv_row, topk_w, y_shared, y, as_stream(stream));
 }
 
+int director_combine_backward(director_ctx* ctx, int32_t T, const void* dy, const void* yp, const int32_t* inv_row,
+                              const float* topk_w, void* dyp, float* dtopk_w, void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PTR(dy);
+    REQUIRE_PTR(yp);
+    REQUIRE_PTR(inv_row);
+    REQUIRE_PTR(topk_w);
+    REQUIRE_PTR(dyp);
+    REQUIRE_PTR(dtopk_w);
+    return launch_combine_backward(ctx, T, dy, yp, inv_row, topk_w, dyp, dtopk_w, as_stream(stream));
+}
+
+int director_dispatch_backward(director_ctx* ctx, int32_t T, const void* dxp, const int32_t* inv_row, const void* dx_shared,
+                               void* dx, void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PTR(dxp);
+    REQUIRE_PTR(inv_row);
+    REQUIRE_PTR(dx);
+    if (dx_shared != nullptr && !aligned16(dx_shared)) return DIRECTOR_ERR_INVALID_ARG;
+    return launch_combine(ctx, T, dxp, inv_row, nullptr, dx_shared, dx, as_stream(stream));
+}
+
+int director_route_backward(director_ctx* ctx, int32_t T, const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
+                            float* dlogits, void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PTR(topk_idx);
+    REQUIRE_PTR(topk_w);
+    REQUIRE_PTR(dtopk_w);
+    REQUIRE_PTR(dlogits);
+    return launch_route_backward(ctx, T, topk_idx, topk_w, dtopk_w, dlogits, as_stream(stream));
+}
+
+int director_expert_ffn_checkpoint(director_ctx* ctx, int32_t T, const void* xp, const int32_t* seg_offsets, const void* w_gate,
+                                   const void* w_up, const void* w_down, int8_t* codes, uint8_t* exps, void* yp, const void* x,
+                                   const void* ws_gate, const void* ws_up, const void* ws_down, int8_t* codes_shared,
+                                   uint8_t* exps_shared, void* y_shared, void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PLACEMENT(ctx);
+    REQUIRE_PTR(xp);
+    REQUIRE_PTR(seg_offsets);
+    REQUIRE_PTR(w_gate);
+    REQUIRE_PTR(w_up);
+    REQUIRE_PTR(w_down);
+    REQUIRE_PTR(codes);
+    REQUIRE_PTR(exps);
+    REQUIRE_PTR(yp);
+    if (ctx->shape.S > 0 && x != nullptr) {
+        REQUIRE_PTR(x);
+        REQUIRE_PTR(ws_gate);
+        REQUIRE_PTR(ws_up);
+        REQUIRE_PTR(ws_down);
+        REQUIRE_PTR(codes_shared);
+        REQUIRE_PTR(exps_shared);
+        REQUIRE_PTR(y_shared);
+    }
+    if (ctx->ffn_variant != 2) return DIRECTOR_ERR_UNSUPPORTED;
+    const Checkpoint kept{codes, reinterpret_cast<uint16_t*>(exps), T * ctx->shape.K};
+    const Checkpoint kept_shared{codes_shared, reinterpret_cast<uint16_t*>(exps_shared), T};
+    return launch_expert_ffn_checkpoint(ctx, T, xp, seg_offsets, w_gate, w_up, w_down, kept, yp, x, ws_gate, ws_up, ws_down,
+                                        kept_shared, y_shared, as_stream(stream));
+}
+
+int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const int8_t* codes, const uint8_t* exps, void* gate,
+                               void* up, void* stream) {
+    REQUIRE_CTX(ctx);
+    if (rows < 1 || F < kCheckpointBlock || F % kCheckpointBlock != 0) return DIRECTOR_ERR_INVALID_ARG;
+    if ((long long)rows * (F / kCheckpointBlock) >= (1ll << 31)) return DIRECTOR_ERR_INVALID_ARG;
+    REQUIRE_PTR(codes);
+    REQUIRE_PTR(exps);
+    REQUIRE_PTR(gate);
+    REQUIRE_PTR(up);
+    const Checkpoint kept{const_cast<int8_t*>(codes), reinterpret_cast<uint16_t*>(const_cast<uint8_t*>(exps)), rows};
+    return launch_checkpoint_decode(ctx, rows, F, kept, gate, up, as_stream(stream));
+}
+
 int director_placement_cost(director_ctx* ctx, int32_t T, const int32_t* topk_idx, const int32_t* token_src_rank,
                             int64_t* workload, int64_t* rank_load, int64_t* dispatch_tokens, uint64_t* dispatch_bytes,
                             void* stream) {

@@ -6,6 +6,9 @@
 // One warp per (token, 1 KB column slice): each lane owns 2 x 8 consecutive bf16 columns, gathers
 // them from the K rows with 16-byte loads (all K loads in flight), accumulates in fp32 in slot
 // order and writes 16 bytes.  HBM-bound gather: 2HK + 8K (+2H) bytes read, 2H written per token.
+//
+// With topk_w == nullptr all weights are one: the gradient of the dispatch (a token's row was copied to its K assignments, so
+// its gradient is the sum of theirs, plus the shared experts').
 #include "director_common.cuh"
 
 #include <cuda_bf16.h>
@@ -49,7 +52,7 @@ combine_kernel(const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row
     float my_w = 0.0f;
     if (lane < K) {
         my_row = __ldg(inv_row + (size_t)t * K + lane);
-        my_w = __ldg(topk_w + (size_t)t * K + lane);
+        my_w = topk_w ? __ldg(topk_w + (size_t)t * K + lane) : 1.0f;
     }
     float acc[kVecPerLane][8];
 #pragma unroll
@@ -102,13 +105,13 @@ combine_kernel(const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row
 
 int launch_combine(director_ctx* ctx, int T, const void* yp, const int32_t* inv_row, const float* topk_w,
                    const void* y_shared, void* y, cudaStream_t st) {
-    StageScope stage(ctx, st, "stage_combine");
+    StageScope stage(ctx, st, topk_w ? "stage_combine" : "stage_dispatch_backward");
     const director_shape& s = ctx->shape;
     const int row_vec = s.H * 2 / 16;
     const int slices = (row_vec + kCombineSliceVec - 1) / kCombineSliceVec;
     const long long items = (long long)T * slices;
     const unsigned grid = (unsigned)((items + kCombineWarps - 1) / kCombineWarps);
-    LaunchScope scope(ctx, st, "combine_kernel");
+    LaunchScope scope(ctx, st, topk_w ? "combine_kernel" : "dispatch_backward_kernel");
 #define COMBINE_LAUNCH(KT)                                                                                      \
     launch_chained(combine_kernel<KT>, dim3(grid), dim3(kCombineWarps * 32), 0, st, static_cast<const uint4*>(yp),  \
                    inv_row, topk_w, static_cast<const uint4*>(y_shared), static_cast<uint4*>(y), T, (int)s.K, row_vec,  \

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "director.h"
+#include "director_checkpoint.cuh"
 
 namespace director {
 
@@ -256,6 +257,16 @@ int launch_expert_ffn(director_ctx*, int T, const void* xp, const int32_t* row_t
                       const void* w_gate, const void* w_up, const void* w_down, void* yp, const void* x,
                       const void* ws_gate, const void* ws_up, const void* ws_down, void* y_shared, cudaStream_t);
 bool ffn_streams_weights(const director_ctx*, int T);   // batch small enough for the weight-streaming FFN kernels
+int launch_expert_ffn_checkpoint(director_ctx*, int T, const void* xp, const int32_t* seg_offsets, const void* w_gate,
+                                 const void* w_up, const void* w_down, const Checkpoint& kept, void* yp, const void* x,
+                                 const void* ws_gate, const void* ws_up, const void* ws_down, const Checkpoint& kept_shared,
+                                 void* y_shared, cudaStream_t);
+int launch_combine_backward(director_ctx*, int T, const void* dy, const void* yp, const int32_t* inv_row, const float* topk_w,
+                            void* dyp, float* dtopk_w, cudaStream_t);
+int launch_route_backward(director_ctx*, int T, const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
+                          float* dlogits, cudaStream_t);
+int launch_checkpoint_decode(director_ctx*, int rows, int F, const Checkpoint& kept, void* gate, void* up, cudaStream_t);
+// topk_w == nullptr: all weights are one (the gradient of the dispatch)
 int launch_combine(director_ctx*, int T, const void* yp, const int32_t* inv_row, const float* topk_w,
                    const void* y_shared, void* y, cudaStream_t);
 

@@ -33,7 +33,8 @@ int ffn_swap_init(director_ctx* ctx);   // director_ffn_swap.cu
 int ffn_pass_swap(director_ctx* ctx, const void* in, uint64_t in_rows, const int32_t* gather_rows, uint64_t rows,
                   const int32_t* seg_offsets, const int32_t* slot_expert, int G, const void* w_gate, const void* w_up,
                   const void* w_down, uint64_t n_experts, int Fw, void* hidden, void* out, unsigned int* counters,
-                  const DenseFfn* dense, uint64_t max_seg_rows, const FusedCombine* fc, cudaStream_t st);
+                  const DenseFfn* dense, uint64_t max_seg_rows, const FusedCombine* fc, const Checkpoint* kept,
+                  const Checkpoint* dense_kept, cudaStream_t st);
 int ffn_small_init(director_ctx* ctx);  // director_ffn_small.cu
 bool ffn_small_applies(const director_ctx* ctx, int T, int Fw);
 int ffn_pass_small(director_ctx* ctx, const void* in, const int32_t* gather_rows, const int32_t* seg_offsets, const int32_t* slot_expert, int G,
@@ -290,7 +291,7 @@ int ffn_pass(director_ctx* ctx, const void* in, uint64_t in_rows, const int32_t*
              uint64_t max_seg_rows, cudaStream_t st) {
     if (ctx->ffn_variant == 2) {
         const int rc = ffn_pass_swap(ctx, in, in_rows, gather_rows, rows, seg_offsets, slot_expert, G, w_gate, w_up, w_down,
-                                     n_experts, Fw, hidden, out, counters, nullptr, max_seg_rows, nullptr, st);
+                                     n_experts, Fw, hidden, out, counters, nullptr, max_seg_rows, nullptr, nullptr, nullptr, st);
         if (rc != DIRECTOR_ERR_UNSUPPORTED) return rc;   // weight arrays not expressible as one map: tile scheme 0
     }
     if (gather_rows != nullptr) return DIRECTOR_ERR_UNSUPPORTED;   // only the weight-stationary scheme gathers
@@ -361,7 +362,7 @@ int launch_expert_ffn(director_ctx* ctx, int T, const void* xp, const int32_t* r
         // routed and shared experts in the same two launches: the shared experts' work items follow the routed ones
         const DenseFfn dense{x, (uint64_t)T, ws_gate, ws_up, ws_down, s.S * s.F, ctx->d_hidden_shared, y_shared};
         const int rc = ffn_pass_swap(ctx, xp, A, nullptr, A, seg_offsets, ctx->d_slot_expert, ctx->G, w_gate, w_up, w_down,
-                                     s.E, s.F, ctx->d_hidden, yp, ctx->d_sched, &dense, (uint64_t)T, nullptr, st);
+                                     s.E, s.F, ctx->d_hidden, yp, ctx->d_sched, &dense, (uint64_t)T, nullptr, nullptr, nullptr, st);
         if (rc != DIRECTOR_ERR_UNSUPPORTED) return rc;    // a weight pair not expressible as one map: separate passes
     }
     int rc = row_token ? ffn_pass(ctx, x, (uint64_t)T, row_token, A, seg_offsets, ctx->d_slot_expert, ctx->G, w_gate, w_up,
@@ -377,6 +378,24 @@ int launch_expert_ffn(director_ctx* ctx, int T, const void* xp, const int32_t* r
     // The S shared experts as one FFN of width S*F over all T rows of x (a single segment, "expert" 0).
     return ffn_pass(ctx, x, (uint64_t)T, nullptr, (uint64_t)T, ctx->d_one_seg, ctx->d_zero_expert, 1, ws_gate, ws_up,
                     ws_down, 1, s.S * s.F, ctx->d_hidden_shared, y_shared, ctx->d_sched + 2, (uint64_t)T, st);
+}
+
+// The forward pass of training: launch_expert_ffn on the tensor-core kernels at every batch size, the gate|up projection
+// writing the 8-bit checkpoint beside the activations.  Same products in the same order: yp and y_shared are the bits that
+// launch_expert_ffn gives on those kernels.
+int launch_expert_ffn_checkpoint(director_ctx* ctx, int T, const void* xp, const int32_t* seg_offsets, const void* w_gate,
+                                 const void* w_up, const void* w_down, const Checkpoint& kept, void* yp, const void* x,
+                                 const void* ws_gate, const void* ws_up, const void* ws_down, const Checkpoint& kept_shared,
+                                 void* y_shared, cudaStream_t st) {
+    StageScope stage(ctx, st, "stage_expert_ffn");
+    const director_shape& s = ctx->shape;
+    const uint64_t A = (uint64_t)T * s.K;
+    const bool shared = s.S > 0 && x != nullptr;
+    if (cudaMemsetAsync(ctx->d_sched, 0, 4 * sizeof(unsigned int), st) != cudaSuccess) return DIRECTOR_ERR_CUDA;
+    const DenseFfn dense{x, (uint64_t)T, ws_gate, ws_up, ws_down, s.S * s.F, ctx->d_hidden_shared, y_shared};
+    return ffn_pass_swap(ctx, xp, A, nullptr, A, seg_offsets, ctx->d_slot_expert, ctx->G, w_gate, w_up, w_down, s.E, s.F,
+                         ctx->d_hidden, yp, ctx->d_sched, shared ? &dense : nullptr, (uint64_t)T, nullptr, &kept,
+                         shared ? &kept_shared : nullptr, st);
 }
 
 namespace {
@@ -443,7 +462,7 @@ int launch_expert_ffn_combine(director_ctx* ctx, int T, const void* xp, const in
         const DenseFfn dense{x, (uint64_t)T, ws_gate, ws_up, ws_down, s.S * s.F, ctx->d_hidden_shared, ctx->e_y_shared};
         const int rc = ffn_pass_swap(ctx, xp, A, nullptr, A, seg_offsets, ctx->d_slot_expert, ctx->G, w_gate, w_up, w_down,
                                      s.E, s.F, ctx->d_hidden, nullptr, ctx->d_sched, shared ? &dense : nullptr, (uint64_t)T,
-                                     &fc, st);
+                                     &fc, nullptr, nullptr, st);
         if (rc != DIRECTOR_OK) return rc;
     }
     StageScope stage(ctx, st, "stage_combine");

@@ -209,6 +209,9 @@ struct SwapParams {
     // cycles / ns is the SM clock the kernel really ran at, which a host-side sampler with millisecond resolution
     // cannot see), and where the MMA-issuing thread and one epilogue warp spent their cycles.  nullptr: nothing is read.
     unsigned long long* clock_out;
+    // ALT_CHECKPOINT only: the 8-bit gate and up values of the grouped and of the dense problem (see Checkpoint)
+    Checkpoint kept;
+    Checkpoint dense_kept;
 };
 
 struct SwapTile {
@@ -281,13 +284,18 @@ struct SwapWalker {
 // GEMM-1 (MODE 0), GATHER: the token rows are not read from a permuted copy but gathered straight from the layer
 // input x through row_token - tm_x then describes x with a one-row box and the whole producer warp issues the
 // loads, four rows per lane - so the dispatch step needs no row copies at all.
-template <int MODE, int EPI_GROUPS, bool ALT, int S_STAGES>
+// GEMM-1, ALT_CHECKPOINT: the forward pass of training - besides the SwiGLU activations the epilogue writes every gate and up
+// value in 8 bits (see checkpoint_exponent), which is what the backward pass reads instead of repeating this GEMM.
+constexpr int ALT_NONE = 0, ALT_FUSED = 1, ALT_CHECKPOINT = 2;
+
+template <int MODE, int EPI_GROUPS, int ALT, int S_STAGES>
 __global__ void __launch_bounds__(96 + 128 * EPI_GROUPS, 1)
 grouped_gemm_swap_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                          const __grid_constant__ CUtensorMap tm_w2 /* dense problem */,
                          const __grid_constant__ CUtensorMap tm_x2, const SwapParams p) {
-    constexpr bool GATHER = ALT && MODE == 0;               // token rows gathered from x
-    constexpr bool COMBINE = ALT && MODE == 1;              // combining epilogue
+    constexpr bool GATHER = ALT == ALT_FUSED && MODE == 0;  // token rows gathered from x
+    constexpr bool COMBINE = ALT == ALT_FUSED && MODE == 1; // combining epilogue
+    constexpr bool CHECKPOINT = ALT == ALT_CHECKPOINT && MODE == 0;
     extern __shared__ uint8_t smem_raw[];
     chain_prologue();
     const uint32_t raw = smem_u32(smem_raw);
@@ -664,6 +672,26 @@ grouped_gemm_swap_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
                     tmem_ld_wait();
                     uint16_t* ptr = ocol + (size_t)c * out_pitch;       // my token of pair m is row c + 2m (+1 if odd)
                     const int rem = t.valid - c - (odd ? 1 : 0);        // store pair m iff 2m < rem
+                    if constexpr (CHECKPOINT) {
+                        // this warp holds the gate and up values of 16 features - one block of the checkpoint - for 32 tokens:
+                        // per token, two warp-wide maxima of the magnitudes' bit patterns give the block's two exponents
+                        const Checkpoint& kept = t.prob ? p.dense_kept : p.kept;
+                        const int chunk_row = t.row0 + c, in_tile = t.valid - c;
+                        int8_t* code = kept.codes + (size_t)chunk_row * (2 * out_pitch) + 2 * f + (i_am_gate ? 0 : 1);
+                        uint32_t exps = 0;                              // lane j keeps token j's pair of exponents
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const uint32_t mag = v[j] & 0x7FFFFFFFu;
+                            const uint32_t eg = checkpoint_exponent(__reduce_max_sync(0xFFFFFFFFu, i_am_gate ? mag : 0u));
+                            const uint32_t eu = checkpoint_exponent(__reduce_max_sync(0xFFFFFFFFu, i_am_gate ? 0u : mag));
+                            if (lane == j) exps = eg | (eu << 8);
+                            if (j < in_tile) *code = (int8_t)checkpoint_code(__uint_as_float(v[j]), i_am_gate ? eg : eu);
+                            code += 2 * out_pitch;
+                        }
+                        if (lane < in_tile)
+                            kept.exps[(size_t)((t.wb * 128 + (int)rank * 64 + quad * 16) / kCheckpointBlock) * kept.rows + chunk_row + lane] =
+                                (uint16_t)exps;
+                    }
 #pragma unroll
                     for (int m = 0; m < 16; ++m) {
                         const float mine = __uint_as_float(odd ? v[2 * m + 1] : v[2 * m]);   // my value at my token
@@ -787,7 +815,7 @@ bool map_interleaved(director_ctx* ctx, CUtensorMap* map, const void* first, uin
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, int EPI_GROUPS, bool GATHER, int STAGES>
+template <int MODE, int EPI_GROUPS, int ALT, int STAGES>
 int launch_swap_n(director_ctx* ctx, const char* name, const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& w2,
                   const CUtensorMap& x2, const SwapParams& p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
@@ -805,39 +833,40 @@ int launch_swap_n(director_ctx* ctx, const char* name, const CUtensorMap& w, con
     cfg.attrs = attr;
     cfg.numAttrs = chain_allowed(st) ? 2 : 1;
     LaunchScope scope(ctx, st, name);
-    return cuda_status(cudaLaunchKernelEx(&cfg, grouped_gemm_swap_kernel<MODE, EPI_GROUPS, GATHER, STAGES>, w, x, w2, x2, p));
+    return cuda_status(cudaLaunchKernelEx(&cfg, grouped_gemm_swap_kernel<MODE, EPI_GROUPS, ALT, STAGES>, w, x, w2, x2, p));
 }
 
 // w2 / x2: the dense problem's maps (any valid map when the launch has none)
-template <int MODE, int EPI_GROUPS, bool GATHER>
+template <int MODE, int EPI_GROUPS, int ALT>
 int launch_swap(director_ctx* ctx, const char* name, const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& w2,
                 const CUtensorMap& x2, const SwapParams& p, bool small, cudaStream_t st) {
-    if constexpr (!GATHER) {
-        if (small) return launch_swap_n<MODE, EPI_GROUPS, GATHER, S_SMALL_STAGES>(ctx, name, w, x, w2, x2, p, st);
+    if constexpr (ALT != ALT_FUSED) {
+        if (small) return launch_swap_n<MODE, EPI_GROUPS, ALT, S_SMALL_STAGES>(ctx, name, w, x, w2, x2, p, st);
     }
-    return swap_stages(p.G, p.slot_order != nullptr) == 7 ? launch_swap_n<MODE, EPI_GROUPS, GATHER, 7>(ctx, name, w, x, w2, x2, p, st)
-                                 : launch_swap_n<MODE, EPI_GROUPS, GATHER, 6>(ctx, name, w, x, w2, x2, p, st);
+    return swap_stages(p.G, p.slot_order != nullptr) == 7 ? launch_swap_n<MODE, EPI_GROUPS, ALT, 7>(ctx, name, w, x, w2, x2, p, st)
+                                 : launch_swap_n<MODE, EPI_GROUPS, ALT, 6>(ctx, name, w, x, w2, x2, p, st);
 }
 
-template <int MODE, int EPI_GROUPS, bool GATHER>
+template <int MODE, int EPI_GROUPS, int ALT>
 bool swap_opt_in() {
-    if constexpr (!GATHER) {
-        if (cudaFuncSetAttribute(grouped_gemm_swap_kernel<MODE, EPI_GROUPS, GATHER, S_SMALL_STAGES>,
+    if constexpr (ALT != ALT_FUSED) {
+        if (cudaFuncSetAttribute(grouped_gemm_swap_kernel<MODE, EPI_GROUPS, ALT, S_SMALL_STAGES>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  swap_smem_bytes(S_SMALL_STAGES, kMaxG, true)) != cudaSuccess)
             return false;
     }
-    return cudaFuncSetAttribute(grouped_gemm_swap_kernel<MODE, EPI_GROUPS, GATHER, 6>,
+    return cudaFuncSetAttribute(grouped_gemm_swap_kernel<MODE, EPI_GROUPS, ALT, 6>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, swap_smem_bytes(6, kMaxG, true)) == cudaSuccess &&
-           cudaFuncSetAttribute(grouped_gemm_swap_kernel<MODE, EPI_GROUPS, GATHER, 7>,
+           cudaFuncSetAttribute(grouped_gemm_swap_kernel<MODE, EPI_GROUPS, ALT, 7>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, S_MAX_SMEM) == cudaSuccess;
 }
 
 }  // namespace
 
 int ffn_swap_init(director_ctx*) {
-    if (!swap_opt_in<0, EPI_GROUPS_GEMM1, false>() || !swap_opt_in<0, EPI_GROUPS_GEMM1, true>() ||
-        !swap_opt_in<1, EPI_GROUPS_GEMM2, false>() || !swap_opt_in<1, EPI_GROUPS_GEMM2, true>())
+    if (!swap_opt_in<0, EPI_GROUPS_GEMM1, ALT_NONE>() || !swap_opt_in<0, EPI_GROUPS_GEMM1, ALT_FUSED>() ||
+        !swap_opt_in<0, EPI_GROUPS_GEMM1, ALT_CHECKPOINT>() || !swap_opt_in<1, EPI_GROUPS_GEMM2, ALT_NONE>() ||
+        !swap_opt_in<1, EPI_GROUPS_GEMM2, ALT_FUSED>())
         return DIRECTOR_ERR_CUDA;
     return DIRECTOR_OK;
 }
@@ -852,12 +881,14 @@ int ffn_swap_init(director_ctx*) {
 // ring also tiles the tokens by 64.
 // fc (optional, not with gather_rows): the down projection combines in its epilogue - `out` is not written; every
 // element of a routed row goes, times the row's gating weight, into fc->y_acc at the row's token (see the kernel's ALT).
+// kept (optional, not with gather_rows): the gate|up projection also writes the 8-bit checkpoint; dense_kept is the dense
+// problem's (with dense and kept).
 // Returns DIRECTOR_ERR_UNSUPPORTED if a pair of weight arrays cannot be described by one interleaving map.
 int ffn_pass_swap(director_ctx* ctx, const void* in, uint64_t in_rows, const int32_t* gather_rows, uint64_t rows,
                   const int32_t* seg_offsets, const int32_t* slot_expert, int G, const void* w_gate, const void* w_up,
                   const void* w_down, uint64_t n_experts, int Fw, void* hidden, void* out,
                   unsigned int* counters /* 2 zeroed work-item counters */, const DenseFfn* dense, uint64_t max_seg_rows,
-                  const FusedCombine* fc, cudaStream_t st) {
+                  const FusedCombine* fc, const Checkpoint* kept, const Checkpoint* dense_kept, cudaStream_t st) {
     const int H = ctx->shape.H;
     // small-batch ring (tiles of 64 tokens, ten stages): when no segment, routed or dense, can be longer than a tile
     const bool small = !gather_rows && !fc && max_seg_rows <= 2u * swap_tok_rows(S_SMALL_STAGES) &&
@@ -872,7 +903,7 @@ int ffn_pass_swap(director_ctx* ctx, const void* in, uint64_t in_rows, const int
     };
     const Interleave ia = interleave(w_gate, w_up);
     if (!ia.ok) return DIRECTOR_ERR_UNSUPPORTED;
-    if ((dense || fc) && gather_rows) return DIRECTOR_ERR_INVALID_ARG;
+    if ((dense || fc || kept) && gather_rows) return DIRECTOR_ERR_INVALID_ARG;
     CUtensorMap m_in, m_gu, m_h, m_d;
     if (!map_2d(ctx, &m_in, in, in_rows, H, gather_rows ? 1 : tok_box) || !map_2d(ctx, &m_h, hidden, rows, Fw, tok_box) ||
         !map_2d(ctx, &m_d, w_down, n_experts * H, Fw))
@@ -896,17 +927,18 @@ int ffn_pass_swap(director_ctx* ctx, const void* in, uint64_t in_rows, const int
     unsigned long long* const clk = ctx->gemm_stats ? ctx->d_gemm_clock : nullptr;
     SwapParams p1{seg_offsets, slot_expert, order, G, Fw / 128, H / BLOCK_K, Fw, Fw, ia.gate_first ? 1 : 0, hidden, ctx->d_status,
                   counters, gather_rows, nullptr, d_rows, d_Fw / 128, H / BLOCK_K, d_Fw, id.gate_first ? 1 : 0,
-                  dense ? dense->hidden : nullptr, clk};
-    int rc = gather_rows ? launch_swap<0, EPI_GROUPS_GEMM1, true>(ctx, "grouped_gemm_swiglu_kernel", m_gu, m_in, d_gu, d_in, p1, false, st)
-                         : launch_swap<0, EPI_GROUPS_GEMM1, false>(ctx, "grouped_gemm_swiglu_kernel", m_gu, m_in, d_gu, d_in, p1, small, st);
+                  dense ? dense->hidden : nullptr, clk, kept ? *kept : Checkpoint{}, dense && dense_kept ? *dense_kept : Checkpoint{}};
+    int rc = gather_rows ? launch_swap<0, EPI_GROUPS_GEMM1, ALT_FUSED>(ctx, "grouped_gemm_swiglu_kernel", m_gu, m_in, d_gu, d_in, p1, false, st)
+             : kept ? launch_swap<0, EPI_GROUPS_GEMM1, ALT_CHECKPOINT>(ctx, "grouped_gemm_checkpoint_kernel", m_gu, m_in, d_gu, d_in, p1, small, st)
+                    : launch_swap<0, EPI_GROUPS_GEMM1, ALT_NONE>(ctx, "grouped_gemm_swiglu_kernel", m_gu, m_in, d_gu, d_in, p1, small, st);
     if (rc != DIRECTOR_OK) return rc;
     // with fc the routed experts' output is not Yp but the fp32 accumulator of y (pitch H floats), see the kernel's ALT
     SwapParams p2{seg_offsets, slot_expert, order, G, H / 256, Fw / BLOCK_K, H, H, 1, fc ? static_cast<void*>(fc->y_acc) : out,
                   ctx->d_status, counters + 1, fc ? fc->row_token : nullptr, fc ? fc->row_weight : nullptr,
                   d_rows, H / 256, d_Fw / BLOCK_K, H, 1, dense ? dense->out : nullptr,
-                  clk ? clk + (size_t)kGemmClockWords * kGemmClockCtas : nullptr};
-    if (fc) return launch_swap<1, EPI_GROUPS_GEMM2, true>(ctx, "grouped_gemm_down_fused_kernel", m_d, m_h, d_d, d_h, p2, false, st);
-    return launch_swap<1, EPI_GROUPS_GEMM2, false>(ctx, "grouped_gemm_down_kernel", m_d, m_h, d_d, d_h, p2, small, st);
+                  clk ? clk + (size_t)kGemmClockWords * kGemmClockCtas : nullptr, {}, {}};
+    if (fc) return launch_swap<1, EPI_GROUPS_GEMM2, ALT_FUSED>(ctx, "grouped_gemm_down_fused_kernel", m_d, m_h, d_d, d_h, p2, false, st);
+    return launch_swap<1, EPI_GROUPS_GEMM2, ALT_NONE>(ctx, "grouped_gemm_down_kernel", m_d, m_h, d_d, d_h, p2, small, st);
 }
 
 }  // namespace director

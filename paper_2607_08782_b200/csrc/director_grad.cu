@@ -1,0 +1,173 @@
+// The row-moving and gating half of the layer's backward pass (the forward's Section II-A weighted sum and gate, Section II-B
+// exchanges, differentiated; the paper itself serves and does not train).  The expert products' gradients are in
+// director_ffn_grad.cu.  All four kernels move data once and compute almost nothing: HBM bounds them.
+#include "director_common.cuh"
+
+#include <cuda_bf16.h>
+
+namespace director {
+
+namespace {
+
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// ---- gradient of the combine -------------------------------------------------------------------------------------
+//
+//   y[t] = sum_s w[t,s] yp[r(t,s)]:   dyp[r(t,s)] = w[t,s] dy[t],   dw[t,s] = <dy[t], yp[r(t,s)]>
+//
+// One warp per assignment (t, s): it reads dy[t] and the row of yp once, writes the row of dyp, and the dot product is a sum
+// over its lanes - no atomics, so dw has the same bits on every run.  The K warps of a token sit next to each other in a CTA,
+// so that dy[t] comes from HBM once and from L1 after that.
+constexpr int kRowWarps = 8;
+
+__global__ void __launch_bounds__(kRowWarps * 32)
+combine_backward_kernel(const uint4* __restrict__ dy, const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row,
+                        const float* __restrict__ topk_w, uint4* __restrict__ dyp, float* __restrict__ dtopk_w, int A, int K,
+                        int row_vec, int32_t* status) {
+    chain_prologue();
+    const int lane = threadIdx.x & 31;
+    const long long item = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    if (item >= A) return;
+    const int t = (int)(item / K);
+    const int row = __ldg(inv_row + item);
+    const float w = __ldg(topk_w + item);
+    if ((unsigned)row >= (unsigned)A) {       // an assignment that the dispatch skipped (-1), or no row of this batch
+        if (lane == 0) {
+            dtopk_w[item] = 0.0f;
+            if (row >= 0) director_set_status(status, DIRECTOR_ERR_BAD_INDEX);
+        }
+        return;
+    }
+    const uint4* g = dy + (size_t)t * row_vec;
+    const uint4* y = yp + (size_t)row * row_vec;
+    uint4* o = dyp + (size_t)row * row_vec;
+    float dot = 0.0f;
+    for (int v = lane; v < row_vec; v += 32) {
+        const uint4 a = __ldg(g + v), b = __ldcs(y + v);
+        const uint32_t ga[4] = {a.x, a.y, a.z, a.w}, yb[4] = {b.x, b.y, b.z, b.w};
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            dot = fmaf(bf16_lo(ga[i]), bf16_lo(yb[i]), dot);
+            dot = fmaf(bf16_hi(ga[i]), bf16_hi(yb[i]), dot);
+            r[i] = pack_bf16x2(w * bf16_lo(ga[i]), w * bf16_hi(ga[i]));
+        }
+        o[v] = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, d);
+    if (lane == 0) dtopk_w[item] = dot;
+}
+
+// ---- gradient of the gate ----------------------------------------------------------------------------------------
+//
+//   w = softmax over the K chosen logits:   dlogits[t, idx[t,s]] = w[t,s] (dw[t,s] - sum_j w[t,j] dw[t,j]),  0 elsewhere
+//
+// A CTA owns 16 tokens: it clears their rows of dlogits in shared memory, puts the K values of each into place and streams
+// the tile out as one contiguous, 16-byte aligned block (16 rows of 4 E bytes are a multiple of 16 bytes for every E).
+constexpr int kGateTokens = 16;
+constexpr int kGateThreads = 128;
+static_assert(kGateTokens * kMaxK <= kGateThreads, "one thread per (token, choice)");
+
+__global__ void __launch_bounds__(kGateThreads)
+route_backward_kernel(const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w, const float* __restrict__ dtopk_w,
+                      float* __restrict__ dlogits, int T, int K, int E, int32_t* status) {
+    extern __shared__ float tile[];                       // [kGateTokens * E]
+    __shared__ int s_idx[kGateTokens * kMaxK];
+    __shared__ float s_w[kGateTokens * kMaxK], s_dw[kGateTokens * kMaxK];
+    chain_prologue();
+    const int t0 = blockIdx.x * kGateTokens, n = min(kGateTokens, T - t0);
+    if ((int)threadIdx.x < n * K) {
+        const size_t i = (size_t)t0 * K + threadIdx.x;
+        s_idx[threadIdx.x] = __ldg(topk_idx + i);
+        s_w[threadIdx.x] = __ldg(topk_w + i);
+        s_dw[threadIdx.x] = __ldg(dtopk_w + i);
+    }
+    for (int i = threadIdx.x; i < n * E; i += kGateThreads) tile[i] = 0.0f;
+    __syncthreads();
+    if ((int)threadIdx.x < n) {
+        const int base = threadIdx.x * K;
+        float mean = 0.0f;
+        for (int s = 0; s < K; ++s) mean = fmaf(s_w[base + s], s_dw[base + s], mean);
+        for (int s = 0; s < K; ++s) {
+            const int e = s_idx[base + s];
+            if ((unsigned)e < (unsigned)E) tile[threadIdx.x * E + e] += s_w[base + s] * (s_dw[base + s] - mean);
+            else director_set_status(status, DIRECTOR_ERR_BAD_INDEX);
+        }
+    }
+    __syncthreads();
+    float* out = dlogits + (size_t)t0 * E;
+    const int total = n * E, vecs = total / 4;
+    for (int i = threadIdx.x; i < vecs; i += kGateThreads)
+        reinterpret_cast<float4*>(out)[i] = reinterpret_cast<const float4*>(tile)[i];
+    for (int i = 4 * vecs + threadIdx.x; i < total; i += kGateThreads) out[i] = tile[i];
+}
+
+// ---- the 8-bit checkpoint as numbers -----------------------------------------------------------------------------
+//
+// One thread per block of 16 features of a row: 32 bytes of codes and two exponents in, 16 gate and 16 up values out in bf16
+// (seven bits and a sign times a power of two: exact).
+__global__ void __launch_bounds__(256)
+checkpoint_decode_kernel(const uint4* __restrict__ codes, const uint16_t* __restrict__ exps, uint4* __restrict__ gate,
+                         uint4* __restrict__ up, int rows, int blocks) {
+    chain_prologue();
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= (long long)rows * blocks) return;
+    const int row = (int)(i / blocks), b = (int)(i % blocks);
+    const uint32_t e = __ldg(exps + (size_t)b * rows + row);
+    const float sg = checkpoint_scale(e & 255u), su = checkpoint_scale(e >> 8);
+    const uint4 c0 = __ldcs(codes + 2 * i), c1 = __ldcs(codes + 2 * i + 1);
+    const uint32_t c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+    uint32_t g[8], u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        g[j] = pack_bf16x2((float)(int8_t)c[j] * sg, (float)(int8_t)(c[j] >> 16) * sg);
+        u[j] = pack_bf16x2((float)(int8_t)(c[j] >> 8) * su, (float)(int8_t)(c[j] >> 24) * su);
+    }
+    gate[2 * i] = make_uint4(g[0], g[1], g[2], g[3]);
+    gate[2 * i + 1] = make_uint4(g[4], g[5], g[6], g[7]);
+    up[2 * i] = make_uint4(u[0], u[1], u[2], u[3]);
+    up[2 * i + 1] = make_uint4(u[4], u[5], u[6], u[7]);
+}
+
+}  // namespace
+
+int launch_combine_backward(director_ctx* ctx, int T, const void* dy, const void* yp, const int32_t* inv_row,
+                            const float* topk_w, void* dyp, float* dtopk_w, cudaStream_t st) {
+    StageScope stage(ctx, st, "stage_combine_backward");
+    const director_shape& s = ctx->shape;
+    const int A = T * s.K;
+    const unsigned grid = ((unsigned)A + kRowWarps - 1) / kRowWarps;
+    LaunchScope scope(ctx, st, "combine_backward_kernel");
+    return cuda_status(launch_chained(combine_backward_kernel, dim3(grid), dim3(kRowWarps * 32), 0, st,
+                                      static_cast<const uint4*>(dy), static_cast<const uint4*>(yp), inv_row, topk_w,
+                                      static_cast<uint4*>(dyp), dtopk_w, A, s.K, s.H * 2 / 16, ctx->d_status));
+}
+
+int launch_route_backward(director_ctx* ctx, int T, const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
+                          float* dlogits, cudaStream_t st) {
+    StageScope stage(ctx, st, "stage_route_backward");
+    const director_shape& s = ctx->shape;
+    const unsigned grid = (unsigned)((T + kGateTokens - 1) / kGateTokens);
+    LaunchScope scope(ctx, st, "route_backward_kernel");
+    return cuda_status(launch_chained(route_backward_kernel, dim3(grid), dim3(kGateThreads),
+                                      sizeof(float) * (size_t)kGateTokens * s.E, st, topk_idx, topk_w, dtopk_w, dlogits, T, s.K,
+                                      s.E, ctx->d_status));
+}
+
+int launch_checkpoint_decode(director_ctx* ctx, int rows, int F, const Checkpoint& kept, void* gate, void* up,
+                             cudaStream_t st) {
+    const int blocks = F / kCheckpointBlock;
+    const unsigned grid = (unsigned)(((long long)rows * blocks + 255) / 256);
+    LaunchScope scope(ctx, st, "checkpoint_decode_kernel");
+    return cuda_status(launch_chained(checkpoint_decode_kernel, dim3(grid), dim3(256), 0, st,
+                                      reinterpret_cast<const uint4*>(kept.codes), static_cast<const uint16_t*>(kept.exps),
+                                      static_cast<uint4*>(gate), static_cast<uint4*>(up), rows, blocks));
+}
+
+}  // namespace director
