@@ -255,6 +255,29 @@ int director_expert_ffn_checkpoint(director_ctx* ctx, int32_t T, const void* xp,
 int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const int8_t* codes, const uint8_t* exps,
                                void* gate, void* up, void* stream);
 
+/* Workspace of director_expert_ffn_backward: two bf16 arrays [T_max*K,F] (and two [T_max,S*F]) on the context.  Allocates on
+ * the first call, does nothing on later ones; serving contexts never pay for it. */
+int director_reserve_training(director_ctx* ctx);
+
+/* Gradients of director_expert_ffn_checkpoint at the gate and up values that it kept (s = sigmoid(g), e the row's expert):
+ *   da = dyp . w_down[e],  du = da g s,  dg = da u s (1 + g (1 - s)),  act = g s u   (dg, du, act rounded to bf16),
+ *   dxp = dg . w_gate[e] + du . w_up[e],
+ *   dw_gate[e] = dg^T . xp,  dw_up[e] = du^T . xp,  dw_down[e] = dyp^T . act,  summed over the rows of all of e's replicas.
+ * xp, dyp: dev bf16 [T*K,H], rows in dispatch order (dyp from director_combine_backward).  seg_offsets, codes, exps: as
+ * written by the forward calls for the same T and placement.  w_gate, w_up: dev bf16 [E,F,H].  w_down: dev bf16 [E,H,F].
+ * dxp: dev bf16 [T*K,H].  dw_*: dev bf16, shaped as the weights and written whole (zeros for an expert without rows).
+ * Shared experts (only if the context has S > 0 and x != NULL): x, dy: dev bf16 [T,H]; codes_shared, exps_shared, ws_*: as for
+ * the forward call; dx_shared: dev bf16 [T,H]; dws_gate, dws_up: dev bf16 [S*F,H]; dws_down: dev bf16 [H,S*F].
+ * Needs director_reserve_training (DIRECTOR_ERR_WORKSPACE otherwise).  The tensor-core kernels run at every batch size; the
+ * tile scheme of the forward plays no part. */
+int director_expert_ffn_backward(director_ctx* ctx, int32_t T, const void* xp, const void* dyp, const int32_t* seg_offsets,
+                                 const int8_t* codes, const uint8_t* exps, const void* w_gate, const void* w_up,
+                                 const void* w_down, void* dxp, void* dw_gate, void* dw_up, void* dw_down,
+                                 const void* x, const void* dy, const int8_t* codes_shared,
+                                 const uint8_t* exps_shared, const void* ws_gate, const void* ws_up,
+                                 const void* ws_down, void* dx_shared, void* dws_gate, void* dws_up, void* dws_down,
+                                 void* stream);
+
 /* (a5) Placement cost (Section VI-A): workload matrix W, per-rank load of Eq. 1 and dispatch
  * volume of Eq. 3 for the current placement, counted per executed assignment.
  * topk_idx: dev int32 [T,K].  token_src_rank: dev int32 [T] home rank of each token, or NULL for

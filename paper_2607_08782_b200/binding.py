@@ -29,7 +29,8 @@ EXPORTED = (
     "director_reserve_placements", "director_select_placement", "director_set_profiling_filter",
     "director_selftest_bounded_wait", "director_gemm_sm_mhz", "director_gemm_counters",
     "director_combine_backward", "director_dispatch_backward", "director_route_backward",
-    "director_expert_ffn_checkpoint", "director_checkpoint_decode",
+    "director_expert_ffn_checkpoint", "director_checkpoint_decode", "director_reserve_training",
+    "director_expert_ffn_backward",
 )
 
 REPLICA_ROUND_ROBIN, REPLICA_LOCAL_FIRST = 0, 1
@@ -94,6 +95,8 @@ def load_library(rebuild_if_stale: bool = True) -> ctypes.CDLL:
     lib.director_dispatch_backward.argtypes = [vp, c_int32] + [vp] * 5
     lib.director_route_backward.argtypes = [vp, c_int32] + [vp] * 5
     lib.director_expert_ffn_checkpoint.argtypes = [vp, c_int32] + [vp] * 16
+    lib.director_reserve_training.argtypes = [vp]
+    lib.director_expert_ffn_backward.argtypes = [vp, c_int32] + [vp] * 24
     lib.director_checkpoint_decode.argtypes = [vp, c_int32, c_int32] + [vp] * 5
     lib.director_kernel_time.argtypes = [vp, c_char_p, POINTER(c_int64)]
     lib.director_kernel_time.restype = c_double
@@ -274,6 +277,33 @@ class Director:
             self._ctx, T, _ptr(xp), _ptr(seg_offsets), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(codes), _ptr(exps), _ptr(yp),
             _ptr(x), _ptr(ws_gate), _ptr(ws_up), _ptr(ws_down), _ptr(codes_shared), _ptr(exps_shared), _ptr(y_shared),
             _stream()), "director_expert_ffn_checkpoint")
+
+    def reserve_training(self):
+        """Allocates the workspace of expert_ffn_backward (once; later calls do nothing)."""
+        _check(self.lib.director_reserve_training(self._ctx), "director_reserve_training")
+
+    def expert_ffn_backward(self, T, xp, dyp, seg_offsets, codes, exps, w_gate, w_up, w_down, dxp, dw_gate, dw_up, dw_down,
+                            x=None, dy=None, codes_shared=None, exps_shared=None, ws_gate=None, ws_up=None, ws_down=None,
+                            dx_shared=None, dws_gate=None, dws_up=None, dws_down=None):
+        """Gradients of expert_ffn_checkpoint from the gate and up values it kept (after reserve_training)."""
+        s = self.shape
+        TK, W = T * s.K, s.E * s.F * s.H
+        need = dict(xp=(xp, _BF16, TK * s.H), dyp=(dyp, _BF16, TK * s.H), seg_offsets=(seg_offsets, _I32, s.R * s.C_max + 1),
+                    codes=(codes, _I8, 2 * TK * s.F), exps=(exps, _U8, TK * s.F // 8), w_gate=(w_gate, _BF16, W),
+                    w_up=(w_up, _BF16, W), w_down=(w_down, _BF16, W), dxp=(dxp, _BF16, TK * s.H), dw_gate=(dw_gate, _BF16, W),
+                    dw_up=(dw_up, _BF16, W), dw_down=(dw_down, _BF16, W))
+        if s.S > 0 and x is not None:
+            SF = s.S * s.F
+            need.update(x=(x, _BF16, T * s.H), dy=(dy, _BF16, T * s.H), codes_shared=(codes_shared, _I8, 2 * T * SF),
+                        exps_shared=(exps_shared, _U8, T * SF // 8), ws_gate=(ws_gate, _BF16, SF * s.H),
+                        ws_up=(ws_up, _BF16, SF * s.H), ws_down=(ws_down, _BF16, SF * s.H), dx_shared=(dx_shared, _BF16, T * s.H),
+                        dws_gate=(dws_gate, _BF16, SF * s.H), dws_up=(dws_up, _BF16, SF * s.H), dws_down=(dws_down, _BF16, SF * s.H))
+        _need("expert_ffn_backward", **need)
+        _check(self.lib.director_expert_ffn_backward(
+            self._ctx, T, _ptr(xp), _ptr(dyp), _ptr(seg_offsets), _ptr(codes), _ptr(exps), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+            _ptr(dxp), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(x), _ptr(dy), _ptr(codes_shared), _ptr(exps_shared),
+            _ptr(ws_gate), _ptr(ws_up), _ptr(ws_down), _ptr(dx_shared), _ptr(dws_gate), _ptr(dws_up), _ptr(dws_down), _stream()),
+            "director_expert_ffn_backward")
 
     def checkpoint_decode(self, rows, F, codes, exps, gate, up):
         """The values that a checkpoint of `rows` rows of F features stands for, into gate and up (bf16 [rows,F])."""

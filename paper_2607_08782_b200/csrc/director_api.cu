@@ -43,7 +43,7 @@ void free_all(director_ctx* c) {
                     c->d_status, c->d_hidden, c->d_hidden_shared, c->d_one_seg, c->d_sched, c->d_gemm_clock,
                     c->d_zero_expert, c->e_logits2[0], c->e_logits2[1], c->e_x2[0], c->e_x2[1], c->e_topk_idx,
                     c->e_topk_w, c->e_xp, c->e_yp, c->e_y2[0], c->e_y2[1], c->e_y_shared, c->e_row_token, c->e_inv_row,
-                    c->e_dest_rank, c->e_cost2[0], c->e_cost2[1]};
+                    c->e_dest_rank, c->e_cost2[0], c->e_cost2[1], c->d_dgu, c->d_dgu_shared, c->d_grad_sched};
     for (void* p : ptrs)
         if (p) cudaFree(p);
     for (int i = 0; i < 2; ++i) {
@@ -519,6 +519,54 @@ int director_expert_ffn_checkpoint(director_ctx* ctx, int32_t T, const void* xp,
     const Checkpoint kept_shared{codes_shared, reinterpret_cast<uint16_t*>(exps_shared), T};
     return launch_expert_ffn_checkpoint(ctx, T, xp, seg_offsets, w_gate, w_up, w_down, kept, yp, x, ws_gate, ws_up, ws_down,
                                         kept_shared, y_shared, as_stream(stream));
+}
+
+int director_reserve_training(director_ctx* ctx) {
+    REQUIRE_CTX(ctx);
+    if (ctx->d_grad_sched != nullptr) return DIRECTOR_OK;
+    if (cudaSetDevice(ctx->device) != cudaSuccess) return DIRECTOR_ERR_CUDA;
+    const director_shape& s = ctx->shape;
+    uint16_t *dgu = nullptr, *dgu_shared = nullptr;
+    unsigned int* sched = nullptr;
+    if (!dev_alloc(&dgu, 2 * (size_t)s.T_max * s.K * s.F) || !dev_alloc(&dgu_shared, 2 * (size_t)s.T_max * s.S * s.F) ||
+        !dev_alloc(&sched, 8)) {
+        cudaGetLastError();
+        void* ptrs[] = {dgu, dgu_shared, sched};
+        for (void* p : ptrs)
+            if (p) cudaFree(p);
+        return DIRECTOR_ERR_WORKSPACE;
+    }
+    ctx->d_dgu = dgu;
+    ctx->d_dgu_shared = dgu_shared;
+    ctx->d_grad_sched = sched;
+    return DIRECTOR_OK;
+}
+
+int director_expert_ffn_backward(director_ctx* ctx, int32_t T, const void* xp, const void* dyp, const int32_t* seg_offsets,
+                                 const int8_t* codes, const uint8_t* exps, const void* w_gate, const void* w_up,
+                                 const void* w_down, void* dxp, void* dw_gate, void* dw_up, void* dw_down, const void* x,
+                                 const void* dy, const int8_t* codes_shared, const uint8_t* exps_shared, const void* ws_gate,
+                                 const void* ws_up, const void* ws_down, void* dx_shared, void* dws_gate, void* dws_up,
+                                 void* dws_down, void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PLACEMENT(ctx);
+    const void* routed_ptrs[] = {xp, dyp, seg_offsets, codes, exps, w_gate, w_up, w_down, dxp, dw_gate, dw_up, dw_down};
+    for (const void* p : routed_ptrs) REQUIRE_PTR(p);
+    const bool with_shared = ctx->shape.S > 0 && x != nullptr;
+    if (with_shared) {
+        const void* shared_ptrs[] = {x, dy, codes_shared, exps_shared, ws_gate, ws_up, ws_down, dx_shared, dws_gate, dws_up, dws_down};
+        for (const void* p : shared_ptrs) REQUIRE_PTR(p);
+    }
+    if (ctx->d_grad_sched == nullptr) return DIRECTOR_ERR_WORKSPACE;
+    auto kept = [](const int8_t* c, const uint8_t* e, int rows) {
+        return Checkpoint{const_cast<int8_t*>(c), reinterpret_cast<uint16_t*>(const_cast<uint8_t*>(e)), rows};
+    };
+    const FfnGrad routed{xp, dyp, kept(codes, exps, T * ctx->shape.K), w_gate, w_up, w_down, dxp, dw_gate, dw_up, dw_down};
+    FfnGrad shared{};
+    if (with_shared)
+        shared = FfnGrad{x, dy, kept(codes_shared, exps_shared, T), ws_gate, ws_up, ws_down, dx_shared, dws_gate, dws_up, dws_down};
+    return launch_expert_ffn_backward(ctx, T, seg_offsets, routed, shared, as_stream(stream));
 }
 
 int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const int8_t* codes, const uint8_t* exps, void* gate,

@@ -75,6 +75,11 @@ struct director_ctx {
     int32_t* d_zero_expert = nullptr;  // [1] = {0}
     unsigned long long* d_gemm_clock = nullptr;   // [2][kGemmClockCtas][kGemmClockWords] per-CTA records of the last gate|up / down launch
 
+    // backward pass, allocated by director_reserve_training
+    void* d_dgu = nullptr;             // bf16 [2][T_max*K, F]     gradients of the gate and up values (act reuses d_hidden)
+    void* d_dgu_shared = nullptr;      // bf16 [2][T_max, S*F]
+    unsigned int* d_grad_sched = nullptr;   // [8] work-item counters of the (up to eight) launches of one backward call
+
     // buffers of the host-buffer entry points; inputs, y and the histograms exist twice so that the
     // copies of one batch overlap the kernels of its neighbours
     float* e_logits2[2] = {nullptr, nullptr};
@@ -261,6 +266,16 @@ int launch_expert_ffn_checkpoint(director_ctx*, int T, const void* xp, const int
                                  const void* w_up, const void* w_down, const Checkpoint& kept, void* yp, const void* x,
                                  const void* ws_gate, const void* ws_up, const void* ws_down, const Checkpoint& kept_shared,
                                  void* y_shared, cudaStream_t);
+// One set of expert FFNs in the backward pass: inputs x and dy, the kept gate and up values (kept.rows rows), weights, and where
+// the gradients go.  All bf16.
+struct FfnGrad {
+    const void *x, *dy;
+    Checkpoint kept;
+    const void *w_gate, *w_up, *w_down;
+    void *dx, *dw_gate, *dw_up, *dw_down;
+};
+int launch_expert_ffn_backward(director_ctx*, int T, const int32_t* seg_offsets, const FfnGrad& routed, const FfnGrad& shared,
+                               cudaStream_t);
 int launch_combine_backward(director_ctx*, int T, const void* dy, const void* yp, const int32_t* inv_row, const float* topk_w,
                             void* dyp, float* dtopk_w, cudaStream_t);
 int launch_route_backward(director_ctx*, int T, const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,

@@ -40,6 +40,7 @@ bool ffn_small_applies(const director_ctx* ctx, int T, int Fw);
 int ffn_pass_small(director_ctx* ctx, const void* in, const int32_t* gather_rows, const int32_t* seg_offsets, const int32_t* slot_expert, int G,
                    const void* w_gate, const void* w_up, const void* w_down, int Fw, void* hidden, void* out, int rows_max,
                    int max_segments, cudaStream_t st);
+int ffn_grad_init(director_ctx* ctx);   // director_ffn_grad.cu
 int ffn_pair_init(director_ctx* ctx);   // director_ffn_pair.cu
 int launch_gemm_pair(director_ctx* ctx, int mode, const char* name, const CUtensorMap& a, const CUtensorMap& b0,
                      const CUtensorMap& b1, const umma::GroupedGemmParams& p, cudaStream_t st);
@@ -256,10 +257,6 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // bf16 matrix [rows, cols] row-major; box = 64 columns (128 bytes) x 128 rows, 128-byte swizzle;
 // out-of-range rows are filled with zeros.
 bool make_map(director_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols) {
@@ -316,7 +313,8 @@ __global__ void one_segment_kernel(int32_t* seg, int T) {
 }  // namespace
 
 int ffn_init(director_ctx* ctx) {
-    if (ffn_pair_init(ctx) != DIRECTOR_OK || ffn_swap_init(ctx) != DIRECTOR_OK || ffn_small_init(ctx) != DIRECTOR_OK)
+    if (ffn_pair_init(ctx) != DIRECTOR_OK || ffn_swap_init(ctx) != DIRECTOR_OK || ffn_small_init(ctx) != DIRECTOR_OK ||
+        ffn_grad_init(ctx) != DIRECTOR_OK)
         return DIRECTOR_ERR_CUDA;
     if (cudaFuncSetAttribute(grouped_gemm_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess ||
         cudaFuncSetAttribute(grouped_gemm_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess)

@@ -167,5 +167,116 @@ __device__ __forceinline__ void umma_commit_both(uint32_t bar) {
                  ::"r"(bar), "h"(mask) : "memory");
 }
 
+// One lane of a converged warp (the same lane every time).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t pred;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+    return pred != 0;
+}
+// Bounded barrier wait for a loop that a whole warp runs in lock step.  The spin, the poll of the CTA's abort flag
+// and the time limit sit inside one block of PTX, so the code around the call has no data-dependent branch: loop
+// counters, shared-memory addresses and matrix descriptors stay warp-uniform, and the instructions that want them in
+// uniform registers (tcgen05.mma, tcgen05.commit, the TMA loads) get them without a move per operand.  With one
+// thread running such a loop inside `if (lane == 0)`, issuing a k-step took ~510 cycles whatever the tile's width - as
+// long as the tensor pipe needs for a FULL tile, so that a ragged tile cost as much as a full one.
+// Only the lane with `polls` != 0 waits (31 more lanes polling the same barrier add nothing but power); the others fall
+// through and meet it at the warp's next converging instruction.  `bad` != 0 skips the wait (an earlier wait of this
+// lane expired: the loop runs out without waiting or issuing); returns the new `bad`.  An expiry raises the CTA's
+// abort flag.
+__device__ __forceinline__ uint32_t mbar_wait_conv(uint32_t bar, uint32_t parity, uint32_t abort_addr, uint32_t bad,
+                                                   uint32_t polls) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p, q;\n\t"
+        ".reg .u64 t0, t1;\n\t"
+        ".reg .u32 ab, n;\n\t"
+        "setp.ne.u32 q, %0, 0;\n\t"
+        "@q bra DONE;\n\t"
+        "setp.eq.u32 q, %5, 0;\n\t"
+        "@q bra DONE;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE;\n\t"
+        "mov.u64 t0, %globaltimer;\n\t"
+        "mov.u32 n, 0;\n\t"
+        "SPIN:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE;\n\t"
+        "add.u32 n, n, 1;\n\t"
+        "and.b32 ab, n, 63;\n\t"
+        "setp.ne.u32 q, ab, 0;\n\t"
+        "@q bra SPIN;\n\t"                       // flag and clock are looked at once in 64 polls
+        "ld.volatile.shared.u32 ab, [%3];\n\t"
+        "setp.ne.u32 q, ab, 0;\n\t"
+        "@q bra FAIL;\n\t"
+        "mov.u64 t1, %globaltimer;\n\t"
+        "sub.u64 t1, t1, t0;\n\t"
+        "setp.lt.u64 q, t1, %4;\n\t"
+        "@q bra SPIN;\n\t"
+        "FAIL:\n\t"
+        "mov.u32 ab, 1;\n\t"
+        "st.volatile.shared.u32 [%3], ab;\n\t"
+        "mov.u32 %0, 1;\n\t"
+        "DONE:\n\t"
+        "}"
+        : "+r"(bad) : "r"(bar), "r"(parity), "r"(abort_addr), "l"(WAIT_LIMIT_NS), "r"(polls) : "memory");
+    return bad;
+}
+
+__device__ __forceinline__ void umma_pair_n(uint32_t tmem_d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                            uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void st_cluster_v4(uint32_t cluster_addr, int4 v) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                 : "memory");
+}
+// remote arrive that publishes this thread's earlier (remote) stores to the waiting CTA
+__device__ __forceinline__ void mbar_arrive_cluster_release(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_acquire_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_acquire_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    if (mbar_try_acquire_cluster(bar, parity)) return true;
+    const unsigned long long t0 = global_ns();
+    uint32_t n = 0;
+    while (!mbar_try_acquire_cluster(bar, parity)) {
+        if ((++n & 63u) == 0u) {
+            if (*abort_flag) return false;
+            if (global_ns() - t0 > WAIT_LIMIT_NS) { *abort_flag = 1; return false; }
+        }
+    }
+    return true;
+}
+
+// ---- tensor maps (host) ----
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// bf16 [rows, cols] row-major, box 64 x box_rows, 128-byte swizzle
+inline bool map_2d(director_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows = 128) {
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {cols * 2};
+    const cuuint32_t box[2] = {BLOCK_K, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
+               map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace umma
 }  // namespace director

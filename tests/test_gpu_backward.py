@@ -407,3 +407,191 @@ def test_refusals_of_the_checkpoint_forward():
     assert e.value.status == 5
     fresh = _context(8)
     assert fresh.lib.director_expert_ffn_checkpoint(fresh._ctx, 8, *([f.xp.data_ptr()] * 8), *([None] * 8)) == 2   # no placement
+
+
+# ---- gradients of the expert FFN -----------------------------------------------------------------------------------
+
+
+class FfnGradient(Ffn):
+    """An Ffn whose forward has run, with gradients to be filled; canaries are 7."""
+
+    def __init__(self, *a, dy_scale=0.1, **k):
+        import torch
+        super().__init__(*a, **k)
+        rng = np.random.default_rng(a[0] + 999)
+        self.checkpoint()
+        self.dyp, self.dyp64 = _bf16(rng, self.A, self.H, scale=dy_scale)
+        self.dxp = torch.full_like(self.xp, 7.0)
+        self.dw = [torch.full_like(w, 7.0) for w in (self.wg, self.wu, self.wd)]
+        if self.S:
+            self.dy, self.dy64 = _bf16(rng, self.T, self.H, scale=dy_scale)
+            self.dx_s = torch.full_like(self.x, 7.0)
+            self.dws = [torch.full_like(w, 7.0) for w in (self.sg, self.su, self.sd)]
+
+    def backward(self):
+        shared = (self.x, self.dy, self.codes_s, self.exps_s, self.sg, self.su, self.sd, self.dx_s, *self.dws) if self.S else ()
+        self.d.expert_ffn_backward(self.T, self.xp, self.dyp, self.seg, self.codes, self.exps, self.wg, self.wu, self.wd, self.dxp,
+                                   *self.dw, *shared)
+
+    def outputs(self):
+        return [self.dxp, *self.dw] + ([self.dx_s, *self.dws] if self.S else [])
+
+
+def _check_expert(label, x, dy, g, u, wg, wu, wd, got):
+    """One expert's gradients (numpy: dx, dwg, dwu, dwd) against the definition.  Bounds: da and the products are fp32 sums; s =
+    sigmoid(g) is off by a few units in the last place, more for large |g| (the argument of the exponential); dg, du and act
+    are rounded to bf16; so are the results."""
+    n, H, F = len(x), x.shape[1], g.shape[1]
+    dx, dwg, dwu, dwd, dg, du, act = gro.swiglu_ffn_backward(x, dy, g, u, wg, wu, wd)
+    s = 1 / (1 + np.exp(-g))
+    eps = (8 + 1.2 * np.abs(g)) * U32
+    da, t_da = dy @ wd, H * U32 * (np.abs(dy) @ np.abs(wd))
+    slope = s * (1 + g * (1 - s))
+    t_dg = U16 * np.abs(dg) * 1.01 + 1.01 * (np.abs(u * slope) * t_da + np.abs(da * u) * eps * s * (1 + 2 * np.abs(g)))
+    t_du = U16 * np.abs(du) * 1.01 + 1.01 * np.abs(g) * s * (t_da + np.abs(da) * eps)
+    t_act = (U16 + 2 * eps) * np.abs(act) * 1.01
+    ax, ay, ag, au, aw = np.abs(x), np.abs(dy), np.abs(wg), np.abs(wu), n + 64
+    for name, ref, val, tol in (
+            ("dx", dx, got[0], t_dg @ ag + t_du @ au + 2 * F * U32 * (np.abs(dg) @ ag + np.abs(du) @ au)),
+            ("dw_gate", dwg, got[1], t_dg.T @ ax + aw * U32 * (np.abs(dg).T @ ax)),
+            ("dw_up", dwu, got[2], t_du.T @ ax + aw * U32 * (np.abs(du).T @ ax)),
+            ("dw_down", dwd, got[3], ay.T @ t_act + aw * U32 * (ay.T @ np.abs(act)))):
+        assert (np.abs(val - ref) <= (U16 * np.abs(ref) + tol) * 1.02 + 1e-30).all(), f"{label}: {name}"
+        # errors of single roundings do not add up in step: the whole is off by about as much as one of them
+        if ref.size > 512:
+            assert np.linalg.norm(val - ref) <= U16 * np.linalg.norm(ref) + 1e-30, f"{label}: {name} as a whole"
+
+
+def _check_backward(f, skip=()):
+    g, u = _kept(f.codes, f.exps, 0), _kept(f.codes, f.exps, 1)
+    dxp, dw = _np(f.dxp), [_np(w) for w in f.dw]
+    for e in range(f.E):
+        rows = np.concatenate([np.arange(f.seg64[k], f.seg64[k + 1]) for k in range(len(f.slot_expert)) if f.slot_expert[k] == e]
+                              or [np.zeros(0)]).astype(int)
+        if e in skip:
+            continue
+        if not len(rows):
+            assert all(not w[e].any() for w in dw), f"expert {e} has no rows"
+            continue
+        _check_expert(f"expert {e}", f.xp64[rows], f.dyp64[rows], g[rows], u[rows], f.wg64[e], f.wu64[e], f.wd64[e],
+                      (dxp[rows], dw[0][e], dw[1][e], dw[2][e]))
+    if f.S:
+        _check_expert("shared", f.x64, f.dy64, _kept(f.codes_s, f.exps_s, 0), _kept(f.codes_s, f.exps_s, 1), f.sg64, f.su64, f.sd64,
+                      [_np(t) for t in (f.dx_s, *f.dws)])
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("H,F,S", [(256, 128, 0), (512, 384, 1), (768, 256, 2)])
+def test_ffn_backward(layout, H, F, S):
+    lengths, X, C = _layout(layout)
+    f = FfnGradient(len(layout) + H, lengths, X, C, H, F, S=S)
+    f.d.reserve_training()
+    f.backward()
+    assert f.d.last_status() == 0
+    _check_backward(f)
+    first = [t.clone() for t in f.outputs()]
+    f.backward()
+    assert all(_same_bits(a, b) for a, b in zip(first, f.outputs()))
+
+
+@pytest.mark.parametrize("length", [1, 15, 16, 17, 47, 48, 63, 64, 65, 79, 80, 127, 128, 129, 191, 255, 256, 271, 513])
+def test_ffn_backward_of_every_kind_of_segment_end(length):
+    """The contraction of the weight gradients ends inside a 64-row step, inside an MMA, or on their borders."""
+    X = np.array([[1], [1]], dtype=np.uint8)
+    f = FfnGradient(length, [length, 37], X, 2, 256, 256)
+    f.d.reserve_training()
+    f.backward()
+    assert f.d.last_status() == 0
+    _check_backward(f)
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_ffn_backward_of_random_layouts(seed):
+    rng = np.random.default_rng(seed)
+    E, R = int(rng.choice([1, 3, 8, 17])), int(rng.choice([1, 2, 4]))
+    C = min(16, -(-E // R) + int(rng.integers(0, 3)))
+    if E > R * C:
+        R = 2
+        C = -(-E // R)
+    X = np.zeros((E, R), dtype=np.uint8)
+    for e in range(E):
+        X[e, e % R] = 1
+    for _ in range(6):
+        e, j = int(rng.integers(E)), int(rng.integers(R))
+        if not X[e, j] and X[:, j].sum() < C:
+            X[e, j] = 1
+    _, _, slot_expert = _tables(X, C)
+    lengths = [int(rng.choice([0, 1, 5, 16, 64, 100, 300])) if e >= 0 else 0 for e in slot_expert]
+    if not sum(lengths):
+        lengths[int(np.argmax(slot_expert >= 0))] = 9
+    f = FfnGradient(seed, lengths, X, C, int(rng.choice([256, 512, 1024])), int(rng.choice([128, 256, 640])), S=int(rng.choice([0, 1])))
+    f.d.reserve_training()
+    f.backward()
+    assert f.d.last_status() == 0
+    _check_backward(f)
+
+
+def test_what_is_not_finite_stays_with_its_expert():
+    """An expert's rows full of NaN and infinity, next to another's in the permuted order: a step of the other's contraction
+    that reads past its segment must not pick them up."""
+    X = np.array([[1], [1], [1]], dtype=np.uint8)
+    f = FfnGradient(4, [37, 30, 41], X, 3, 256, 256)
+    f.d.reserve_training()
+    bad = slice(37, 67)
+    f.xp[bad] = float("nan")
+    f.dyp[bad] = float("inf")
+    f.codes[bad] = 5
+    f.exps[:, bad] = 255
+    f.backward()
+    assert f.d.last_status() == 0
+    _check_backward(f, skip=(1,))
+    import torch
+    assert all(not torch.isfinite(w[1]).any() for w in f.dw) and not torch.isfinite(f.dxp[bad]).any()
+
+
+def test_ffn_backward_is_the_derivative():
+    """Against central differences of the fp64 forward: the slope of <dy, y> along each gradient is the gradient's own length, up
+    to what the 8-bit values cost (steps of 2^-6 of a block's largest: 0.6 % of a value on average, 2 % is far outside)."""
+    X = np.array([[1, 1], [0, 1]], dtype=np.uint8)
+    f = FfnGradient(11, [120, 0, 95, 9], X, 2, 256, 128, scale=0.08)
+    f.d.reserve_training()
+    f.backward()
+    rows = {0: np.r_[0:120, 120:215], 1: np.r_[215:224]}
+    for e in (0, 1):
+        args = dict(x=f.xp64[rows[e]], wg=f.wg64[e], wu=f.wu64[e], wd=f.wd64[e])
+        got = dict(x=_np(f.dxp)[rows[e]], wg=_np(f.dw[0])[e], wu=_np(f.dw[1])[e], wd=_np(f.dw[2])[e])
+        for name, grad in got.items():
+            size = np.linalg.norm(grad)
+            step = 1e-4 * grad / size
+            value = [np.sum(f.dyp64[rows[e]] * gro.swiglu_ffn(**{**args, name: args[name] + k * step})[0]) for k in (1, -1)]
+            assert abs((value[0] - value[1]) / 2e-4 - size) <= 0.02 * size, (e, name)
+
+
+def test_refusals_of_the_ffn_gradient():
+    import torch
+    from paper_2607_08782_b200.binding import DirectorError
+    lengths, X, C = _layout("ragged")
+    f = FfnGradient(3, lengths, X, C, 256, 128)
+    with pytest.raises(DirectorError) as e:
+        f.backward()
+    assert e.value.status == 3                            # no workspace yet
+    f.d.reserve_training()
+    f.d.reserve_training()
+    f.backward()
+    good = [f.xp, f.dyp, f.seg, f.codes, f.exps, f.wg, f.wu, f.wd, f.dxp, *f.dw]
+    for k, wrong in ((1, f.dyp.float()), (2, f.seg.long()), (3, f.codes.view(torch.uint8)), (11, f.dw[2].float())):
+        with pytest.raises(TypeError):
+            f.d.expert_ffn_backward(f.T, *good[:k], wrong, *good[k + 1:])
+    for k, wrong in ((0, f.xp[:-1]), (9, f.dw[0][1:]), (5, f.wg.transpose(1, 2))):
+        with pytest.raises(ValueError):
+            f.d.expert_ffn_backward(f.T, *good[:k], wrong, *good[k + 1:])
+    lib, ptr = f.d.lib, f.xp.data_ptr()
+    call = lib.director_expert_ffn_backward
+    assert call(None, f.T, *([ptr] * 12), *([None] * 12)) == 1
+    assert call(f.d._ctx, 0, *([ptr] * 12), *([None] * 12)) == 1
+    assert call(f.d._ctx, f.T + 1, *([ptr] * 12), *([None] * 12)) == 1
+    assert call(f.d._ctx, f.T, *([ptr] * 11), None, *([None] * 12)) == 1
+    assert call(f.d._ctx, f.T, *([ptr] * 11), ptr + 2, *([None] * 12)) == 1
+    fresh = _context(8)
+    assert call(fresh._ctx, 8, *([ptr] * 12), *([None] * 12)) == 2      # no placement
+    assert f.d.last_status() == 0
