@@ -529,7 +529,7 @@ int director_reserve_training(director_ctx* ctx) {
     uint16_t *dgu = nullptr, *dgu_shared = nullptr;
     unsigned int* sched = nullptr;
     if (!dev_alloc(&dgu, 2 * (size_t)s.T_max * s.K * s.F) || !dev_alloc(&dgu_shared, 2 * (size_t)s.T_max * s.S * s.F) ||
-        !dev_alloc(&sched, 8)) {
+        !dev_alloc(&sched, 2) || cudaMemset(sched, 0, 2 * sizeof(unsigned int)) != cudaSuccess) {
         cudaGetLastError();
         void* ptrs[] = {dgu, dgu_shared, sched};
         for (void* p : ptrs)
@@ -566,7 +566,7 @@ int director_expert_ffn_backward(director_ctx* ctx, int32_t T, const void* xp, c
     FfnGrad shared{};
     if (with_shared)
         shared = FfnGrad{x, dy, kept(codes_shared, exps_shared, T), ws_gate, ws_up, ws_down, dx_shared, dws_gate, dws_up, dws_down};
-    return launch_expert_ffn_backward(ctx, T, seg_offsets, routed, shared, as_stream(stream));
+    return launch_expert_ffn_backward(ctx, seg_offsets, routed, shared, as_stream(stream));
 }
 
 int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const int8_t* codes, const uint8_t* exps, void* gate,

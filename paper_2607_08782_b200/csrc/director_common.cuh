@@ -78,7 +78,7 @@ struct director_ctx {
     // backward pass, allocated by director_reserve_training
     void* d_dgu = nullptr;             // bf16 [2][T_max*K, F]     gradients of the gate and up values (act reuses d_hidden)
     void* d_dgu_shared = nullptr;      // bf16 [2][T_max, S*F]
-    unsigned int* d_grad_sched = nullptr;   // [8] work-item counters of the (up to eight) launches of one backward call
+    unsigned int* d_grad_sched = nullptr;   // [2] work-item counters of the two launches of a backward call, each cleared by the other
 
     // buffers of the host-buffer entry points; inputs, y and the histograms exist twice so that the
     // copies of one batch overlap the kernels of its neighbours
@@ -274,7 +274,7 @@ struct FfnGrad {
     const void *w_gate, *w_up, *w_down;
     void *dx, *dw_gate, *dw_up, *dw_down;
 };
-int launch_expert_ffn_backward(director_ctx*, int T, const int32_t* seg_offsets, const FfnGrad& routed, const FfnGrad& shared,
+int launch_expert_ffn_backward(director_ctx*, const int32_t* seg_offsets, const FfnGrad& routed, const FfnGrad& shared,
                                cudaStream_t);
 int launch_combine_backward(director_ctx*, int T, const void* dy, const void* yp, const int32_t* inv_row, const float* topk_w,
                             void* dyp, float* dtopk_w, cudaStream_t);

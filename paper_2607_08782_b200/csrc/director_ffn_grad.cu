@@ -8,6 +8,10 @@
 // dg, du and act are rounded to bf16 between the products (the tensor cores' operand type): an error of the size of the
 // outputs' own rounding.  All sums are fp32 in tensor memory, in a fixed order.
 //
+// Two launches: GRAD_ACT, and the other three kinds together - they need nothing of each other, and the many short work items
+// of the weight gradients fill the idle end that the few long ones of GRAD_DX would leave.  The shared experts are one more
+// expert with a width and row space of its own (problem 1), in the same launches.
+//
 // CTA pairs as in the forward kernel (tcgen05.mma cta_group::2, M = 256: 128 rows of D per CTA, accumulators of up to 256
 // columns, two of them), operands by TMA through a ring of 32 KB stages.  What differs is the operands' direction: no matrix
 // is transposed in memory.  An operand whose rows run along the contraction (Wd, Wg, Wu as the left operand; everything in
@@ -15,13 +19,14 @@
 // MN-major tile.
 //   GRAD_ACT / GRAD_DX: D[feature, token], as in the forward: 256 weight columns x up to 256 tokens, the token count a runtime
 //     operand in steps of 32, so a segment's ragged end costs little.
-//   GRAD_GATEUP: D[h, f]: 256 columns of xp x 128 features of dg and the same 128 of du - the left tile serves both products,
-//     and each CTA of the pair supplies one of the right ones.   GRAD_DOWN: D[h, f]: 256 columns of dyp x up to 256 of act.
+//   GRAD_GATEUP: D[f, h]: CTA 0 of the pair holds 128 features of dg, CTA 1 the same 128 of du, and both share 256 columns of
+//     xp.   GRAD_DOWN: D[h, f]: 256 columns of dyp x up to 256 of act.
 //     The contraction runs over the segments of all of an expert's replicas.  Where a segment ends inside a 64-row step the
 //     rows behind it belong to another expert: the step issues only the MMAs it needs (16 rows each), and a warp of each CTA
 //     zeroes the rows behind the end inside the last one, in both operands (a zero times another expert's infinity would be
 //     NaN).  Experts are taken by descending length, so that the longest contractions do not end the launch.
-//     An expert without rows gets zeros.
+//     A tile goes out through shared memory and TMA stores: a lane holds 32 consecutive columns of one row, which as plain
+//     stores would touch 32 lines an instruction.  An expert without rows gets its zeros the same way, from a cleared buffer.
 // Work items are claimed from a global counter and handed to all roles through a small ring, as in the forward kernel.
 // Every wait is bounded; an expired one raises DIRECTOR_ERR_TIMEOUT.
 #include "director_common.cuh"
@@ -46,6 +51,8 @@ constexpr int G_TILE = 256;                            // tokens per full tile; 
 constexpr int G_SLOTS = 4;                             // ring of work items
 constexpr int G_CLAIM_LEAD = 32;                       // k-steps of claimed work ahead of the producer
 
+constexpr int G_OUT_BYTES = 32 * 64;                   // per epilogue warp: 32 rows x 32 bf16 columns of a weight gradient
+
 struct GradHeader {
     uint64_t full[G_STAGES], empty[G_STAGES];
     uint64_t part[G_STAGES];                           // this CTA's loads of a step that still has rows to be zeroed
@@ -54,13 +61,14 @@ struct GradHeader {
     uint32_t tmem;
     int abort;
     int prod_k;                                        // k-steps issued by the scheduler CTA's producer
-    int warp_sum[8];
+    int warp_sum[2][G_THREADS / 32];
 };
-constexpr int grad_smem_bytes(int n_rep, int E) {
-    return 1024 + G_STAGES * G_STAGE_BYTES + (int)sizeof(GradHeader) + 8 * n_rep + 4 * (2 * (E + 1) + 2 * E);
+// experts: all of them, the shared one among them; n_rep: their segments
+constexpr int grad_smem_bytes(int n_rep, int experts) {
+    return 1024 + G_STAGES * G_STAGE_BYTES + G_EPI_WARPS * G_OUT_BYTES + (int)sizeof(GradHeader) + 8 * n_rep + 4 * (5 * experts + 3);
 }
-static_assert(grad_smem_bytes(kMaxG, kMaxE) <= 232448, "the ring does not fit with the largest tables");
-static_assert(kMaxE <= G_THREADS, "one thread per expert builds the tables");
+static_assert(grad_smem_bytes(kMaxG + 1, kMaxE + 1) <= 232448, "the ring does not fit with the largest tables");
+static_assert(kMaxE + 1 <= G_THREADS, "one thread per expert builds the tables");
 
 constexpr uint32_t G_IDESC_BASE = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) /* left operand MN-major */ |
                                   ((uint32_t)(256 >> 4) << 24);
@@ -74,48 +82,64 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
            (1ull << 46) | (2ull << 61);
 }
 
+// Problem 0: the routed experts over the segment table.  Problem 1: the shared experts, one FFN over all rows of the batch.
+struct GradProblem {
+    int F;
+    int rows;                      // rows of the permuted operands
+    const int8_t* codes;           // the checkpoint
+    const uint16_t* exps;
+    uint16_t *dg, *du, *act;       // written by GRAD_ACT, [rows, F]
+    uint16_t* dx;                  // [rows, H]
+};
+// What a launch loads from and, for the weight gradients, stores to.  _K: boxes of 128 rows, contraction along the row; all
+// others: boxes of 64 contraction rows; OUT_*: boxes of 32 rows x 32 columns.
+enum GradMap { MAP_WD, MAP_DY_K, MAP_WG, MAP_WU, MAP_DG_K, MAP_DU_K, MAP_X, MAP_DG, MAP_DU, MAP_DY, MAP_ACT, MAP_OUT_G, MAP_OUT_U,
+               MAP_OUT_D, GRAD_MAPS };
+struct GradMaps {
+    CUtensorMap m[2][GRAD_MAPS];
+};
 struct GradParams {
     const int32_t* seg_offsets;    // [G+1], clamped to [0, rows]
     const int32_t* rep_start;      // [E+1] replicas of expert e: rep_slot[rep_start[e] .. rep_start[e+1])
     const int32_t* rep_slot;
-    int E, n_rep;
-    int rows;                      // rows of the permuted operands
-    int dense;                     // 1: one expert whose only segment is [0, rows); the three tables are not read
-    int H, F;
-    int m_blocks;                  // blocks of 256 D rows (per expert)
-    int n_blocks;                  // weight gradients: blocks of D columns per expert
-    int k_steps;                   // GRAD_ACT, GRAD_DX
-    const int8_t* codes;           // GRAD_ACT: the checkpoint
-    const uint16_t* exps;
-    uint16_t* out0;                // dg | dxp | dWg | dWd
-    uint16_t* out1;                // du |  -  | dWu |  -
-    uint16_t* out2;                // act
+    int E;                         // routed experts
+    int experts;                   // E, or E + 1 with the shared one behind them
+    int n_rep;                     // segments: the routed experts' replicas, and the shared expert's one
+    int H;
+    GradProblem prob[2];
     int32_t* status;
-    unsigned int* counter;
+    unsigned int* counter;         // next unclaimed work item of this launch (zero when the kernel starts)
+    unsigned int* other_counter;   // the other launch's, cleared here for its next run
 };
 
 struct GradItem {
-    int a, valid, e, b;            // tokens: first row, rows (0: end), expert, block;   weights: h block, 1, expert, f block
+    int a, valid, e, b, kind;      // tokens: first row, rows (0: end), expert, block;   weights: h block, 1, expert, f block
 };
 
 __device__ __forceinline__ uint16_t to_bf16(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
-template <int KIND>
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y) : "memory");
+}
+
+// PHASE 0: GRAD_ACT.  PHASE 1: GRAD_DX, GRAD_GATEUP, GRAD_DOWN.
+template <int PHASE>
 __global__ void __launch_bounds__(G_THREADS, 1)
-grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_constant__ CUtensorMap tm_a1,
-                    const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1, const GradParams p) {
-    constexpr bool WEIGHTS = KIND == GRAD_GATEUP || KIND == GRAD_DOWN;
+grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
     extern __shared__ uint8_t smem_raw[];
     chain_prologue();
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
-    GradHeader& hd = *reinterpret_cast<GradHeader*>(smem_raw + (ring - raw) + G_STAGES * G_STAGE_BYTES);
-    const int E = p.E;
-    int32_t* const s_rep = reinterpret_cast<int32_t*>(&hd + 1);        // [E+1] first replica of every expert
-    int32_t* const s_pre = s_rep + (E + 1);                            // [E+1] token tiles before expert e
-    int32_t* const s_steps = s_pre + (E + 1);                          // [E] weight gradients: 64-row steps of expert e
-    int32_t* const s_order = s_steps + E;                              // [E] weight gradients: experts, longest first
-    int32_t* const s_lo = s_order + E;                                 // [n_rep] rows of every replica
+    uint8_t* const out_buf = smem_raw + (ring - raw) + G_STAGES * G_STAGE_BYTES;      // [G_EPI_WARPS][G_OUT_BYTES]
+    GradHeader& hd = *reinterpret_cast<GradHeader*>(out_buf + G_EPI_WARPS * G_OUT_BYTES);
+    const int experts = p.experts;
+    int32_t* const s_rep = reinterpret_cast<int32_t*>(&hd + 1);        // [experts+1] first segment of every expert
+    int32_t* const s_pre = s_rep + (experts + 1);                      // [experts+1] token work items before expert e
+    int32_t* const s_wpre = s_pre + (experts + 1);                     // [experts+1] weight work items before s_order[i]
+    int32_t* const s_steps = s_wpre + (experts + 1);                   // [experts] 64-row steps of expert e
+    int32_t* const s_order = s_steps + experts;                        // [experts] experts, longest first
+    int32_t* const s_lo = s_order + experts;                           // [n_rep] rows of every segment
     int32_t* const s_hi = s_lo + p.n_rep;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -124,20 +148,23 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
     volatile int* const abort_flag = &hd.abort;
     volatile int* const prod_k = &hd.prod_k;
     const uint32_t abort_addr = smem_u32(&hd.abort);
+    const int h_blocks = p.H / 256;
+    auto problem_of = [&](int e) -> int { return e >= p.E ? 1 : 0; };
 
     // ---- tables and barriers ----
     for (int r = tid; r < p.n_rep; r += G_THREADS) {
-        int lo = 0, hi = p.rows;
-        if (!p.dense) {
+        int lo = 0, hi = p.prob[1].rows;
+        if (r < p.n_rep - (experts - p.E)) {
             const int g = __ldg(p.rep_slot + r);
-            lo = min(max(__ldg(p.seg_offsets + g), 0), p.rows);
-            hi = min(max(__ldg(p.seg_offsets + g + 1), lo), p.rows);
+            lo = min(max(__ldg(p.seg_offsets + g), 0), p.prob[0].rows);
+            hi = min(max(__ldg(p.seg_offsets + g + 1), lo), p.prob[0].rows);
         }
         s_lo[r] = lo;
         s_hi[r] = hi;
     }
-    for (int e = tid; e <= E; e += G_THREADS) s_rep[e] = p.dense ? e : __ldg(p.rep_start + e);
+    for (int e = tid; e <= experts; e += G_THREADS) s_rep[e] = e <= p.E ? __ldg(p.rep_start + e) : p.n_rep;
     if (tid == 0) {
+        if (blockIdx.x == 0) *p.other_counter = 0u;     // its launch has ended (chain_prologue), or has not begun
         *abort_flag = 0;
         *prod_k = 0;
         for (int s = 0; s < G_STAGES; ++s) {
@@ -149,40 +176,48 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
             mbar_init(smem_u32(&hd.tfull[a]), 1);
             mbar_init(smem_u32(&hd.tempty[a]), 2 * G_EPI_WARPS);
         }
-        // readers of an item: the MMA warp, both producers, all epilogue warps, for the weight gradients both tail warps
+        // readers of an item: the MMA warp, both producers, all epilogue warps, in phase 1 both tail warps
         for (int q = 0; q < G_SLOTS; ++q) {
             mbar_init(smem_u32(&hd.sched_full[q]), 1);
-            mbar_init(smem_u32(&hd.sched_empty[q]), 3 + 2 * G_EPI_WARPS + (WEIGHTS ? 2 : 0));
+            mbar_init(smem_u32(&hd.sched_empty[q]), 3 + 2 * G_EPI_WARPS + 2 * PHASE);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
     {
-        int mine = 0;                                   // token tiles (or 64-row steps) of expert tid
-        if (tid < E)
-            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r)
-                mine += WEIGHTS ? (s_hi[r] - s_lo[r] + 63) / 64 : (s_hi[r] - s_lo[r] + G_TILE - 1) / G_TILE;
-        if constexpr (WEIGHTS) {
-            if (tid < E) s_steps[tid] = mine;
-            __syncthreads();
-            if (tid < E) {
-                int before = 0;
-                for (int e = 0; e < E; ++e) before += s_steps[e] > mine || (s_steps[e] == mine && e < tid) ? 1 : 0;
-                s_order[before] = tid;
+        int tiles = 0, steps = 0;                       // token tiles and 64-row steps of expert tid
+        if (tid < experts) {
+            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r) {
+                tiles += (s_hi[r] - s_lo[r] + G_TILE - 1) / G_TILE;
+                steps += (s_hi[r] - s_lo[r] + 63) / 64;
             }
-        } else {
-            int incl = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += v;
-            }
-            if (warp < 8 && lane == 31) hd.warp_sum[warp] = incl;
-            __syncthreads();
-            for (int w = 0; w < min(warp, 8); ++w) incl += hd.warp_sum[w];
-            if (tid < E) s_pre[tid + 1] = incl;
-            if (tid == 0) s_pre[0] = 0;
+            s_steps[tid] = steps;
         }
+        __syncthreads();
+        if (PHASE == 1 && tid < experts) {
+            int before = 0;
+            for (int e = 0; e < experts; ++e) before += s_steps[e] > steps || (s_steps[e] == steps && e < tid) ? 1 : 0;
+            s_order[before] = tid;
+        }
+        __syncthreads();
+        int items = 0, w_items = 0;
+        if (tid < experts) {
+            items = tiles * (PHASE == 0 ? (p.prob[problem_of(tid)].F + 255) / 256 : h_blocks);
+            if (PHASE == 1) {
+                const int F = p.prob[problem_of(s_order[tid])].F;
+                w_items = h_blocks * (F / 128 + (F + 255) / 256);
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, items, o), w = __shfl_up_sync(0xFFFFFFFFu, w_items, o);
+            if (lane >= o) { items += v; w_items += w; }
+        }
+        if (lane == 31) { hd.warp_sum[0][warp] = items; hd.warp_sum[1][warp] = w_items; }
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) { items += hd.warp_sum[0][w]; w_items += hd.warp_sum[1][w]; }
+        if (tid < experts) { s_pre[tid + 1] = items; s_wpre[tid + 1] = w_items; }
+        if (tid == 0) { s_pre[0] = 0; s_wpre[0] = 0; }
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&hd.tmem)), "r"(TMEM_COLS)
@@ -202,7 +237,7 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
         const bool ok = leader ? mbar_wait(bar, par, abort_flag) : mbar_wait_acquire_cluster(bar, par, abort_flag);
         if (ok) {
             const int4 v = hd.item[q];
-            it = GradItem{v.x, v.y, v.z, v.w};
+            it = GradItem{v.x, v.y, v.z, v.w & 0x0FFFFFFF, v.w >> 28};
         }
         return ok;
     };
@@ -217,14 +252,16 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
         it.valid = __shfl_sync(0xFFFFFFFFu, it.valid, 0);
         it.e = __shfl_sync(0xFFFFFFFFu, it.e, 0);
         it.b = __shfl_sync(0xFFFFFFFFu, it.b, 0);
+        it.kind = PHASE == 0 ? GRAD_ACT : __shfl_sync(0xFFFFFFFFu, it.kind, 0);
         if (ok && lane == 0) release_item(i);
         return ok && it.valid != 0;
     };
+    auto is_weights = [&](const GradItem& it) -> bool { return PHASE == 1 && it.kind != GRAD_DX; };
     auto columns_of = [&](const GradItem& it) -> int {            // N of the item's MMAs
-        if (KIND == GRAD_GATEUP) return 256;
-        if (KIND == GRAD_DOWN) return min(256, p.F - it.b * 256);
+        if (is_weights(it)) return it.kind == GRAD_GATEUP ? 256 : min(256, p.prob[problem_of(it.e)].F - it.b * 256);
         return (it.valid + 31) / 32 * 32;
     };
+    auto token_steps = [&](int e) -> int { return PHASE == 0 ? p.H / 64 : 2 * (p.prob[problem_of(e)].F / 64); };
 
     GradItem it{};
     if (warp == 0) {
@@ -233,11 +270,23 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
         int stage = 0, issued_k = 0;
         uint32_t phase = 0, bad = 0;
         for (int i = 0; take_item_warp(i, it); ++i) {
-            if constexpr (WEIGHTS) {
-                const int m_col = it.a * 256 + (int)rank * 128;
+            const int pr = problem_of(it.e);
+            const CUtensorMap* const map = maps.m[pr];
+            if (is_weights(it)) {
                 const int half = columns_of(it) >> 1;             // columns of the right operand this CTA supplies: 128 or 64
-                const int n_col = KIND == GRAD_GATEUP ? it.b * 128 : it.b * 256 + (int)rank * half;
-                const CUtensorMap* mb = KIND == GRAD_GATEUP && rank ? &tm_b1 : &tm_b0;
+                const CUtensorMap *ma, *mb;
+                int m_col, n_col;
+                if (it.kind == GRAD_GATEUP) {
+                    ma = map + (rank ? MAP_DU : MAP_DG);
+                    m_col = it.b * 128;
+                    mb = map + MAP_X;
+                    n_col = it.a * 256 + (int)rank * 128;
+                } else {
+                    ma = map + MAP_DY;
+                    m_col = it.a * 256 + (int)rank * 128;
+                    mb = map + MAP_ACT;
+                    n_col = it.b * 256 + (int)rank * half;
+                }
                 const uint32_t tx = 2 * G_BOX_BYTES + half * 128;
                 for (int r = s_rep[it.e]; r < s_rep[it.e + 1]; ++r) {
                     const int hi = s_hi[r];
@@ -250,8 +299,8 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
                         ++issued_k;
                         if (lead_lane && !bad) {
                             mbar_expect_tx_cluster(bar, tx);
-                            tma_load_2d_pair(dst, &tm_a0, bar, m_col, k0);
-                            tma_load_2d_pair(dst + G_BOX_BYTES, &tm_a0, bar, m_col + 64, k0);
+                            tma_load_2d_pair(dst, ma, bar, m_col, k0);
+                            tma_load_2d_pair(dst + G_BOX_BYTES, ma, bar, m_col + 64, k0);
                             tma_load_2d_pair(dst + 2 * G_BOX_BYTES, mb, bar, n_col, k0);
                             if (half > 64) tma_load_2d_pair(dst + 3 * G_BOX_BYTES, mb, bar, n_col + 64, k0);
                             if (leader) *prod_k = issued_k;
@@ -262,12 +311,13 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
             } else {
                 const int m_col = it.b * 256 + (int)rank * 128;
                 const int x_row = it.a + (int)rank * (columns_of(it) >> 1);
-                for (int kb = 0; kb < p.k_steps; ++kb) {
-                    const bool second = KIND == GRAD_DX && kb >= p.k_steps / 2;
-                    const int k = (second ? kb - p.k_steps / 2 : kb) * 64;
-                    const int w_row = it.e * (KIND == GRAD_ACT ? p.H : p.F) + k;
-                    const CUtensorMap* ma = second ? &tm_a1 : &tm_a0;
-                    const CUtensorMap* mb = second ? &tm_b1 : &tm_b0;
+                const int k_steps = token_steps(it.e), e = pr ? 0 : it.e;
+                for (int kb = 0; kb < k_steps; ++kb) {
+                    const bool second = PHASE == 1 && kb >= k_steps / 2;
+                    const int k = (second ? kb - k_steps / 2 : kb) * 64;
+                    const int w_row = e * (PHASE == 0 ? p.H : p.prob[pr].F) + k;
+                    const CUtensorMap* ma = map + (PHASE == 0 ? MAP_WD : second ? MAP_WU : MAP_WG);
+                    const CUtensorMap* mb = map + (PHASE == 0 ? MAP_DY_K : second ? MAP_DU_K : MAP_DG_K);
                     const uint32_t dst = ring + stage * G_STAGE_BYTES;
                     const uint32_t bar = map_to_cta(smem_u32(&hd.full[stage]), 0);
                     bad = mbar_wait_conv(smem_u32(&hd.empty[stage]), phase ^ 1u, abort_addr, bad, lead_lane);
@@ -295,8 +345,8 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
                 bad = mbar_wait_conv(smem_u32(&hd.tempty[acc]), (((uint32_t)i >> 1) & 1u) ^ 1u, abort_addr, bad, lead_lane);
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + (uint32_t)(acc * G_TILE);
-                const uint32_t idesc = G_IDESC_BASE | (WEIGHTS ? G_IDESC_B_MN : 0u) | ((uint32_t)(columns_of(it) >> 3) << 17);
-                if constexpr (WEIGHTS) {
+                const uint32_t idesc = G_IDESC_BASE | (is_weights(it) ? G_IDESC_B_MN : 0u) | ((uint32_t)(columns_of(it) >> 3) << 17);
+                if (is_weights(it)) {
                     uint32_t accumulate = 0;
                     for (int r = s_rep[it.e]; r < s_rep[it.e + 1]; ++r) {
                         const int hi = s_hi[r];
@@ -318,7 +368,8 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
                         }
                     }
                 } else {
-                    for (int kb = 0; kb < p.k_steps; ++kb) {
+                    const int k_steps = token_steps(it.e);
+                    for (int kb = 0; kb < k_steps; ++kb) {
                         const uint32_t src = ring + stage * G_STAGE_BYTES;
                         const uint64_t a_desc = smem_desc_mn(src), b_desc = smem_desc(src + 2 * G_BOX_BYTES);
                         bad = mbar_wait_conv(smem_u32(&hd.full[stage]), phase, abort_addr, bad, lead_lane);
@@ -339,9 +390,9 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
     } else if (warp == 2) {
         // ---- scheduler, leader CTA (see the forward kernel for why claims are held back to G_CLAIM_LEAD k-steps) ----
         if (lane == 0 && leader) {
-            const int per_expert = p.m_blocks * p.n_blocks;            // weight gradients
-            const int total = WEIGHTS ? E * per_expert : s_pre[E] * p.m_blocks;
-            int e = 0, pub_k = 0;
+            const int token_items = s_pre[experts];
+            const int total = token_items + (PHASE == 1 ? s_wpre[experts] : 0);
+            int e = 0, ord = 0, pub_k = 0;
             for (int i = 0;; ++i) {
                 if (pub_k - *prod_k >= G_CLAIM_LEAD) {
                     const unsigned long long t0 = global_ns();
@@ -359,13 +410,10 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
                 if (!mbar_wait(smem_u32(&hd.sched_empty[q]), (((uint32_t)i / G_SLOTS) & 1u) ^ 1u, abort_flag)) break;
                 int4 item = make_int4(0, 0, 0, 0);
                 if (w < total) {
-                    if constexpr (WEIGHTS) {
-                        const int ex = s_order[w / per_expert], local = w % per_expert;
-                        item = make_int4(local % p.m_blocks, 1, ex, local / p.m_blocks);
-                        pub_k += s_steps[ex];
-                    } else {
-                        while (w >= s_pre[e + 1] * p.m_blocks) ++e;    // w only grows
-                        const int nt = s_pre[e + 1] - s_pre[e], local = w - s_pre[e] * p.m_blocks;
+                    if (w < token_items) {
+                        while (w >= s_pre[e + 1]) ++e;                 // w only grows
+                        const int blocks = PHASE == 0 ? (p.prob[problem_of(e)].F + 255) / 256 : h_blocks;
+                        const int nt = (s_pre[e + 1] - s_pre[e]) / blocks, local = w - s_pre[e];
                         const int wb = local / nt;                     // block by block, so that an expert's token tiles share it
                         int tile = local - wb * nt, r = s_rep[e];
                         for (;; ++r) {
@@ -374,8 +422,17 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
                             tile -= n;
                         }
                         const int row0 = s_lo[r] + tile * G_TILE;
-                        item = make_int4(row0, min(G_TILE, s_hi[r] - row0), e, wb);
-                        pub_k += p.k_steps;
+                        item = make_int4(row0, min(G_TILE, s_hi[r] - row0), e, wb | ((PHASE == 0 ? GRAD_ACT : GRAD_DX) << 28));
+                        pub_k += token_steps(e);
+                    } else if (PHASE == 1) {
+                        const int v = w - token_items;
+                        while (v >= s_wpre[ord + 1]) ++ord;
+                        const int ex = s_order[ord], gateup = h_blocks * (p.prob[problem_of(ex)].F / 128);
+                        int local = v - s_wpre[ord];
+                        const int kind = local < gateup ? GRAD_GATEUP : GRAD_DOWN;
+                        if (kind == GRAD_DOWN) local -= gateup;
+                        item = make_int4(local % h_blocks, 1, ex, (local / h_blocks) | (kind << 28));
+                        pub_k += s_steps[ex];
                     }
                 }
                 hd.item[q] = item;
@@ -387,10 +444,14 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
         }
     } else if (warp == 3) {
         // ---- tail warp, both CTAs: zeroes the rows behind a segment's end inside the last MMA of a step ----
-        if constexpr (WEIGHTS) {
+        if constexpr (PHASE == 1) {
             int stage = 0;
             uint32_t part_phase = 0, bad = 0;                          // one phase bit per stage
             for (int i = 0; take_item_warp(i, it); ++i) {
+                if (!is_weights(it)) {
+                    stage = (stage + token_steps(it.e)) % G_STAGES;
+                    continue;
+                }
                 const int boxes = 2 + (columns_of(it) >> 7);           // 64-column boxes of both operands in this CTA
                 for (int r = s_rep[it.e]; r < s_rep[it.e + 1]; ++r) {
                     const int hi = s_hi[r];
@@ -426,50 +487,61 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
             __syncwarp();
             if (lane == 0) release_item(i);
             if (it.valid == 0) break;
+            const GradProblem& pr = p.prob[problem_of(it.e)];
+            // GRAD_ACT: the kept values of the warp's 32 features for 32 tokens from c on (lane j: the exponents of token c + j for the
+            // two blocks).  The first chunk's are fetched while the products still run.
+            const int f = it.b * 256 + d_row;
+            const bool live = f < pr.F;                                // the last block may be half a block (warp-uniform)
+            const size_t at0 = (size_t)it.a * pr.F + f;
+            auto fetch = [&](int c, uint32_t (&code)[32], uint32_t& ex) {
+                const uint16_t* const codes = reinterpret_cast<const uint16_t*>(pr.codes) + at0 + (size_t)c * pr.F;
+                const int rem = live ? it.valid - c : 0;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) code[j] = j < rem ? (uint32_t)__ldg(codes + (size_t)j * pr.F) : 0u;
+                if (lane < rem) {
+                    const uint16_t* const e0 = pr.exps + (size_t)(f / kCheckpointBlock - (lane >> 4)) * pr.rows + it.a + c + lane;
+                    ex = (uint32_t)__ldg(e0) | ((uint32_t)__ldg(e0 + pr.rows) << 16);
+                }
+            };
+            uint32_t code[32], ex = 0;
+            if constexpr (PHASE == 0) fetch(c_first, code, ex);
             const int acc = i & 1;
             if (!mbar_wait(smem_u32(&hd.tfull[acc]), ((uint32_t)i >> 1) & 1u, abort_flag)) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * G_TILE);
             const int n = columns_of(it);
-            if constexpr (KIND == GRAD_ACT) {
-                const int f = it.b * 256 + d_row;
-                const bool live = f < p.F;                             // the last block may be half a block (warp-uniform)
-                const int blk = f / kCheckpointBlock;
+            if constexpr (PHASE == 0) {
+                if (live) {
+                    uint16_t *dg = pr.dg + at0, *du = pr.du + at0, *act = pr.act + at0;
 #pragma unroll 1
-                for (int c = c_first; c < n && live; c += CSTEP) {
-                    uint32_t v[32];
-                    tmem_ld32(taddr + c, v);
-                    const int row = it.a + c, rem = it.valid - c;
-                    // lane j: the exponents of row j for the warp's two blocks
-                    uint32_t ex = 0;
-                    if (lane < rem) {
-                        const uint16_t* e0 = p.exps + (size_t)(blk - (lane >> 4)) * p.rows + row + lane;
-                        ex = (uint32_t)__ldg(e0) | ((uint32_t)__ldg(e0 + p.rows) << 16);
-                    }
-                    const uint16_t* code = reinterpret_cast<const uint16_t*>(p.codes) + (size_t)row * p.F + f;
-                    uint16_t *dg = p.out0 + (size_t)row * p.F + f, *du = p.out1 + (size_t)row * p.F + f, *act = p.out2 + (size_t)row * p.F + f;
-                    tmem_ld_wait();
+                    for (int c = c_first; c < n; c += CSTEP) {
+                        // The next chunk's values are all asked for before this chunk's arithmetic: a load among the arithmetic
+                        // would make the warp wait for it at the next use of any other load.
+                        uint32_t next[32], next_ex = 0, v[32];
+                        fetch(c + CSTEP, next, next_ex);
+                        tmem_ld32(taddr + c, v);
+                        const int rem = it.valid - c;
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const uint32_t pair = __shfl_sync(0xFFFFFFFFu, ex, j) >> (lane & 16);
-                        if (j < rem) {
-                            const uint32_t k = __ldg(code);
-                            const float g = (float)(int8_t)k * checkpoint_scale(pair & 255u);
-                            const float u = (float)(int8_t)(k >> 8) * checkpoint_scale((pair >> 8) & 255u);
-                            const float da = __uint_as_float(v[j]);
-                            const float s = __fdividef(1.0f, 1.0f + __expf(-g)), gs = g * s;
-                            *dg = to_bf16(da * u * (s * (1.0f + g * (1.0f - s))));
-                            *du = to_bf16(da * gs);
-                            *act = to_bf16(gs * u);
+                        for (int j = 0; j < 32; ++j) {
+                            const uint32_t pair = __shfl_sync(0xFFFFFFFFu, ex, j) >> (lane & 16);
+                            const size_t at = (size_t)(c + j) * pr.F;
+                            if (j < rem) {
+                                const float g = (float)(int8_t)code[j] * checkpoint_scale(pair & 255u);
+                                const float u = (float)(int8_t)(code[j] >> 8) * checkpoint_scale((pair >> 8) & 255u);
+                                const float da = __uint_as_float(v[j]);
+                                const float s = __fdividef(1.0f, 1.0f + __expf(-g)), gs = g * s;
+                                dg[at] = to_bf16(da * u * (s * (1.0f + g * (1.0f - s))));
+                                du[at] = to_bf16(da * gs);
+                                act[at] = to_bf16(gs * u);
+                            }
+                            code[j] = next[j];
                         }
-                        code += p.F;
-                        dg += p.F;
-                        du += p.F;
-                        act += p.F;
+                        ex = next_ex;
                     }
                 }
-            } else if constexpr (KIND == GRAD_DX) {
-                uint16_t* const col = p.out0 + (size_t)it.a * p.H + it.b * 256 + d_row;
+            } else if (it.kind == GRAD_DX) {
+                uint16_t* const col = pr.dx + (size_t)it.a * p.H + it.b * 256 + d_row;
 #pragma unroll 1
                 for (int c = c_first; c < n; c += CSTEP) {
                     uint32_t v[32];
@@ -484,36 +556,46 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
                     }
                 }
             } else {
-                const bool empty = s_steps[it.e] == 0;                 // nothing was accumulated: the gradient is zero
-                const int h = it.a * 256 + d_row;
+                const bool zero = s_steps[it.e] == 0;                  // nothing was accumulated: the gradient is zero
+                const int e = problem_of(it.e) ? 0 : it.e;
+                const CUtensorMap* mo;
+                int row, col;                                          // of this warp's 32 rows in the gradient
+                if (it.kind == GRAD_GATEUP) {
+                    mo = maps.m[problem_of(it.e)] + (rank ? MAP_OUT_U : MAP_OUT_G);
+                    row = e * pr.F + it.b * 128 + quad * 32;
+                    col = it.a * 256;
+                } else {
+                    mo = maps.m[problem_of(it.e)] + MAP_OUT_D;
+                    row = e * p.H + it.a * 256 + (int)rank * 128 + quad * 32;
+                    col = it.b * 256;
+                }
+                // row r of the buffer: 64 bytes, its 16-byte pieces in the 64-byte swizzle's order
+                uint8_t* const buf = out_buf + (warp - 4) * G_OUT_BYTES;
+                uint4* const mine = reinterpret_cast<uint4*>(buf + lane * 64);
 #pragma unroll 1
                 for (int c = c_first; c < n; c += CSTEP) {
                     uint32_t v[32];
-                    if (empty) {
+                    if (zero) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0u;
                     } else {
                         tmem_ld32(taddr + c, v);
                         tmem_ld_wait();
                     }
-                    if constexpr (KIND == GRAD_GATEUP) {
-                        // columns 0..127: dWg, 128..255: dWu; 32 lanes write 32 consecutive h of one feature
-                        const int f = it.b * 128 + (c & 127);
-                        uint16_t* ptr = (c < 128 ? p.out0 : p.out1) + ((size_t)it.e * p.F + f) * p.H + h;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the buffer's last store has read it
+                    __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            *ptr = to_bf16(__uint_as_float(v[j]));
-                            ptr += p.H;
-                        }
-                    } else {
-                        // a lane writes 32 consecutive features of its h
-                        uint4* ptr = reinterpret_cast<uint4*>(p.out0 + ((size_t)it.e * p.H + h) * p.F + it.b * 256 + c);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            ptr[j] = make_uint4(pack_bf16(__uint_as_float(v[8 * j]), __uint_as_float(v[8 * j + 1])),
-                                                pack_bf16(__uint_as_float(v[8 * j + 2]), __uint_as_float(v[8 * j + 3])),
-                                                pack_bf16(__uint_as_float(v[8 * j + 4]), __uint_as_float(v[8 * j + 5])),
-                                                pack_bf16(__uint_as_float(v[8 * j + 6]), __uint_as_float(v[8 * j + 7])));
+                    for (int j = 0; j < 4; ++j)
+                        mine[j ^ ((lane >> 1) & 3)] =
+                            make_uint4(pack_bf16(__uint_as_float(v[8 * j]), __uint_as_float(v[8 * j + 1])),
+                                       pack_bf16(__uint_as_float(v[8 * j + 2]), __uint_as_float(v[8 * j + 3])),
+                                       pack_bf16(__uint_as_float(v[8 * j + 4]), __uint_as_float(v[8 * j + 5])),
+                                       pack_bf16(__uint_as_float(v[8 * j + 6]), __uint_as_float(v[8 * j + 7])));
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(mo, smem_u32(buf), col + c, row);
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 }
             }
@@ -523,6 +605,7 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
         }
     }
 
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");          // a lane's own stores, none for most
     // ---- teardown, as in the forward kernel: a role that gave up tells the peer CTA ----
     if (*abort_flag)
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cta(abort_addr, 1u - rank)), "r"(1) : "memory");
@@ -536,13 +619,12 @@ grouped_grad_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_cons
     }
 }
 
-template <int KIND>
-int launch_grad(director_ctx* ctx, const char* name, const CUtensorMap& a0, const CUtensorMap& a1, const CUtensorMap& b0,
-                const CUtensorMap& b1, const GradParams& p, cudaStream_t st) {
+template <int PHASE>
+int launch_grad(director_ctx* ctx, const char* name, const GradMaps& maps, const GradParams& p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * ctx->pair_clusters));
     cfg.blockDim = dim3(G_THREADS);
-    cfg.dynamicSmemBytes = (size_t)grad_smem_bytes(p.n_rep, p.E);
+    cfg.dynamicSmemBytes = (size_t)grad_smem_bytes(p.n_rep, p.experts);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -554,76 +636,66 @@ int launch_grad(director_ctx* ctx, const char* name, const CUtensorMap& a0, cons
     cfg.attrs = attr;
     cfg.numAttrs = chain_allowed(st) ? 2 : 1;
     LaunchScope scope(ctx, st, name);
-    return cuda_status(cudaLaunchKernelEx(&cfg, grouped_grad_kernel<KIND>, a0, a1, b0, b1, p));
+    return cuda_status(cudaLaunchKernelEx(&cfg, grouped_grad_kernel<PHASE>, maps, p));
 }
 
-// The four launches for one set of experts over one segment table.
-int ffn_grad_pass(director_ctx* ctx, const FfnGrad& f, const int32_t* seg_offsets, int n_experts, int n_rep, int Fw, bool dense,
-                  void* dgu, void* act, unsigned int* counters, cudaStream_t st) {
-    const int H = ctx->shape.H;
-    const uint64_t rows = (uint64_t)f.kept.rows;
+// bf16 [rows, cols] row-major as the target of TMA stores: boxes of 32 rows x 32 columns, 64-byte swizzle
+bool map_out(director_ctx* ctx, CUtensorMap* map, void* base, uint64_t rows, uint64_t cols) {
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {cols * 2};
+    const cuuint32_t box[2] = {32, 32};
+    const cuuint32_t estr[2] = {1, 1};
+    return reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
+               map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// One problem's tensor maps and pointers.  dgu, act: the context's workspace.
+bool describe(director_ctx* ctx, const FfnGrad& f, uint64_t n_experts, int F, void* dgu, void* act, CUtensorMap* m, GradProblem& pr) {
+    const uint64_t H = (uint64_t)ctx->shape.H, rows = (uint64_t)f.kept.rows;
     uint16_t* const dg = static_cast<uint16_t*>(dgu);
-    uint16_t* const du = dg + rows * (uint64_t)Fw;
-    CUtensorMap wd, wg, wu;                                   // left operands: boxes of 64 contraction rows
-    CUtensorMap x_mn, dy_mn, dg_mn, du_mn, act_mn;            // operands of the weight gradients: the same boxes
-    CUtensorMap dy_k, dg_k, du_k;                             // token rows, contraction along the row
-    if (!map_2d(ctx, &wd, f.w_down, (uint64_t)n_experts * H, Fw, 64) || !map_2d(ctx, &wg, f.w_gate, (uint64_t)n_experts * Fw, H, 64) ||
-        !map_2d(ctx, &wu, f.w_up, (uint64_t)n_experts * Fw, H, 64) || !map_2d(ctx, &x_mn, f.x, rows, H, 64) ||
-        !map_2d(ctx, &dy_mn, f.dy, rows, H, 64) || !map_2d(ctx, &dg_mn, dg, rows, Fw, 64) || !map_2d(ctx, &du_mn, du, rows, Fw, 64) ||
-        !map_2d(ctx, &act_mn, act, rows, Fw, 64) || !map_2d(ctx, &dy_k, f.dy, rows, H) || !map_2d(ctx, &dg_k, dg, rows, Fw) ||
-        !map_2d(ctx, &du_k, du, rows, Fw))
-        return DIRECTOR_ERR_CUDA;
-    GradParams p{seg_offsets, ctx->d_rep_start, ctx->d_rep_slot, n_experts, n_rep, (int)rows, dense ? 1 : 0, H, Fw, 0, 0, 0,
-                 f.kept.codes, f.kept.exps, nullptr, nullptr, nullptr, ctx->d_status, counters};
-    p.m_blocks = (Fw + 255) / 256;
-    p.k_steps = H / 64;
-    p.out0 = dg;
-    p.out1 = du;
-    p.out2 = static_cast<uint16_t*>(act);
-    int rc = launch_grad<GRAD_ACT>(ctx, "grouped_grad_act_kernel", wd, wd, dy_k, dy_k, p, st);
-    if (rc != DIRECTOR_OK) return rc;
-    p.m_blocks = H / 256;
-    p.k_steps = 2 * (Fw / 64);
-    p.out0 = static_cast<uint16_t*>(f.dx);
-    p.counter = counters + 1;
-    rc = launch_grad<GRAD_DX>(ctx, "grouped_grad_dx_kernel", wg, wu, dg_k, du_k, p, st);
-    if (rc != DIRECTOR_OK) return rc;
-    p.n_blocks = Fw / 128;
-    p.out0 = static_cast<uint16_t*>(f.dw_gate);
-    p.out1 = static_cast<uint16_t*>(f.dw_up);
-    p.counter = counters + 2;
-    rc = launch_grad<GRAD_GATEUP>(ctx, "grouped_grad_gateup_kernel", x_mn, x_mn, dg_mn, du_mn, p, st);
-    if (rc != DIRECTOR_OK) return rc;
-    p.n_blocks = (Fw + 255) / 256;
-    p.out0 = static_cast<uint16_t*>(f.dw_down);
-    p.counter = counters + 3;
-    return launch_grad<GRAD_DOWN>(ctx, "grouped_grad_down_kernel", dy_mn, dy_mn, act_mn, act_mn, p, st);
+    uint16_t* const du = dg + rows * (uint64_t)F;
+    pr = GradProblem{F, (int)rows, f.kept.codes, f.kept.exps, dg, du, static_cast<uint16_t*>(act), static_cast<uint16_t*>(f.dx)};
+    return map_2d(ctx, m + MAP_WD, f.w_down, n_experts * H, F, 64) && map_2d(ctx, m + MAP_DY_K, f.dy, rows, H) &&
+           map_2d(ctx, m + MAP_WG, f.w_gate, n_experts * F, H, 64) && map_2d(ctx, m + MAP_WU, f.w_up, n_experts * F, H, 64) &&
+           map_2d(ctx, m + MAP_DG_K, dg, rows, F) && map_2d(ctx, m + MAP_DU_K, du, rows, F) &&
+           map_2d(ctx, m + MAP_X, f.x, rows, H, 64) && map_2d(ctx, m + MAP_DG, dg, rows, F, 64) &&
+           map_2d(ctx, m + MAP_DU, du, rows, F, 64) && map_2d(ctx, m + MAP_DY, f.dy, rows, H, 64) &&
+           map_2d(ctx, m + MAP_ACT, act, rows, F, 64) && map_out(ctx, m + MAP_OUT_G, f.dw_gate, n_experts * F, H) &&
+           map_out(ctx, m + MAP_OUT_U, f.dw_up, n_experts * F, H) && map_out(ctx, m + MAP_OUT_D, f.dw_down, n_experts * H, F);
 }
 
-template <int KIND>
+template <int PHASE>
 bool grad_opt_in() {
-    return cudaFuncSetAttribute(grouped_grad_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                grad_smem_bytes(kMaxG, kMaxE)) == cudaSuccess;
+    return cudaFuncSetAttribute(grouped_grad_kernel<PHASE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                grad_smem_bytes(kMaxG + 1, kMaxE + 1)) == cudaSuccess;
 }
 
 }  // namespace
 
-int ffn_grad_init(director_ctx*) {
-    return grad_opt_in<GRAD_ACT>() && grad_opt_in<GRAD_DX>() && grad_opt_in<GRAD_GATEUP>() && grad_opt_in<GRAD_DOWN>()
-               ? DIRECTOR_OK : DIRECTOR_ERR_CUDA;
-}
+int ffn_grad_init(director_ctx*) { return grad_opt_in<0>() && grad_opt_in<1>() ? DIRECTOR_OK : DIRECTOR_ERR_CUDA; }
 
 // routed: the permuted rows.  shared (x != nullptr): the S shared experts as one FFN of width S*F over the batch's own rows.
-int launch_expert_ffn_backward(director_ctx* ctx, int T, const int32_t* seg_offsets, const FfnGrad& routed, const FfnGrad& shared,
+int launch_expert_ffn_backward(director_ctx* ctx, const int32_t* seg_offsets, const FfnGrad& routed, const FfnGrad& shared,
                                cudaStream_t st) {
     StageScope stage(ctx, st, "stage_expert_ffn_backward");
     const director_shape& s = ctx->shape;
-    if (cudaMemsetAsync(ctx->d_grad_sched, 0, 8 * sizeof(unsigned int), st) != cudaSuccess) return DIRECTOR_ERR_CUDA;
-    const int rc = ffn_grad_pass(ctx, routed, seg_offsets, s.E, ctx->n_replicas, s.F, false, ctx->d_dgu, ctx->d_hidden,
-                                 ctx->d_grad_sched, st);
-    if (rc != DIRECTOR_OK || shared.x == nullptr) return rc;
-    return ffn_grad_pass(ctx, shared, nullptr, 1, 1, s.S * s.F, true, ctx->d_dgu_shared, ctx->d_hidden_shared,
-                         ctx->d_grad_sched + 4, st);
+    const int extra = shared.x != nullptr ? 1 : 0;
+    GradMaps maps;
+    GradParams p{seg_offsets, ctx->d_rep_start, ctx->d_rep_slot, s.E, s.E + extra, ctx->n_replicas + extra, s.H, {}, ctx->d_status,
+                 ctx->d_grad_sched, ctx->d_grad_sched + 1};
+    if (!describe(ctx, routed, s.E, s.F, ctx->d_dgu, ctx->d_hidden, maps.m[0], p.prob[0])) return DIRECTOR_ERR_CUDA;
+    if (extra) {
+        if (!describe(ctx, shared, 1, s.S * s.F, ctx->d_dgu_shared, ctx->d_hidden_shared, maps.m[1], p.prob[1])) return DIRECTOR_ERR_CUDA;
+    } else {
+        memcpy(maps.m[1], maps.m[0], sizeof(maps.m[0]));      // never used
+        p.prob[1] = p.prob[0];
+    }
+    const int rc = launch_grad<0>(ctx, "grouped_grad_act_kernel", maps, p, st);
+    if (rc != DIRECTOR_OK) return rc;
+    p.counter = ctx->d_grad_sched + 1;
+    p.other_counter = ctx->d_grad_sched;
+    return launch_grad<1>(ctx, "grouped_grad_weights_kernel", maps, p, st);
 }
 
 }  // namespace director
