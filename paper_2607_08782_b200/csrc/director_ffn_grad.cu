@@ -116,8 +116,6 @@ struct GradItem {
     int a, valid, e, b, kind;      // tokens: first row, rows (0: end), expert, block;   weights: h block, 1, expert, f block
 };
 
-__device__ __forceinline__ uint16_t to_bf16(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
-
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y) : "memory");
@@ -347,23 +345,24 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                 const uint32_t d_tmem = tmem_base + (uint32_t)(acc * G_TILE);
                 const uint32_t idesc = G_IDESC_BASE | (is_weights(it) ? G_IDESC_B_MN : 0u) | ((uint32_t)(columns_of(it) >> 3) << 17);
                 if (is_weights(it)) {
-                    uint32_t accumulate = 0;
+                    bool first = true;
                     for (int r = s_rep[it.e]; r < s_rep[it.e + 1]; ++r) {
                         const int hi = s_hi[r];
                         for (int k0 = s_lo[r]; k0 < hi; k0 += 64) {
-                            const int slices = (min(64, hi - k0) + 15) >> 4;
+                            const int rows = hi - k0;                  // MMAs of 16 rows each, up to four
                             const uint32_t src = ring + stage * G_STAGE_BYTES;
                             const uint64_t a_desc = smem_desc_mn(src), b_desc = smem_desc_mn(src + 2 * G_BOX_BYTES);
                             bad = mbar_wait_conv(smem_u32(&hd.full[stage]), phase, abort_addr, bad, lead_lane);
-                            if (hi - k0 < 64) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the tail warps' zeros
+                            if (rows < 64) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the tail warps' zeros
                             tc_fence_after();
                             if (lead_lane && !bad) {
-                                for (int k = 0; k < slices; ++k) {
-                                    umma_pair_n(d_tmem, a_desc + 128u * k, b_desc + 128u * k, idesc, accumulate);
-                                    accumulate = 1;
-                                }
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (16 * k < rows)
+                                        umma_pair_n(d_tmem, a_desc + 128u * k, b_desc + 128u * k, idesc, first && k == 0 ? 0u : 1u);
                                 umma_commit_both(smem_u32(&hd.empty[stage]));
                             }
+                            first = false;
                             if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
                         }
                     }
@@ -488,22 +487,27 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
             if (lane == 0) release_item(i);
             if (it.valid == 0) break;
             const GradProblem& pr = p.prob[problem_of(it.e)];
-            // GRAD_ACT: the kept values of the warp's 32 features for 32 tokens from c on (lane j: the exponents of token c + j for the
-            // two blocks).  The first chunk's are fetched while the products still run.
-            const int f = it.b * 256 + d_row;
-            const bool live = f < pr.F;                                // the last block may be half a block (warp-uniform)
-            const size_t at0 = (size_t)it.a * pr.F + f;
-            auto fetch = [&](int c, uint32_t (&code)[32], uint32_t& ex) {
+            // D[feature, token] has a feature a lane.  Two lanes share their two features and split the tokens between them - the even
+            // lane finishes the even tokens, the odd lane the odd ones, one shuffle per token pair - so that what is read and
+            // written in global memory are pairs of features.
+            const bool odd = (lane & 1) != 0;
+            const int d_pair = d_row & ~1;                             // first of the lane pair's two features
+            // GRAD_ACT: the kept values of 32 tokens from c on (code[m]: both features at token c + 2m + odd; ex of lane j: the
+            // exponents of token c + j for the warp's two blocks).  The first chunk's are fetched while the products still run.
+            const bool live = it.b * 256 + d_row < pr.F;               // the last block may be half a block (warp-uniform)
+            const size_t at0 = (size_t)(it.a + (odd ? 1 : 0)) * pr.F + it.b * 256 + d_pair;
+            auto fetch = [&](int c, uint32_t (&code)[16], uint32_t& ex) {
                 const uint16_t* const codes = reinterpret_cast<const uint16_t*>(pr.codes) + at0 + (size_t)c * pr.F;
                 const int rem = live ? it.valid - c : 0;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) code[j] = j < rem ? (uint32_t)__ldg(codes + (size_t)j * pr.F) : 0u;
+                for (int m = 0; m < 16; ++m)
+                    code[m] = 2 * m + (odd ? 1 : 0) < rem ? __ldg(reinterpret_cast<const uint32_t*>(codes + (size_t)(2 * m) * pr.F)) : 0u;
                 if (lane < rem) {
-                    const uint16_t* const e0 = pr.exps + (size_t)(f / kCheckpointBlock - (lane >> 4)) * pr.rows + it.a + c + lane;
+                    const uint16_t* const e0 = pr.exps + (size_t)((it.b * 256 + d_row - lane) / kCheckpointBlock) * pr.rows + it.a + c + lane;
                     ex = (uint32_t)__ldg(e0) | ((uint32_t)__ldg(e0 + pr.rows) << 16);
                 }
             };
-            uint32_t code[32], ex = 0;
+            uint32_t code[16], ex = 0;
             if constexpr (PHASE == 0) fetch(c_first, code, ex);
             const int acc = i & 1;
             if (!mbar_wait(smem_u32(&hd.tfull[acc]), ((uint32_t)i >> 1) & 1u, abort_flag)) break;
@@ -517,42 +521,53 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     for (int c = c_first; c < n; c += CSTEP) {
                         // The next chunk's values are all asked for before this chunk's arithmetic: a load among the arithmetic
                         // would make the warp wait for it at the next use of any other load.
-                        uint32_t next[32], next_ex = 0, v[32];
+                        uint32_t next[16], next_ex = 0, v[32];
                         fetch(c + CSTEP, next, next_ex);
                         tmem_ld32(taddr + c, v);
-                        const int rem = it.valid - c;
+                        const int rem = it.valid - c - (odd ? 1 : 0);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const uint32_t pair = __shfl_sync(0xFFFFFFFFu, ex, j) >> (lane & 16);
-                            const size_t at = (size_t)(c + j) * pr.F;
-                            if (j < rem) {
-                                const float g = (float)(int8_t)code[j] * checkpoint_scale(pair & 255u);
-                                const float u = (float)(int8_t)(code[j] >> 8) * checkpoint_scale((pair >> 8) & 255u);
-                                const float da = __uint_as_float(v[j]);
+                        for (int m = 0; m < 16; ++m) {
+                            const float other = __uint_as_float(__shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * m] : v[2 * m + 1], 1));
+                            const float mine = __uint_as_float(odd ? v[2 * m + 1] : v[2 * m]);
+                            const uint32_t pair = __shfl_sync(0xFFFFFFFFu, ex, 2 * m + (odd ? 1 : 0)) >> (lane & 16);
+                            const size_t at = (size_t)(c + 2 * m) * pr.F;
+                            const float sg = checkpoint_scale(pair & 255u), su = checkpoint_scale((pair >> 8) & 255u);
+                            float dg2[2], du2[2], act2[2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const float da = (k == 0) == odd ? other : mine;
+                                const float g = (float)(int8_t)(code[m] >> (16 * k)) * sg, u = (float)(int8_t)(code[m] >> (16 * k + 8)) * su;
                                 const float s = __fdividef(1.0f, 1.0f + __expf(-g)), gs = g * s;
-                                dg[at] = to_bf16(da * u * (s * (1.0f + g * (1.0f - s))));
-                                du[at] = to_bf16(da * gs);
-                                act[at] = to_bf16(gs * u);
+                                dg2[k] = da * u * (s * (1.0f + g * (1.0f - s)));
+                                du2[k] = da * gs;
+                                act2[k] = gs * u;
                             }
-                            code[j] = next[j];
+                            if (2 * m < rem) {
+                                *reinterpret_cast<uint32_t*>(dg + at) = pack_bf16(dg2[0], dg2[1]);
+                                *reinterpret_cast<uint32_t*>(du + at) = pack_bf16(du2[0], du2[1]);
+                                *reinterpret_cast<uint32_t*>(act + at) = pack_bf16(act2[0], act2[1]);
+                            }
+                            code[m] = next[m];
                         }
                         ex = next_ex;
                     }
                 }
             } else if (it.kind == GRAD_DX) {
-                uint16_t* const col = pr.dx + (size_t)it.a * p.H + it.b * 256 + d_row;
+                uint16_t* const col = pr.dx + (size_t)(it.a + (odd ? 1 : 0)) * p.H + it.b * 256 + d_pair;
 #pragma unroll 1
                 for (int c = c_first; c < n; c += CSTEP) {
                     uint32_t v[32];
                     tmem_ld32(taddr + c, v);
                     tmem_ld_wait();
                     uint16_t* ptr = col + (size_t)c * p.H;
-                    const int rem = it.valid - c;
+                    const int rem = it.valid - c - (odd ? 1 : 0);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        if (j < rem) *ptr = to_bf16(__uint_as_float(v[j]));
-                        ptr += p.H;
+                    for (int m = 0; m < 16; ++m) {
+                        const float other = __uint_as_float(__shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * m] : v[2 * m + 1], 1));
+                        const float mine = __uint_as_float(odd ? v[2 * m + 1] : v[2 * m]);
+                        if (2 * m < rem) *reinterpret_cast<uint32_t*>(ptr) = odd ? pack_bf16(other, mine) : pack_bf16(mine, other);
+                        ptr += 2 * (size_t)p.H;
                     }
                 }
             } else {
