@@ -121,6 +121,12 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y) : "memory");
 }
 
+// 16 bytes into the shared memory of a CTA of the cluster, counted on an mbarrier there when they have arrived
+__device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, int4 v, uint32_t cluster_bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(cluster_bar) : "memory");
+}
+
 // PHASE 0: GRAD_ACT.  PHASE 1: GRAD_DX, GRAD_GATEUP, GRAD_DOWN.
 template <int PHASE>
 __global__ void __launch_bounds__(G_THREADS, 1)
@@ -232,7 +238,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     auto take_item = [&](int i, GradItem& it) -> bool {
         const int q = i & (G_SLOTS - 1);
         const uint32_t par = ((uint32_t)i / G_SLOTS) & 1u, bar = smem_u32(&hd.sched_full[q]);
-        const bool ok = leader ? mbar_wait(bar, par, abort_flag) : mbar_wait_acquire_cluster(bar, par, abort_flag);
+        const bool ok = mbar_wait(bar, par, abort_flag);
         if (ok) {
             const int4 v = hd.item[q];
             it = GradItem{v.x, v.y, v.z, v.w & 0x0FFFFFFF, v.w >> 28};
@@ -353,7 +359,6 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                             const uint32_t src = ring + stage * G_STAGE_BYTES;
                             const uint64_t a_desc = smem_desc_mn(src), b_desc = smem_desc_mn(src + 2 * G_BOX_BYTES);
                             bad = mbar_wait_conv(smem_u32(&hd.full[stage]), phase, abort_addr, bad, lead_lane);
-                            if (rows < 64) asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the tail warps' zeros
                             tc_fence_after();
                             if (lead_lane && !bad) {
 #pragma unroll
@@ -435,9 +440,11 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     }
                 }
                 hd.item[q] = item;
-                st_cluster_v4(map_to_cta(smem_u32(&hd.item[q]), 1), item);
                 mbar_arrive(smem_u32(&hd.sched_full[q]));
-                mbar_arrive_cluster_release(map_to_cta(smem_u32(&hd.sched_full[q]), 1));
+                // the peer's copy carries its own signal: no release at cluster scope, which would cost as much as a short item
+                const uint32_t peer_bar = map_to_cta(smem_u32(&hd.sched_full[q]), 1);
+                mbar_expect_tx_cluster(peer_bar, 16);
+                st_async_v4(map_to_cta(smem_u32(&hd.item[q]), 1), item, peer_bar);
                 if (w >= total) break;
             }
         }
@@ -460,14 +467,18 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                             bad = mbar_wait_conv(smem_u32(&hd.part[stage]), (part_phase >> stage) & 1u, abort_addr, bad, 1u);
                             part_phase ^= 1u << stage;
                             if (!bad) {
-                                const int zero = ((valid + 15) & ~15) - valid, vecs = zero * 8;    // whole rows: the swizzle stays inside one
-                                uint8_t* const base = smem_raw + (ring - raw) + stage * G_STAGE_BYTES + valid * 128;
-                                for (int v = lane; v < boxes * vecs; v += 32)
-                                    *reinterpret_cast<uint4*>(base + (v / vecs) * G_BOX_BYTES + (v % vecs) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                // whole rows of 128 bytes (the swizzle stays inside one): eight lanes a row, four rows at a time
+                                const int last = (valid + 15) & ~15;
+                                uint8_t* const base = smem_raw + (ring - raw) + stage * G_STAGE_BYTES + (lane & 7) * 16;
+                                for (int row = valid + (lane >> 3); row < last; row += 4)
+                                    for (int b = 0; b < boxes; ++b)
+                                        *reinterpret_cast<uint4*>(base + b * G_BOX_BYTES + row * 128) = make_uint4(0u, 0u, 0u, 0u);
                                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // before the tensor core reads them
                             }
                             __syncwarp();
-                            if (lane == 0 && !bad) mbar_arrive_cluster_release(map_to_cta(smem_u32(&hd.full[stage]), 0));
+                            // The zeros lie in this CTA's own shared memory and are read by its own tensor core: the proxy fence has put
+                            // them there, a plain arrive tells the leader (cluster-scope release and acquire cost 1700 cycles each).
+                            if (lane == 0 && !bad) mbar_arrive_cluster(map_to_cta(smem_u32(&hd.full[stage]), 0));
                         }
                         if (++stage == G_STAGES) stage = 0;
                     }
