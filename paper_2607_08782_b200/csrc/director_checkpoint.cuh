@@ -7,7 +7,7 @@
 // The largest magnitude gets a code of 64 to 127, so the error of a value is at most 2^-7 of the largest of its block (half a
 // step of 2^-6; a magnitude above 127.5 steps is held at 127, which adds less than another half step).  A power of two makes
 // both conversions exact up to the one rounding.  Why 16: in the gate|up GEMM's accumulator a warp holds exactly 16 features
-// of both, so the maxima are warp reductions.  Why gate and up apart: their magnitudes differ by layer, and the smaller of the
+// of both, so the maxima stay inside a warp.  Why gate and up apart: their magnitudes differ by layer, and the smaller of the
 // two would lose its bits to the other's scale.  A block that holds a NaN or an infinity has e = 255 and codes of zero, and its
 // values read as NaN: the gradient then shows that the activations were not finite.
 #pragma once
@@ -27,19 +27,26 @@ struct Checkpoint {
 };
 
 #ifdef __CUDACC__
-// from the bit pattern of the block's largest magnitude (magnitudes order as their bit patterns do; NaN above infinity)
-__device__ __forceinline__ uint32_t checkpoint_exponent(uint32_t max_bits) {
-    const uint32_t biased = max_bits >> 23;
-    return biased == 255u ? 255u : (biased > 7u ? biased - 6u : 1u);
+// The code in the low byte, two's complement; scale = 2^(127 - e).  Adding 1.5 * 2^23 rounds to the nearest integer, ties to
+// even, and leaves it in the low bits (the product is exact, so there is the one rounding).
+__device__ __forceinline__ uint32_t checkpoint_code(float v, float scale) {
+    constexpr float magic = 12582912.0f;
+    return __float_as_uint(fminf(fmaxf(fmaf(v, scale, magic), magic - 127.0f), magic + 127.0f));
 }
-__device__ __forceinline__ int checkpoint_code(float v, uint32_t e) {
-    const float scaled = v * __uint_as_float((254u - e) << 23);       // 2^(127 - e)
-    const int code = __float2int_rn(fminf(fmaxf(scaled, -127.0f), 127.0f));
-    return e == 255u ? 0 : code;
+// Magnitudes order as their bit patterns do, NaN above infinity, and so do their upper halves, which hold the exponents.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 // 2^(e - 127), NaN for e = 255
 __device__ __forceinline__ float checkpoint_scale(uint32_t e) {
     return __uint_as_float(e == 255u ? 0x7FC00000u : e << 23);
+}
+// The value of byte `byte` of four codes, given as codes ^ 0x80808080 (each plus 128): the byte in the low end of 2^23 is that
+// integer as a float.  (An integer conversion instruction has a quarter of the rate of these.)
+__device__ __forceinline__ float checkpoint_value(uint32_t biased_codes, int byte, float scale) {
+    return (__uint_as_float(__byte_perm(biased_codes, 0x4B000000u, 0x7440u + byte)) - 8388736.0f) * scale;
 }
 #endif
 

@@ -544,11 +544,12 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                             const uint32_t pair = __shfl_sync(0xFFFFFFFFu, ex, 2 * m + (odd ? 1 : 0)) >> (lane & 16);
                             const size_t at = (size_t)(c + 2 * m) * pr.F;
                             const float sg = checkpoint_scale(pair & 255u), su = checkpoint_scale((pair >> 8) & 255u);
+                            const uint32_t biased = code[m] ^ 0x80808080u;
                             float dg2[2], du2[2], act2[2];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
                                 const float da = (k == 0) == odd ? other : mine;
-                                const float g = (float)(int8_t)(code[m] >> (16 * k)) * sg, u = (float)(int8_t)(code[m] >> (16 * k + 8)) * su;
+                                const float g = checkpoint_value(biased, 2 * k, sg), u = checkpoint_value(biased, 2 * k + 1, su);
                                 const float s = __fdividef(1.0f, 1.0f + __expf(-g)), gs = g * s;
                                 dg2[k] = da * u * (s * (1.0f + g * (1.0f - s)));
                                 du2[k] = da * gs;

@@ -579,25 +579,32 @@ grouped_gemm_swap_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
                     tmem_ld_wait();
                     uint16_t* ptr = ocol + (size_t)c * out_pitch;       // my token of pair m is row c + 2m (+1 if odd)
                     const int rem = t.valid - c - (odd ? 1 : 0);        // store pair m iff 2m < rem
+                    const Checkpoint& kept = t.prob ? p.dense_kept : p.kept;
+                    // a (gate, up) pair of codes is one 16-bit word of [rows][F]
+                    uint16_t* code = reinterpret_cast<uint16_t*>(kept.codes) + (CHECKPOINT ? (ptr - out) : 0);
+                    uint16_t* const code0 = code;
+                    uint32_t exps = 0, top[16];
+                    bool not_finite = false;                            // in this chunk, warp-uniform
+                    const uint32_t pick_codes = i_am_gate ? 0x0040u : 0x0004u;                       // byte 0: the gate's, byte 1: the up's
+                    const uint32_t pick_exps = (i_am_gate ? 0x0040u : 0x0004u) + (odd ? 0x0022u : 0u);
                     if constexpr (CHECKPOINT) {
-                        // this warp holds the gate and up values of 16 features - one block of the checkpoint - for 32 tokens:
-                        // per token, two warp-wide maxima of the magnitudes' bit patterns give the block's two exponents
-                        const Checkpoint& kept = t.prob ? p.dense_kept : p.kept;
-                        const int chunk_row = t.row0 + c, in_tile = t.valid - c;
-                        int8_t* code = kept.codes + (size_t)chunk_row * (2 * out_pitch) + 2 * f + (i_am_gate ? 0 : 1);
-                        uint32_t exps = 0;                              // lane j keeps token j's pair of exponents
+                        // The warp holds the gate and up values of 16 features - one block of the checkpoint.  A block's exponent is
+                        // that of its largest magnitude: the upper halves of two tokens' magnitudes are packed into a word and
+                        // reduced over the lanes of this lane's kind (gate or up) by shuffles.  All 16 words take a step together:
+                        // one after the other, the 64 dependent shuffles were most of the epilogue's time.
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const uint32_t mag = v[j] & 0x7FFFFFFFu;
-                            const uint32_t eg = checkpoint_exponent(__reduce_max_sync(0xFFFFFFFFu, i_am_gate ? mag : 0u));
-                            const uint32_t eu = checkpoint_exponent(__reduce_max_sync(0xFFFFFFFFu, i_am_gate ? 0u : mag));
-                            if (lane == j) exps = eg | (eu << 8);
-                            if (j < in_tile) *code = (int8_t)checkpoint_code(__uint_as_float(v[j]), i_am_gate ? eg : eu);
-                            code += 2 * out_pitch;
+                        for (int m = 0; m < 16; ++m) top[m] = __byte_perm(v[2 * m], v[2 * m + 1], 0x7632) & 0x7FFF7FFFu;
+#pragma unroll
+                        for (int o = 2; o < 32; o <<= 1)
+#pragma unroll
+                            for (int m = 0; m < 16; ++m) top[m] = max_u16x2(top[m], __shfl_xor_sync(0xFFFFFFFFu, top[m], o));
+                        uint32_t all = 0;
+#pragma unroll
+                        for (int m = 0; m < 16; ++m) {
+                            all = max_u16x2(all, top[m]);
+                            top[m] = max_u16x2((top[m] >> 7) & 0x00FF00FFu, 0x00070007u) - 0x00060006u;   // checkpoint_exponent, finite
                         }
-                        if (lane < in_tile)
-                            kept.exps[(size_t)((t.wb * 128 + (int)rank * 64 + quad * 16) / kCheckpointBlock) * kept.rows + chunk_row + lane] =
-                                (uint16_t)exps;
+                        not_finite = __any_sync(0xFFFFFFFFu, (all & 0xFFFFu) >= 0x7F80u || all >= 0x7F800000u);
                     }
 #pragma unroll
                     for (int m = 0; m < 16; ++m) {
@@ -605,9 +612,38 @@ grouped_gemm_swap_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
                         const float send = __uint_as_float(odd ? v[2 * m] : v[2 * m + 1]);   // my value at the partner's token
                         const float other = __shfl_xor_sync(0xFFFFFFFFu, send, 1);           // partner's value at my token
                         const float g = i_am_gate ? mine : other, u = i_am_gate ? other : mine;
+                        if constexpr (CHECKPOINT) {
+                            const uint32_t e_mine = top[m], e_other = __shfl_xor_sync(0xFFFFFFFFu, e_mine, 1);   // two tokens each
+                            // 2^(127 - e) of my token's block of my kind and of the partner's
+                            const float s_mine = __uint_as_float(((0x00FE00FEu - e_mine) << (odd ? 7 : 23)) & 0x7F800000u);
+                            const float s_other = __uint_as_float(((0x00FE00FEu - e_other) << (odd ? 7 : 23)) & 0x7F800000u);
+                            const uint32_t pair = __byte_perm(e_mine, e_other, pick_exps);
+                            if ((lane >> 1) == m) exps = pair;               // lane j keeps token j's
+                            if (2 * m < rem)
+                                *code = (uint16_t)__byte_perm(checkpoint_code(mine, s_mine), checkpoint_code(other, s_other), pick_codes);
+                            code += two_rows;
+                        }
                         const float h = __fdividef(g * u, 1.0f + __expf(-g));
                         if (2 * m < rem) *ptr = __bfloat16_as_ushort(__float2bfloat16_rn(h));
                         ptr += two_rows;
+                    }
+                    if constexpr (CHECKPOINT) {
+                        if (not_finite) {
+                            // rare: blocks with a NaN or an infinity (their exponents came out as 249) get exponent 255 and codes of zero
+#pragma unroll 1
+                            for (int j = 0; j < 32; ++j) {
+                                const uint32_t pair = __shfl_sync(0xFFFFFFFFu, exps, j);
+                                const bool bad_g = (pair & 255u) == 249u, bad_u = ((pair >> 8) & 255u) == 249u;
+                                if ((bad_g || bad_u) && odd == ((j & 1) != 0) && c + j < t.valid) {
+                                    uint16_t* const at = code0 + (size_t)(j & ~1) * out_pitch;
+                                    *at = (uint16_t)(*at & ((bad_g ? 0u : 0x00FFu) | (bad_u ? 0u : 0xFF00u)));
+                                }
+                            }
+                            exps |= ((exps & 255u) == 249u ? 255u : 0u) | (((exps >> 8) & 255u) == 249u ? 0xFF00u : 0u);
+                        }
+                        if (c + lane < t.valid)
+                            kept.exps[(size_t)((t.wb * 128 + (int)rank * 64 + quad * 16) / kCheckpointBlock) * kept.rows + t.row0 + c + lane] =
+                                (uint16_t)exps;
                     }
                 }
             } else {

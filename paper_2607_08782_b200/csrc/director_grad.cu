@@ -110,29 +110,46 @@ route_backward_kernel(const int32_t* __restrict__ topk_idx, const float* __restr
 
 // ---- the 8-bit checkpoint as numbers -----------------------------------------------------------------------------
 //
-// One thread per block of 16 features of a row: 32 bytes of codes and two exponents in, 16 gate and 16 up values out in bf16
-// (seven bits and a sign times a power of two: exact).
+// A CTA takes 32 rows x 16 blocks of 16 features: the exponents, which lie along the rows, go through shared memory; a lane
+// turns half a block - 16 bytes of codes - into 8 gate and 8 up values, so that a warp reads 512 and writes 2 x 512
+// consecutive bytes.  Codes of seven bits and a sign times a power of two are exact in bf16.
+constexpr int kDecodeRows = 32, kDecodeBlocks = 16;
+
 __global__ void __launch_bounds__(256)
 checkpoint_decode_kernel(const uint4* __restrict__ codes, const uint16_t* __restrict__ exps, uint4* __restrict__ gate,
-                         uint4* __restrict__ up, int rows, int blocks) {
+                         uint4* __restrict__ up, int rows, int blocks, int row_tiles) {
+    __shared__ uint16_t s_exp[kDecodeBlocks][kDecodeRows];
     chain_prologue();
-    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= (long long)rows * blocks) return;
-    const int row = (int)(i / blocks), b = (int)(i % blocks);
-    const uint32_t e = __ldg(exps + (size_t)b * rows + row);
-    const float sg = checkpoint_scale(e & 255u), su = checkpoint_scale(e >> 8);
-    const uint4 c0 = __ldcs(codes + 2 * i), c1 = __ldcs(codes + 2 * i + 1);
-    const uint32_t c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-    uint32_t g[8], u[8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row0 = (int)(blockIdx.x % row_tiles) * kDecodeRows, b0 = (int)(blockIdx.x / row_tiles) * kDecodeBlocks;
+    for (int b = warp; b < kDecodeBlocks; b += 8)
+        s_exp[b][lane] = b0 + b < blocks && row0 + lane < rows ? __ldg(exps + (size_t)(b0 + b) * rows + row0 + lane) : 0;
+    const int half = 2 * b0 + lane;                           // which 8 features of the row
+    uint4 c[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        g[j] = pack_bf16x2((float)(int8_t)c[j] * sg, (float)(int8_t)(c[j] >> 16) * sg);
-        u[j] = pack_bf16x2((float)(int8_t)(c[j] >> 8) * su, (float)(int8_t)(c[j] >> 24) * su);
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + warp * 4 + i;
+        c[i] = half < 2 * blocks && row < rows ? __ldcs(codes + (size_t)row * (2 * blocks) + half) : make_uint4(0u, 0u, 0u, 0u);
     }
-    gate[2 * i] = make_uint4(g[0], g[1], g[2], g[3]);
-    gate[2 * i + 1] = make_uint4(g[4], g[5], g[6], g[7]);
-    up[2 * i] = make_uint4(u[0], u[1], u[2], u[3]);
-    up[2 * i + 1] = make_uint4(u[4], u[5], u[6], u[7]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + warp * 4 + i;
+        if (half >= 2 * blocks || row >= rows) continue;
+        const uint32_t e = s_exp[lane >> 1][warp * 4 + i];
+        const float sg = checkpoint_scale(e & 255u), su = checkpoint_scale(e >> 8);
+        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+        uint32_t g[4], u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t biased = w[j] ^ 0x80808080u;
+            g[j] = pack_bf16x2(checkpoint_value(biased, 0, sg), checkpoint_value(biased, 2, sg));
+            u[j] = pack_bf16x2(checkpoint_value(biased, 1, su), checkpoint_value(biased, 3, su));
+        }
+        const size_t at = (size_t)row * (2 * blocks) + half;
+        gate[at] = make_uint4(g[0], g[1], g[2], g[3]);
+        up[at] = make_uint4(u[0], u[1], u[2], u[3]);
+    }
 }
 
 }  // namespace
@@ -163,11 +180,12 @@ int launch_route_backward(director_ctx* ctx, int T, const int32_t* topk_idx, con
 int launch_checkpoint_decode(director_ctx* ctx, int rows, int F, const Checkpoint& kept, void* gate, void* up,
                              cudaStream_t st) {
     const int blocks = F / kCheckpointBlock;
-    const unsigned grid = (unsigned)(((long long)rows * blocks + 255) / 256);
+    const int row_tiles = (rows + kDecodeRows - 1) / kDecodeRows;
+    const unsigned grid = (unsigned)row_tiles * (unsigned)((blocks + kDecodeBlocks - 1) / kDecodeBlocks);
     LaunchScope scope(ctx, st, "checkpoint_decode_kernel");
     return cuda_status(launch_chained(checkpoint_decode_kernel, dim3(grid), dim3(256), 0, st,
                                       reinterpret_cast<const uint4*>(kept.codes), static_cast<const uint16_t*>(kept.exps),
-                                      static_cast<uint4*>(gate), static_cast<uint4*>(up), rows, blocks));
+                                      static_cast<uint4*>(gate), static_cast<uint4*>(up), rows, blocks, row_tiles));
 }
 
 }  // namespace director
