@@ -118,11 +118,23 @@ def _ptr(t):
     return t.ctypes.data
 
 
-def _need(where: str, **tensors):
-    """Checks the tensors of a training call: name = (tensor, dtype name, elements).  The C entry points see bare addresses; a
+# torch's dtypes and its raw-stream query, looked up once by the first context (torch is imported no earlier than that)
+_BF16 = _F32 = _I32 = _I8 = _U8 = _raw_stream = _current_device = None
+
+
+def _bind_torch():
+    global _BF16, _F32, _I32, _I8, _U8, _raw_stream, _current_device
+    import torch
+    _BF16, _F32, _I32, _I8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
+    _current_device = torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _need(where: str, *tensors):
+    """Checks the tensors of a training call, (name, tensor, dtype, elements) each.  The C entry points see bare addresses; a
     tensor of another type, a strided view or one too short would be read as something else."""
-    for name, (t, dtype, numel) in tensors.items():
-        if str(t.dtype) != dtype:
+    for name, t, dtype, numel in tensors:
+        if t.dtype is not dtype:
             raise TypeError(f"{where}: {name} is {t.dtype}, {dtype} is needed")
         if not t.is_contiguous() or not t.is_cuda:
             raise ValueError(f"{where}: {name} has to be a contiguous CUDA tensor")
@@ -130,10 +142,11 @@ def _need(where: str, **tensors):
             raise ValueError(f"{where}: {name} has {t.numel()} elements, {numel} are needed")
 
 
-_BF16, _F32, _I32, _I8, _U8 = "torch.bfloat16", "torch.float32", "torch.int32", "torch.int8", "torch.uint8"
-
-
 def _stream():
+    """The current stream of the current device, as torch.cuda.current_stream() has it (which builds an object for it: 3 us, as
+    long as a launch)."""
+    if _raw_stream is not None:
+        return _raw_stream(_current_device())
     import torch
     return torch.cuda.current_stream().cuda_stream
 
@@ -149,6 +162,7 @@ class Director:
 
     def __init__(self, T_max: int, H: int, F: int, E: int, K: int, S: int, R: int, C_max: int):
         self.lib = load_library()
+        _bind_torch()
         self.shape = DirectorShape(T_max, H, F, E, K, S, R, C_max)
         self._ctx = c_void_p()
         _check(self.lib.director_create(ctypes.byref(self.shape), ctypes.byref(self._ctx)), "director_create")
@@ -236,24 +250,25 @@ class Director:
     def combine_backward(self, T, dy, yp, inv_row, topk_w, dyp, dtopk_w):
         """Gradient of combine: dyp = each row's weight times its token's dy, dtopk_w = the dot products of dy and yp."""
         TK, H = T * self.shape.K, self.shape.H
-        _need("combine_backward", dy=(dy, _BF16, T * H), yp=(yp, _BF16, TK * H), inv_row=(inv_row, _I32, TK),
-              topk_w=(topk_w, _F32, TK), dyp=(dyp, _BF16, TK * H), dtopk_w=(dtopk_w, _F32, TK))
+        _need("combine_backward", ("dy", dy, _BF16, T * H), ("yp", yp, _BF16, TK * H), ("inv_row", inv_row, _I32, TK),
+              ("topk_w", topk_w, _F32, TK), ("dyp", dyp, _BF16, TK * H), ("dtopk_w", dtopk_w, _F32, TK))
         _check(self.lib.director_combine_backward(self._ctx, T, _ptr(dy), _ptr(yp), _ptr(inv_row), _ptr(topk_w), _ptr(dyp),
                                                   _ptr(dtopk_w), _stream()), "director_combine_backward")
 
     def dispatch_backward(self, T, dxp, inv_row, dx_shared, dx):
         """Gradient of dispatch's row copies: dx = the sum of a token's rows of dxp (+ dx_shared, which may be None)."""
         TK, H = T * self.shape.K, self.shape.H
-        _need("dispatch_backward", dxp=(dxp, _BF16, TK * H), inv_row=(inv_row, _I32, TK), dx=(dx, _BF16, T * H),
-              **({} if dx_shared is None else {"dx_shared": (dx_shared, _BF16, T * H)}))
+        _need("dispatch_backward", ("dxp", dxp, _BF16, TK * H), ("inv_row", inv_row, _I32, TK), ("dx", dx, _BF16, T * H))
+        if dx_shared is not None:
+            _need("dispatch_backward", ("dx_shared", dx_shared, _BF16, T * H))
         _check(self.lib.director_dispatch_backward(self._ctx, T, _ptr(dxp), _ptr(inv_row), _ptr(dx_shared), _ptr(dx),
                                                    _stream()), "director_dispatch_backward")
 
     def route_backward(self, T, topk_idx, topk_w, dtopk_w, dlogits):
         """Gradient of route: dlogits [T,E], zero where an expert was not chosen."""
         TK = T * self.shape.K
-        _need("route_backward", topk_idx=(topk_idx, _I32, TK), topk_w=(topk_w, _F32, TK), dtopk_w=(dtopk_w, _F32, TK),
-              dlogits=(dlogits, _F32, T * self.shape.E))
+        _need("route_backward", ("topk_idx", topk_idx, _I32, TK), ("topk_w", topk_w, _F32, TK), ("dtopk_w", dtopk_w, _F32, TK),
+              ("dlogits", dlogits, _F32, T * self.shape.E))
         _check(self.lib.director_route_backward(self._ctx, T, _ptr(topk_idx), _ptr(topk_w), _ptr(dtopk_w), _ptr(dlogits),
                                                 _stream()), "director_route_backward")
 
@@ -263,16 +278,16 @@ class Director:
         [F/16,T*K,2]; the shared experts' likewise) for expert_ffn_backward."""
         s = self.shape
         TK = T * s.K
-        need = dict(xp=(xp, _BF16, TK * s.H), seg_offsets=(seg_offsets, _I32, s.R * s.C_max + 1),
-                    w_gate=(w_gate, _BF16, s.E * s.F * s.H), w_up=(w_up, _BF16, s.E * s.F * s.H),
-                    w_down=(w_down, _BF16, s.E * s.F * s.H), codes=(codes, _I8, 2 * TK * s.F),
-                    exps=(exps, _U8, TK * s.F // 8), yp=(yp, _BF16, TK * s.H))
+        W = s.E * s.F * s.H
+        _need("expert_ffn_checkpoint", ("xp", xp, _BF16, TK * s.H), ("seg_offsets", seg_offsets, _I32, s.R * s.C_max + 1),
+              ("w_gate", w_gate, _BF16, W), ("w_up", w_up, _BF16, W), ("w_down", w_down, _BF16, W),
+              ("codes", codes, _I8, 2 * TK * s.F), ("exps", exps, _U8, TK * s.F // 8), ("yp", yp, _BF16, TK * s.H))
         if s.S > 0 and x is not None:
             SF = s.S * s.F
-            need.update(x=(x, _BF16, T * s.H), ws_gate=(ws_gate, _BF16, SF * s.H), ws_up=(ws_up, _BF16, SF * s.H),
-                        ws_down=(ws_down, _BF16, SF * s.H), codes_shared=(codes_shared, _I8, 2 * T * SF),
-                        exps_shared=(exps_shared, _U8, T * SF // 8), y_shared=(y_shared, _BF16, T * s.H))
-        _need("expert_ffn_checkpoint", **need)
+            _need("expert_ffn_checkpoint", ("x", x, _BF16, T * s.H), ("ws_gate", ws_gate, _BF16, SF * s.H),
+                  ("ws_up", ws_up, _BF16, SF * s.H), ("ws_down", ws_down, _BF16, SF * s.H),
+                  ("codes_shared", codes_shared, _I8, 2 * T * SF), ("exps_shared", exps_shared, _U8, T * SF // 8),
+                  ("y_shared", y_shared, _BF16, T * s.H))
         _check(self.lib.director_expert_ffn_checkpoint(
             self._ctx, T, _ptr(xp), _ptr(seg_offsets), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(codes), _ptr(exps), _ptr(yp),
             _ptr(x), _ptr(ws_gate), _ptr(ws_up), _ptr(ws_down), _ptr(codes_shared), _ptr(exps_shared), _ptr(y_shared),
@@ -288,17 +303,18 @@ class Director:
         """Gradients of expert_ffn_checkpoint from the gate and up values it kept (after reserve_training)."""
         s = self.shape
         TK, W = T * s.K, s.E * s.F * s.H
-        need = dict(xp=(xp, _BF16, TK * s.H), dyp=(dyp, _BF16, TK * s.H), seg_offsets=(seg_offsets, _I32, s.R * s.C_max + 1),
-                    codes=(codes, _I8, 2 * TK * s.F), exps=(exps, _U8, TK * s.F // 8), w_gate=(w_gate, _BF16, W),
-                    w_up=(w_up, _BF16, W), w_down=(w_down, _BF16, W), dxp=(dxp, _BF16, TK * s.H), dw_gate=(dw_gate, _BF16, W),
-                    dw_up=(dw_up, _BF16, W), dw_down=(dw_down, _BF16, W))
+        _need("expert_ffn_backward", ("xp", xp, _BF16, TK * s.H), ("dyp", dyp, _BF16, TK * s.H),
+              ("seg_offsets", seg_offsets, _I32, s.R * s.C_max + 1), ("codes", codes, _I8, 2 * TK * s.F),
+              ("exps", exps, _U8, TK * s.F // 8), ("w_gate", w_gate, _BF16, W), ("w_up", w_up, _BF16, W),
+              ("w_down", w_down, _BF16, W), ("dxp", dxp, _BF16, TK * s.H), ("dw_gate", dw_gate, _BF16, W),
+              ("dw_up", dw_up, _BF16, W), ("dw_down", dw_down, _BF16, W))
         if s.S > 0 and x is not None:
             SF = s.S * s.F
-            need.update(x=(x, _BF16, T * s.H), dy=(dy, _BF16, T * s.H), codes_shared=(codes_shared, _I8, 2 * T * SF),
-                        exps_shared=(exps_shared, _U8, T * SF // 8), ws_gate=(ws_gate, _BF16, SF * s.H),
-                        ws_up=(ws_up, _BF16, SF * s.H), ws_down=(ws_down, _BF16, SF * s.H), dx_shared=(dx_shared, _BF16, T * s.H),
-                        dws_gate=(dws_gate, _BF16, SF * s.H), dws_up=(dws_up, _BF16, SF * s.H), dws_down=(dws_down, _BF16, SF * s.H))
-        _need("expert_ffn_backward", **need)
+            _need("expert_ffn_backward", ("x", x, _BF16, T * s.H), ("dy", dy, _BF16, T * s.H),
+                  ("codes_shared", codes_shared, _I8, 2 * T * SF), ("exps_shared", exps_shared, _U8, T * SF // 8),
+                  ("ws_gate", ws_gate, _BF16, SF * s.H), ("ws_up", ws_up, _BF16, SF * s.H), ("ws_down", ws_down, _BF16, SF * s.H),
+                  ("dx_shared", dx_shared, _BF16, T * s.H), ("dws_gate", dws_gate, _BF16, SF * s.H),
+                  ("dws_up", dws_up, _BF16, SF * s.H), ("dws_down", dws_down, _BF16, SF * s.H))
         _check(self.lib.director_expert_ffn_backward(
             self._ctx, T, _ptr(xp), _ptr(dyp), _ptr(seg_offsets), _ptr(codes), _ptr(exps), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
             _ptr(dxp), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(x), _ptr(dy), _ptr(codes_shared), _ptr(exps_shared),
@@ -307,8 +323,8 @@ class Director:
 
     def checkpoint_decode(self, rows, F, codes, exps, gate, up):
         """The values that a checkpoint of `rows` rows of F features stands for, into gate and up (bf16 [rows,F])."""
-        _need("checkpoint_decode", codes=(codes, _I8, 2 * rows * F), exps=(exps, _U8, rows * F // 8), gate=(gate, _BF16, rows * F),
-              up=(up, _BF16, rows * F))
+        _need("checkpoint_decode", ("codes", codes, _I8, 2 * rows * F), ("exps", exps, _U8, rows * F // 8),
+              ("gate", gate, _BF16, rows * F), ("up", up, _BF16, rows * F))
         _check(self.lib.director_checkpoint_decode(self._ctx, rows, F, _ptr(codes), _ptr(exps), _ptr(gate), _ptr(up), _stream()),
                "director_checkpoint_decode")
 

@@ -132,7 +132,6 @@ template <int PHASE>
 __global__ void __launch_bounds__(G_THREADS, 1)
 grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
     extern __shared__ uint8_t smem_raw[];
-    chain_prologue();
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
     uint8_t* const out_buf = smem_raw + (ring - raw) + G_STAGES * G_STAGE_BYTES;      // [G_EPI_WARPS][G_OUT_BYTES]
@@ -155,20 +154,8 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     const int h_blocks = p.H / 256;
     auto problem_of = [&](int e) -> int { return e >= p.E ? 1 : 0; };
 
-    // ---- tables and barriers ----
-    for (int r = tid; r < p.n_rep; r += G_THREADS) {
-        int lo = 0, hi = p.prob[1].rows;
-        if (r < p.n_rep - (experts - p.E)) {
-            const int g = __ldg(p.rep_slot + r);
-            lo = min(max(__ldg(p.seg_offsets + g), 0), p.prob[0].rows);
-            hi = min(max(__ldg(p.seg_offsets + g + 1), lo), p.prob[0].rows);
-        }
-        s_lo[r] = lo;
-        s_hi[r] = hi;
-    }
-    for (int e = tid; e <= experts; e += G_THREADS) s_rep[e] = e <= p.E ? __ldg(p.rep_start + e) : p.n_rep;
+    // ---- barriers, tensor memory and tensor maps: nothing here depends on the kernels before, so it comes before the wait ----
     if (tid == 0) {
-        if (blockIdx.x == 0) *p.other_counter = 0u;     // its launch has ended (chain_prologue), or has not begun
         *abort_flag = 0;
         *prod_k = 0;
         for (int s = 0; s < G_STAGES; ++s) {
@@ -187,6 +174,28 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&hd.tmem)), "r"(TMEM_COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (warp == 2 && lane < (p.experts > p.E ? 2 : 1) * GRAD_MAPS)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.m[0][0] + lane)) : "memory");
+    chain_prologue();
+
+    // ---- tables ----
+    for (int r = tid; r < p.n_rep; r += G_THREADS) {
+        int lo = 0, hi = p.prob[1].rows;
+        if (r < p.n_rep - (experts - p.E)) {
+            const int g = __ldg(p.rep_slot + r);
+            lo = min(max(__ldg(p.seg_offsets + g), 0), p.prob[0].rows);
+            hi = min(max(__ldg(p.seg_offsets + g + 1), lo), p.prob[0].rows);
+        }
+        s_lo[r] = lo;
+        s_hi[r] = hi;
+    }
+    for (int e = tid; e <= experts; e += G_THREADS) s_rep[e] = e <= p.E ? __ldg(p.rep_start + e) : p.n_rep;
+    if (tid == 0 && blockIdx.x == 0) *p.other_counter = 0u;   // its launch has ended (chain_prologue), or has not begun
     __syncthreads();
     {
         int tiles = 0, steps = 0;                       // token tiles and 64-row steps of expert tid
@@ -222,11 +231,6 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
         for (int w = 0; w < warp; ++w) { items += hd.warp_sum[0][w]; w_items += hd.warp_sum[1][w]; }
         if (tid < experts) { s_pre[tid + 1] = items; s_wpre[tid + 1] = w_items; }
         if (tid == 0) { s_pre[0] = 0; s_wpre[0] = 0; }
-    }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&hd.tmem)), "r"(TMEM_COLS)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
