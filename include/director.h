@@ -229,7 +229,8 @@ int director_dispatch_backward(director_ctx* ctx, int32_t T, const void* dxp, co
 
 /* Gradient of director_route (the choice of experts is piecewise constant; the weights are the softmax of the chosen
  * logits):  dlogits[t,topk_idx[t,s]] = topk_w[t,s] * (dtopk_w[t,s] - sum_j topk_w[t,j] * dtopk_w[t,j]), all other
- * entries 0.  topk_idx: dev int32 [T,K].  topk_w, dtopk_w: dev fp32 [T,K].  dlogits: dev fp32 [T,E], written whole.
+ * entries 0.  topk_idx: dev int32 [T,K], the K experts of a token distinct, as director_route gives them.  topk_w, dtopk_w:
+ * dev fp32 [T,K].  dlogits: dev fp32 [T,E], written whole.
  * An index outside [0,E) is skipped and reported as DIRECTOR_ERR_BAD_INDEX. */
 int director_route_backward(director_ctx* ctx, int32_t T, const int32_t* topk_idx, const float* topk_w,
                             const float* dtopk_w, float* dlogits, void* stream);

@@ -131,8 +131,9 @@ def _bind_torch():
 
 
 def _need(where: str, *tensors):
-    """Checks the tensors of a training call, (name, tensor, dtype, elements) each.  The C entry points see bare addresses; a
-    tensor of another type, a strided view or one too short would be read as something else."""
+    """Checks the tensors of a training call, (name, tensor, dtype, elements) each, and returns their addresses.  The C entry
+    points see bare addresses; a tensor of another type, a strided view or one too short would be read as something else."""
+    addresses = []
     for name, t, dtype, numel in tensors:
         if t.dtype is not dtype:
             raise TypeError(f"{where}: {name} is {t.dtype}, {dtype} is needed")
@@ -140,6 +141,8 @@ def _need(where: str, *tensors):
             raise ValueError(f"{where}: {name} has to be a contiguous CUDA tensor")
         if t.numel() < numel:
             raise ValueError(f"{where}: {name} has {t.numel()} elements, {numel} are needed")
+        addresses.append(t.data_ptr())
+    return addresses
 
 
 def _stream():
@@ -250,27 +253,24 @@ class Director:
     def combine_backward(self, T, dy, yp, inv_row, topk_w, dyp, dtopk_w):
         """Gradient of combine: dyp = each row's weight times its token's dy, dtopk_w = the dot products of dy and yp."""
         TK, H = T * self.shape.K, self.shape.H
-        _need("combine_backward", ("dy", dy, _BF16, T * H), ("yp", yp, _BF16, TK * H), ("inv_row", inv_row, _I32, TK),
-              ("topk_w", topk_w, _F32, TK), ("dyp", dyp, _BF16, TK * H), ("dtopk_w", dtopk_w, _F32, TK))
-        _check(self.lib.director_combine_backward(self._ctx, T, _ptr(dy), _ptr(yp), _ptr(inv_row), _ptr(topk_w), _ptr(dyp),
-                                                  _ptr(dtopk_w), _stream()), "director_combine_backward")
+        args = _need("combine_backward", ("dy", dy, _BF16, T * H), ("yp", yp, _BF16, TK * H), ("inv_row", inv_row, _I32, TK),
+                     ("topk_w", topk_w, _F32, TK), ("dyp", dyp, _BF16, TK * H), ("dtopk_w", dtopk_w, _F32, TK))
+        _check(self.lib.director_combine_backward(self._ctx, T, *args, _stream()), "director_combine_backward")
 
     def dispatch_backward(self, T, dxp, inv_row, dx_shared, dx):
         """Gradient of dispatch's row copies: dx = the sum of a token's rows of dxp (+ dx_shared, which may be None)."""
         TK, H = T * self.shape.K, self.shape.H
-        _need("dispatch_backward", ("dxp", dxp, _BF16, TK * H), ("inv_row", inv_row, _I32, TK), ("dx", dx, _BF16, T * H))
+        dxp, inv_row, dx = _need("dispatch_backward", ("dxp", dxp, _BF16, TK * H), ("inv_row", inv_row, _I32, TK), ("dx", dx, _BF16, T * H))
         if dx_shared is not None:
-            _need("dispatch_backward", ("dx_shared", dx_shared, _BF16, T * H))
-        _check(self.lib.director_dispatch_backward(self._ctx, T, _ptr(dxp), _ptr(inv_row), _ptr(dx_shared), _ptr(dx),
-                                                   _stream()), "director_dispatch_backward")
+            dx_shared, = _need("dispatch_backward", ("dx_shared", dx_shared, _BF16, T * H))
+        _check(self.lib.director_dispatch_backward(self._ctx, T, dxp, inv_row, dx_shared, dx, _stream()), "director_dispatch_backward")
 
     def route_backward(self, T, topk_idx, topk_w, dtopk_w, dlogits):
         """Gradient of route: dlogits [T,E], zero where an expert was not chosen."""
         TK = T * self.shape.K
-        _need("route_backward", ("topk_idx", topk_idx, _I32, TK), ("topk_w", topk_w, _F32, TK), ("dtopk_w", dtopk_w, _F32, TK),
-              ("dlogits", dlogits, _F32, T * self.shape.E))
-        _check(self.lib.director_route_backward(self._ctx, T, _ptr(topk_idx), _ptr(topk_w), _ptr(dtopk_w), _ptr(dlogits),
-                                                _stream()), "director_route_backward")
+        args = _need("route_backward", ("topk_idx", topk_idx, _I32, TK), ("topk_w", topk_w, _F32, TK), ("dtopk_w", dtopk_w, _F32, TK),
+                     ("dlogits", dlogits, _F32, T * self.shape.E))
+        _check(self.lib.director_route_backward(self._ctx, T, *args, _stream()), "director_route_backward")
 
     def expert_ffn_checkpoint(self, T, xp, seg_offsets, w_gate, w_up, w_down, codes, exps, yp, x=None, ws_gate=None,
                               ws_up=None, ws_down=None, codes_shared=None, exps_shared=None, y_shared=None):
@@ -279,19 +279,17 @@ class Director:
         s = self.shape
         TK = T * s.K
         W = s.E * s.F * s.H
-        _need("expert_ffn_checkpoint", ("xp", xp, _BF16, TK * s.H), ("seg_offsets", seg_offsets, _I32, s.R * s.C_max + 1),
-              ("w_gate", w_gate, _BF16, W), ("w_up", w_up, _BF16, W), ("w_down", w_down, _BF16, W),
-              ("codes", codes, _I8, 2 * TK * s.F), ("exps", exps, _U8, TK * s.F // 8), ("yp", yp, _BF16, TK * s.H))
+        args = _need("expert_ffn_checkpoint", ("xp", xp, _BF16, TK * s.H), ("seg_offsets", seg_offsets, _I32, s.R * s.C_max + 1),
+                     ("w_gate", w_gate, _BF16, W), ("w_up", w_up, _BF16, W), ("w_down", w_down, _BF16, W),
+                     ("codes", codes, _I8, 2 * TK * s.F), ("exps", exps, _U8, TK * s.F // 8), ("yp", yp, _BF16, TK * s.H))
+        shared = [None] * 7
         if s.S > 0 and x is not None:
             SF = s.S * s.F
-            _need("expert_ffn_checkpoint", ("x", x, _BF16, T * s.H), ("ws_gate", ws_gate, _BF16, SF * s.H),
-                  ("ws_up", ws_up, _BF16, SF * s.H), ("ws_down", ws_down, _BF16, SF * s.H),
-                  ("codes_shared", codes_shared, _I8, 2 * T * SF), ("exps_shared", exps_shared, _U8, T * SF // 8),
-                  ("y_shared", y_shared, _BF16, T * s.H))
-        _check(self.lib.director_expert_ffn_checkpoint(
-            self._ctx, T, _ptr(xp), _ptr(seg_offsets), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(codes), _ptr(exps), _ptr(yp),
-            _ptr(x), _ptr(ws_gate), _ptr(ws_up), _ptr(ws_down), _ptr(codes_shared), _ptr(exps_shared), _ptr(y_shared),
-            _stream()), "director_expert_ffn_checkpoint")
+            shared = _need("expert_ffn_checkpoint", ("x", x, _BF16, T * s.H), ("ws_gate", ws_gate, _BF16, SF * s.H),
+                           ("ws_up", ws_up, _BF16, SF * s.H), ("ws_down", ws_down, _BF16, SF * s.H),
+                           ("codes_shared", codes_shared, _I8, 2 * T * SF), ("exps_shared", exps_shared, _U8, T * SF // 8),
+                           ("y_shared", y_shared, _BF16, T * s.H))
+        _check(self.lib.director_expert_ffn_checkpoint(self._ctx, T, *args, *shared, _stream()), "director_expert_ffn_checkpoint")
 
     def reserve_training(self):
         """Allocates the workspace of expert_ffn_backward (once; later calls do nothing)."""
@@ -303,30 +301,27 @@ class Director:
         """Gradients of expert_ffn_checkpoint from the gate and up values it kept (after reserve_training)."""
         s = self.shape
         TK, W = T * s.K, s.E * s.F * s.H
-        _need("expert_ffn_backward", ("xp", xp, _BF16, TK * s.H), ("dyp", dyp, _BF16, TK * s.H),
-              ("seg_offsets", seg_offsets, _I32, s.R * s.C_max + 1), ("codes", codes, _I8, 2 * TK * s.F),
-              ("exps", exps, _U8, TK * s.F // 8), ("w_gate", w_gate, _BF16, W), ("w_up", w_up, _BF16, W),
-              ("w_down", w_down, _BF16, W), ("dxp", dxp, _BF16, TK * s.H), ("dw_gate", dw_gate, _BF16, W),
-              ("dw_up", dw_up, _BF16, W), ("dw_down", dw_down, _BF16, W))
+        args = _need("expert_ffn_backward", ("xp", xp, _BF16, TK * s.H), ("dyp", dyp, _BF16, TK * s.H),
+                     ("seg_offsets", seg_offsets, _I32, s.R * s.C_max + 1), ("codes", codes, _I8, 2 * TK * s.F),
+                     ("exps", exps, _U8, TK * s.F // 8), ("w_gate", w_gate, _BF16, W), ("w_up", w_up, _BF16, W),
+                     ("w_down", w_down, _BF16, W), ("dxp", dxp, _BF16, TK * s.H), ("dw_gate", dw_gate, _BF16, W),
+                     ("dw_up", dw_up, _BF16, W), ("dw_down", dw_down, _BF16, W))
+        shared = [None] * 11
         if s.S > 0 and x is not None:
             SF = s.S * s.F
-            _need("expert_ffn_backward", ("x", x, _BF16, T * s.H), ("dy", dy, _BF16, T * s.H),
-                  ("codes_shared", codes_shared, _I8, 2 * T * SF), ("exps_shared", exps_shared, _U8, T * SF // 8),
-                  ("ws_gate", ws_gate, _BF16, SF * s.H), ("ws_up", ws_up, _BF16, SF * s.H), ("ws_down", ws_down, _BF16, SF * s.H),
-                  ("dx_shared", dx_shared, _BF16, T * s.H), ("dws_gate", dws_gate, _BF16, SF * s.H),
-                  ("dws_up", dws_up, _BF16, SF * s.H), ("dws_down", dws_down, _BF16, SF * s.H))
-        _check(self.lib.director_expert_ffn_backward(
-            self._ctx, T, _ptr(xp), _ptr(dyp), _ptr(seg_offsets), _ptr(codes), _ptr(exps), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
-            _ptr(dxp), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(x), _ptr(dy), _ptr(codes_shared), _ptr(exps_shared),
-            _ptr(ws_gate), _ptr(ws_up), _ptr(ws_down), _ptr(dx_shared), _ptr(dws_gate), _ptr(dws_up), _ptr(dws_down), _stream()),
-            "director_expert_ffn_backward")
+            shared = _need("expert_ffn_backward", ("x", x, _BF16, T * s.H), ("dy", dy, _BF16, T * s.H),
+                           ("codes_shared", codes_shared, _I8, 2 * T * SF), ("exps_shared", exps_shared, _U8, T * SF // 8),
+                           ("ws_gate", ws_gate, _BF16, SF * s.H), ("ws_up", ws_up, _BF16, SF * s.H),
+                           ("ws_down", ws_down, _BF16, SF * s.H), ("dx_shared", dx_shared, _BF16, T * s.H),
+                           ("dws_gate", dws_gate, _BF16, SF * s.H), ("dws_up", dws_up, _BF16, SF * s.H),
+                           ("dws_down", dws_down, _BF16, SF * s.H))
+        _check(self.lib.director_expert_ffn_backward(self._ctx, T, *args, *shared, _stream()), "director_expert_ffn_backward")
 
     def checkpoint_decode(self, rows, F, codes, exps, gate, up):
         """The values that a checkpoint of `rows` rows of F features stands for, into gate and up (bf16 [rows,F])."""
-        _need("checkpoint_decode", ("codes", codes, _I8, 2 * rows * F), ("exps", exps, _U8, rows * F // 8),
-              ("gate", gate, _BF16, rows * F), ("up", up, _BF16, rows * F))
-        _check(self.lib.director_checkpoint_decode(self._ctx, rows, F, _ptr(codes), _ptr(exps), _ptr(gate), _ptr(up), _stream()),
-               "director_checkpoint_decode")
+        args = _need("checkpoint_decode", ("codes", codes, _I8, 2 * rows * F), ("exps", exps, _U8, rows * F // 8),
+                     ("gate", gate, _BF16, rows * F), ("up", up, _BF16, rows * F))
+        _check(self.lib.director_checkpoint_decode(self._ctx, rows, F, *args, _stream()), "director_checkpoint_decode")
 
     def placement_cost(self, T, topk_idx, token_src_rank, workload, rank_load, dispatch_tokens, dispatch_bytes):
         _check(self.lib.director_placement_cost(self._ctx, T, _ptr(topk_idx), _ptr(token_src_rank), _ptr(workload),
