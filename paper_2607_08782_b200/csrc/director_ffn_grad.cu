@@ -637,9 +637,12 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     }
 
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");          // a lane's own stores, none for most
-    // ---- teardown, as in the forward kernel: a role that gave up tells the peer CTA ----
-    if (*abort_flag)
+    // ---- teardown, as in the forward kernel: a role that gave up tells the peer CTA; loads and products still under way then
+    // get a millisecond to land before the shared and tensor memory they write to is given back ----
+    if (*abort_flag) {
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cta(abort_addr, 1u - rank)), "r"(1) : "memory");
+        for (const unsigned long long t0 = global_ns(); global_ns() - t0 < 1000000ull;) __nanosleep(1000);
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();

@@ -106,6 +106,57 @@ class MoELayer:
                                   x if S > 0 else None, *(self.ws if S > 0 else (None, None, None)), self.y_acc,
                                   self.row_weight, self.y)
 
+    # -- training ----------------------------------------------------------------------------------
+    def enable_training(self):
+        """Allocates what a training step keeps between its two passes (the 8-bit gate and up values) and its gradients; a layer
+        that only serves never holds them.  Calling it again does nothing."""
+        if getattr(self, "grads", None) is not None:
+            return
+        d, dev = self.dims, self.y.device
+        T, A, H, F, SF = d["T_max"], d["T_max"] * d["K"], d["H"], d["F"], d["S"] * d["F"]
+        self.d.reserve_training()
+        self.kept = (torch.empty((A, F, 2), dtype=torch.int8, device=dev), torch.empty((F // 16, A, 2), dtype=torch.uint8, device=dev))
+        self.dyp, self.dxp = torch.empty_like(self.yp), torch.empty_like(self.xp)
+        self.dtopk_w = torch.empty_like(self.topk_w)
+        grads = dict(x=torch.empty((T, H), dtype=torch.bfloat16, device=dev),
+                     logits=torch.empty((T, d["E"]), dtype=torch.float32, device=dev),
+                     **{n: torch.empty_like(w) for n, w in zip(("w_gate", "w_up", "w_down"), self.w)})
+        if SF > 0:
+            self.kept_shared = (torch.empty((T, SF, 2), dtype=torch.int8, device=dev),
+                                torch.empty((SF // 16, T, 2), dtype=torch.uint8, device=dev))
+            self.dx_shared = torch.empty_like(grads["x"])
+            grads.update({n: torch.empty_like(w) for n, w in zip(("ws_gate", "ws_up", "ws_down"), self.ws)})
+        self.trained = None                    # (T, x) of the forward pass whose backward pass is due
+        self.grads = grads
+
+    def forward_train(self, T, logits, x):
+        """The layer's forward pass, keeping what backward() needs (xp, yp, the gate's weights, the 8-bit gate and up values) in the
+        layer's buffers; returns y[:T].  x has to stay as it is until backward()."""
+        self.enable_training()
+        self.route(T, logits)
+        self.dispatch(T, x)
+        shared = (x, *self.ws, *self.kept_shared, self.y_shared) if self.dims["S"] > 0 else ()
+        self.d.expert_ffn_checkpoint(T, self.xp, self.seg_offsets, *self.w, *self.kept, self.yp, *shared)
+        self.combine(T)
+        self.trained = (T, x)
+        return self.y[:T]
+
+    def backward(self, T, dy):
+        """Gradients of the forward_train() before, given dy = dL/dy [T,H] (bf16): a dict of x [T,H], logits [T,E], w_gate, w_up,
+        w_down and, with shared experts, ws_gate, ws_up, ws_down - views of the layer's buffers, overwritten by the next call."""
+        if getattr(self, "trained", None) is None or self.trained[0] != T:
+            raise RuntimeError("backward() without a forward_train() of the same batch")
+        (_, x), self.trained = self.trained, None
+        g = self.grads
+        self.d.combine_backward(T, dy, self.yp, self.inv_row, self.topk_w, self.dyp, self.dtopk_w)
+        with_shared = self.dims["S"] > 0
+        shared = (x, dy, *self.kept_shared, *self.ws, self.dx_shared, g["ws_gate"], g["ws_up"], g["ws_down"]) if with_shared else ()
+        self.d.expert_ffn_backward(T, self.xp, self.dyp, self.seg_offsets, *self.kept, *self.w, self.dxp, g["w_gate"], g["w_up"],
+                                   g["w_down"], *shared)
+        self.d.dispatch_backward(T, self.dxp, self.inv_row, self.dx_shared if with_shared else None, g["x"])
+        self.d.route_backward(T, self.topk_idx, self.topk_w, self.dtopk_w, g["logits"])
+        return {n: t[:T] if n in ("x", "logits") else t for n, t in g.items()}
+
     def placement_cost(self, T, token_src_rank=None):
         self.d.placement_cost(T, self.topk_idx, token_src_rank, self.workload, self.rank_load,
                               self.dispatch_tokens, self.dispatch_bytes)
