@@ -45,9 +45,12 @@ enum GradKind { GRAD_ACT = 0, GRAD_DX = 1, GRAD_GATEUP = 2, GRAD_DOWN = 3 };
 constexpr int G_STAGES = 6;
 constexpr int G_BOX_BYTES = 64 * 128;                  // 64 rows of 64 bf16 columns
 constexpr int G_STAGE_BYTES = 4 * G_BOX_BYTES;         // 16 KB of each operand
-constexpr int G_EPI_WARPS = 8;                         // two per TMEM lane quadrant
-constexpr int G_THREADS = 128 + 32 * G_EPI_WARPS;      // producer, MMA, scheduler and tail warps + epilogue
-constexpr int G_TILE = 256;                            // tokens per full tile; accumulators are this many columns apart
+// Epilogue warps, a multiple of the four TMEM lane quadrants; each takes every second or third chunk of 32 columns.  GRAD_ACT's epilogue (a
+// sigmoid, two kept values in and three outputs an element) bounds contractions shorter than about 2048: at H = 1536, F = 640,
+// 120 432 rows, the launch took 320 us with 8 warps, 291 with 12 and 293 with 16, at H = 4096 780, 754 and 766 us.
+constexpr int grad_epi_warps(int phase) { return phase == 0 ? 12 : 8; }
+constexpr int grad_threads(int phase) { return 128 + 32 * grad_epi_warps(phase); }   // producer, MMA, scheduler and tail warps + epilogue
+constexpr int G_TILE = 256;                            // most tokens per tile; accumulators are this many columns apart
 constexpr int G_SLOTS = 4;                             // ring of work items
 constexpr int G_CLAIM_LEAD = 32;                       // k-steps of claimed work ahead of the producer
 
@@ -61,14 +64,16 @@ struct GradHeader {
     uint32_t tmem;
     int abort;
     int prod_k;                                        // k-steps issued by the scheduler CTA's producer
-    int warp_sum[2][G_THREADS / 32];
+    int warp_sum[2][20];
+    int tile;                                          // tokens per full tile of this launch
 };
 // experts: all of them, the shared one among them; n_rep: their segments
-constexpr int grad_smem_bytes(int n_rep, int experts) {
-    return 1024 + G_STAGES * G_STAGE_BYTES + G_EPI_WARPS * G_OUT_BYTES + (int)sizeof(GradHeader) + 8 * n_rep + 4 * (5 * experts + 3);
+constexpr int grad_out_bytes(int phase) { return phase == 1 ? grad_epi_warps(1) * G_OUT_BYTES : 0; }
+constexpr int grad_smem_bytes(int phase, int n_rep, int experts) {
+    return 1024 + G_STAGES * G_STAGE_BYTES + grad_out_bytes(phase) + (int)sizeof(GradHeader) + 8 * n_rep + 4 * (5 * experts + 3);
 }
-static_assert(grad_smem_bytes(kMaxG + 1, kMaxE + 1) <= 232448, "the ring does not fit with the largest tables");
-static_assert(kMaxE + 1 <= G_THREADS, "one thread per expert builds the tables");
+static_assert(grad_smem_bytes(1, kMaxG + 1, kMaxE + 1) <= 232448, "the ring does not fit with the largest tables");
+static_assert(kMaxE + 1 <= grad_threads(1), "one thread per expert builds the tables");
 
 constexpr uint32_t G_IDESC_BASE = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) /* left operand MN-major */ |
                                   ((uint32_t)(256 >> 4) << 24);
@@ -91,9 +96,9 @@ struct GradProblem {
     uint16_t *dg, *du, *act;       // written by GRAD_ACT, [rows, F]
     uint16_t* dx;                  // [rows, H]
 };
-// What a launch loads from and, for the weight gradients, stores to.  _K: boxes of 128 rows, contraction along the row; all
-// others: boxes of 64 contraction rows; OUT_*: boxes of 32 rows x 32 columns.
-enum GradMap { MAP_WD, MAP_DY_K, MAP_WG, MAP_WU, MAP_DG_K, MAP_DU_K, MAP_X, MAP_DG, MAP_DU, MAP_DY, MAP_ACT, MAP_OUT_G, MAP_OUT_U,
+// What a launch loads from and, for the weight gradients, stores to.  _K: boxes of 32 rows, contraction along the row (as many
+// as a tile's tokens need); all others: boxes of 64 contraction rows; OUT_*: boxes of 32 rows x 32 columns.
+enum GradMap { MAP_WD, MAP_WG, MAP_WU, MAP_DY_K, MAP_DG_K, MAP_DU_K, MAP_X, MAP_DG, MAP_DU, MAP_DY, MAP_ACT, MAP_OUT_G, MAP_OUT_U,
                MAP_OUT_D, GRAD_MAPS };
 struct GradMaps {
     CUtensorMap m[2][GRAD_MAPS];
@@ -121,6 +126,23 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y) : "memory");
 }
 
+// 1 / (1 + exp(-g)) from the two approximate units alone.  exp(-g) below 2^-126 counts as zero, above 2^127 as infinity, and so does the
+// result: all it costs are sigmoids below 2^-126.
+__device__ __forceinline__ float sigmoid(float g) {
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+    return s;
+}
+__device__ __forceinline__ uint64_t offset_by(const void* base, uint32_t bytes) {
+    uint64_t r;
+    asm("mad.wide.u32 %0, %1, 1, %2;" : "=l"(r) : "r"(bytes), "l"(reinterpret_cast<uint64_t>(base)));
+    return r;
+}
+__device__ __forceinline__ void store_u32(uint64_t addr, uint32_t v) {
+    *reinterpret_cast<uint32_t*>(addr) = v;
+}
+
 // 16 bytes into the shared memory of a CTA of the cluster, counted on an mbarrier there when they have arrived
 __device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, int4 v, uint32_t cluster_bar) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
@@ -129,13 +151,14 @@ __device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, int4 v, uint3
 
 // PHASE 0: GRAD_ACT.  PHASE 1: GRAD_DX, GRAD_GATEUP, GRAD_DOWN.
 template <int PHASE>
-__global__ void __launch_bounds__(G_THREADS, 1)
+__global__ void __launch_bounds__(grad_threads(PHASE), 1)
 grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
+    constexpr int G_THREADS = grad_threads(PHASE), G_EPI_WARPS = grad_epi_warps(PHASE);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
-    uint8_t* const out_buf = smem_raw + (ring - raw) + G_STAGES * G_STAGE_BYTES;      // [G_EPI_WARPS][G_OUT_BYTES]
-    GradHeader& hd = *reinterpret_cast<GradHeader*>(out_buf + G_EPI_WARPS * G_OUT_BYTES);
+    uint8_t* const out_buf = smem_raw + (ring - raw) + G_STAGES * G_STAGE_BYTES;      // phase 1: [G_EPI_WARPS][G_OUT_BYTES]
+    GradHeader& hd = *reinterpret_cast<GradHeader*>(out_buf + grad_out_bytes(PHASE));
     const int experts = p.experts;
     int32_t* const s_rep = reinterpret_cast<int32_t*>(&hd + 1);        // [experts+1] first segment of every expert
     int32_t* const s_pre = s_rep + (experts + 1);                      // [experts+1] token work items before expert e
@@ -179,8 +202,9 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
-    if (warp == 2 && lane < (p.experts > p.E ? 2 : 1) * GRAD_MAPS)
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.m[0][0] + lane)) : "memory");
+    if (warp == 2)
+        for (int i = lane; i < (p.experts > p.E ? 2 : 1) * GRAD_MAPS; i += 32)
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.m[0][0] + i)) : "memory");
     chain_prologue();
 
     // ---- tables ----
@@ -198,28 +222,45 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     if (tid == 0 && blockIdx.x == 0) *p.other_counter = 0u;   // its launch has ended (chain_prologue), or has not begun
     __syncthreads();
     {
-        int tiles = 0, steps = 0;                       // token tiles and 64-row steps of expert tid
+        int steps = 0;                                  // 64-row steps of expert tid
         if (tid < experts) {
-            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r) {
-                tiles += (s_hi[r] - s_lo[r] + G_TILE - 1) / G_TILE;
-                steps += (s_hi[r] - s_lo[r] + 63) / 64;
-            }
+            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r) steps += (s_hi[r] - s_lo[r] + 63) / 64;
             s_steps[tid] = steps;
         }
+        // Token tiles are 256 rows; where that leaves fewer items than CTA pairs, 128 or 64: the same products on more SMs, each tile
+        // with its own pass over the weights, which then come from L2 (1579 rows of three experts: 7 items of 256 rows on 74
+        // pairs, 26 of 64).  Every CTA comes to the same tile.
+        int tiles[3] = {0, 0, 0};                       // of 256, 128 and 64 rows
+        int blocks = 0;
+        if (tid < experts) {
+            blocks = PHASE == 0 ? (p.prob[problem_of(tid)].F + 255) / 256 : h_blocks;
+            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r)
+#pragma unroll
+                for (int k = 0; k < 3; ++k) tiles[k] += (s_hi[r] - s_lo[r] + (G_TILE >> k) - 1) / (G_TILE >> k);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int in_warp = __reduce_add_sync(0xFFFFFFFFu, tiles[k] * blocks);
+            if (lane == 0) hd.warp_sum[k][warp] = in_warp;
+        }
         __syncthreads();
+        int total[2] = {0, 0};
+        for (int w = 0; w < G_THREADS / 32; ++w) { total[0] += hd.warp_sum[0][w]; total[1] += hd.warp_sum[1][w]; }
+        __syncthreads();
+        const int pairs = (int)(gridDim.x >> 1), shift = total[0] >= pairs ? 0 : total[1] >= pairs ? 1 : 2;
+        const int tile = G_TILE >> shift;
+        int items = (shift == 0 ? tiles[0] : shift == 1 ? tiles[1] : tiles[2]) * blocks;
+        if (tid == 0) hd.tile = tile;
         if (PHASE == 1 && tid < experts) {
             int before = 0;
             for (int e = 0; e < experts; ++e) before += s_steps[e] > steps || (s_steps[e] == steps && e < tid) ? 1 : 0;
             s_order[before] = tid;
         }
         __syncthreads();
-        int items = 0, w_items = 0;
-        if (tid < experts) {
-            items = tiles * (PHASE == 0 ? (p.prob[problem_of(tid)].F + 255) / 256 : h_blocks);
-            if (PHASE == 1) {
-                const int F = p.prob[problem_of(s_order[tid])].F;
-                w_items = h_blocks * (F / 128 + (F + 255) / 256);
-            }
+        int w_items = 0;
+        if (PHASE == 1 && tid < experts) {
+            const int F = p.prob[problem_of(s_order[tid])].F;
+            w_items = h_blocks * (F / 128 + (F + 255) / 256);
         }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -318,7 +359,9 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                 }
             } else {
                 const int m_col = it.b * 256 + (int)rank * 128;
-                const int x_row = it.a + (int)rank * (columns_of(it) >> 1);
+                const int half = columns_of(it) >> 1, x_row = it.a + (int)rank * half;      // tokens this CTA supplies
+                const int boxes = (half + 31) >> 5;                       // of 32 tokens
+                const uint32_t tx = 2 * G_BOX_BYTES + boxes * (G_BOX_BYTES / 2);
                 const int k_steps = token_steps(it.e), e = pr ? 0 : it.e;
                 for (int kb = 0; kb < k_steps; ++kb) {
                     const bool second = PHASE == 1 && kb >= k_steps / 2;
@@ -331,10 +374,12 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     bad = mbar_wait_conv(smem_u32(&hd.empty[stage]), phase ^ 1u, abort_addr, bad, lead_lane);
                     ++issued_k;
                     if (lead_lane && !bad) {
-                        mbar_expect_tx_cluster(bar, G_STAGE_BYTES);
+                        mbar_expect_tx_cluster(bar, tx);
                         tma_load_2d_pair(dst, ma, bar, m_col, w_row);
                         tma_load_2d_pair(dst + G_BOX_BYTES, ma, bar, m_col + 64, w_row);
-                        tma_load_2d_pair(dst + 2 * G_BOX_BYTES, mb, bar, k, x_row);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (x < boxes) tma_load_2d_pair(dst + 2 * G_BOX_BYTES + x * (G_BOX_BYTES / 2), mb, bar, k, x_row + 32 * x);
                         if (leader) *prod_k = issued_k;
                     }
                     if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
@@ -398,7 +443,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     } else if (warp == 2) {
         // ---- scheduler, leader CTA (see the forward kernel for why claims are held back to G_CLAIM_LEAD k-steps) ----
         if (lane == 0 && leader) {
-            const int token_items = s_pre[experts];
+            const int token_items = s_pre[experts], tile = hd.tile;
             const int total = token_items + (PHASE == 1 ? s_wpre[experts] : 0);
             int e = 0, ord = 0, pub_k = 0;
             for (int i = 0;; ++i) {
@@ -423,14 +468,14 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                         const int blocks = PHASE == 0 ? (p.prob[problem_of(e)].F + 255) / 256 : h_blocks;
                         const int nt = (s_pre[e + 1] - s_pre[e]) / blocks, local = w - s_pre[e];
                         const int wb = local / nt;                     // block by block, so that an expert's token tiles share it
-                        int tile = local - wb * nt, r = s_rep[e];
+                        int nth = local - wb * nt, r = s_rep[e];       // the expert's nth tile: in which segment?
                         for (;; ++r) {
-                            const int n = (s_hi[r] - s_lo[r] + G_TILE - 1) / G_TILE;
-                            if (tile < n) break;
-                            tile -= n;
+                            const int n = (s_hi[r] - s_lo[r] + tile - 1) / tile;
+                            if (nth < n) break;
+                            nth -= n;
                         }
-                        const int row0 = s_lo[r] + tile * G_TILE;
-                        item = make_int4(row0, min(G_TILE, s_hi[r] - row0), e, wb | ((PHASE == 0 ? GRAD_ACT : GRAD_DX) << 28));
+                        const int row0 = s_lo[r] + nth * tile;
+                        item = make_int4(row0, min(tile, s_hi[r] - row0), e, wb | ((PHASE == 0 ? GRAD_ACT : GRAD_DX) << 28));
                         pub_k += token_steps(e);
                     } else if (PHASE == 1) {
                         const int v = w - token_items;
@@ -491,7 +536,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
             }
         }
     } else {
-        // ---- epilogue, both CTAs: 32 rows of D per warp (its TMEM quadrant), every other 32 columns ----
+        // ---- epilogue, both CTAs: 32 rows of D per warp (its TMEM quadrant), chunks of 32 columns ----
         const int quad = warp & 3;
         const int c_first = 32 * ((warp - 4) >> 2);
         constexpr int CSTEP = 32 * (G_EPI_WARPS / 4);
@@ -508,7 +553,8 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
             const bool odd = (lane & 1) != 0;
             const int d_pair = d_row & ~1;                             // first of the lane pair's two features
             // GRAD_ACT: the kept values of 32 tokens from c on (code[m]: both features at token c + 2m + odd; ex of lane j: the
-            // exponents of token c + j for the warp's two blocks).  The first chunk's are fetched while the products still run.
+            // exponents of token c + j for the warp's two blocks).  The first chunk's are asked for while the products still run, the
+            // others a chunk ahead - all before the chunk's arithmetic, among which a load would be waited for at the next use of any other.
             const bool live = it.b * 256 + d_row < pr.F;               // the last block may be half a block (warp-uniform)
             const size_t at0 = (size_t)(it.a + (odd ? 1 : 0)) * pr.F + it.b * 256 + d_pair;
             auto fetch = [&](int c, uint32_t (&code)[16], uint32_t& ex) {
@@ -531,39 +577,39 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
             const int n = columns_of(it);
             if constexpr (PHASE == 0) {
                 if (live) {
-                    uint16_t *dg = pr.dg + at0, *du = pr.du + at0, *act = pr.act + at0;
+                    const uint16_t *dg = pr.dg + at0, *du = pr.du + at0, *act = pr.act + at0;
 #pragma unroll 1
                     for (int c = c_first; c < n; c += CSTEP) {
-                        // The next chunk's values are all asked for before this chunk's arithmetic: a load among the arithmetic
-                        // would make the warp wait for it at the next use of any other load.
                         uint32_t next[16], next_ex = 0, v[32];
                         fetch(c + CSTEP, next, next_ex);
                         tmem_ld32(taddr + c, v);
                         const int rem = it.valid - c - (odd ? 1 : 0);
+                        uint32_t at = 2u * (uint32_t)c * (uint32_t)pr.F;              // bytes from the tile's first row: below 2^32
                         tmem_ld_wait();
 #pragma unroll
                         for (int m = 0; m < 16; ++m) {
                             const float other = __uint_as_float(__shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * m] : v[2 * m + 1], 1));
                             const float mine = __uint_as_float(odd ? v[2 * m + 1] : v[2 * m]);
                             const uint32_t pair = __shfl_sync(0xFFFFFFFFu, ex, 2 * m + (odd ? 1 : 0)) >> (lane & 16);
-                            const size_t at = (size_t)(c + 2 * m) * pr.F;
-                            const float sg = checkpoint_scale(pair & 255u), su = checkpoint_scale((pair >> 8) & 255u);
+                            // 2^(e - 127); e = 255 makes it infinity, and a code of zero times that NaN
+                            const float sg = __uint_as_float((pair << 23) & 0x7F800000u), su = __uint_as_float((pair << 15) & 0x7F800000u);
                             const uint32_t biased = code[m] ^ 0x80808080u;
                             float dg2[2], du2[2], act2[2];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
                                 const float da = (k == 0) == odd ? other : mine;
                                 const float g = checkpoint_value(biased, 2 * k, sg), u = checkpoint_value(biased, 2 * k + 1, su);
-                                const float s = __fdividef(1.0f, 1.0f + __expf(-g)), gs = g * s;
-                                dg2[k] = da * u * (s * (1.0f + g * (1.0f - s)));
+                                const float s = sigmoid(g), gs = g * s;
+                                dg2[k] = da * u * fmaf(gs, 1.0f - s, s);
                                 du2[k] = da * gs;
                                 act2[k] = gs * u;
                             }
                             if (2 * m < rem) {
-                                *reinterpret_cast<uint32_t*>(dg + at) = pack_bf16(dg2[0], dg2[1]);
-                                *reinterpret_cast<uint32_t*>(du + at) = pack_bf16(du2[0], du2[1]);
-                                *reinterpret_cast<uint32_t*>(act + at) = pack_bf16(act2[0], act2[1]);
+                                store_u32(offset_by(dg, at), pack_bf16(dg2[0], dg2[1]));
+                                store_u32(offset_by(du, at), pack_bf16(du2[0], du2[1]));
+                                store_u32(offset_by(act, at), pack_bf16(act2[0], act2[1]));
                             }
+                            at += 4u * (uint32_t)pr.F;
                             code[m] = next[m];
                         }
                         ex = next_ex;
@@ -657,8 +703,8 @@ template <int PHASE>
 int launch_grad(director_ctx* ctx, const char* name, const GradMaps& maps, const GradParams& p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * ctx->pair_clusters));
-    cfg.blockDim = dim3(G_THREADS);
-    cfg.dynamicSmemBytes = (size_t)grad_smem_bytes(p.n_rep, p.experts);
+    cfg.blockDim = dim3(grad_threads(PHASE));
+    cfg.dynamicSmemBytes = (size_t)grad_smem_bytes(PHASE, p.n_rep, p.experts);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -690,9 +736,9 @@ bool describe(director_ctx* ctx, const FfnGrad& f, uint64_t n_experts, int F, vo
     uint16_t* const dg = static_cast<uint16_t*>(dgu);
     uint16_t* const du = dg + rows * (uint64_t)F;
     pr = GradProblem{F, (int)rows, f.kept.codes, f.kept.exps, dg, du, static_cast<uint16_t*>(act), static_cast<uint16_t*>(f.dx)};
-    return map_2d(ctx, m + MAP_WD, f.w_down, n_experts * H, F, 64) && map_2d(ctx, m + MAP_DY_K, f.dy, rows, H) &&
+    return map_2d(ctx, m + MAP_WD, f.w_down, n_experts * H, F, 64) && map_2d(ctx, m + MAP_DY_K, f.dy, rows, H, 32) &&
            map_2d(ctx, m + MAP_WG, f.w_gate, n_experts * F, H, 64) && map_2d(ctx, m + MAP_WU, f.w_up, n_experts * F, H, 64) &&
-           map_2d(ctx, m + MAP_DG_K, dg, rows, F) && map_2d(ctx, m + MAP_DU_K, du, rows, F) &&
+           map_2d(ctx, m + MAP_DG_K, dg, rows, F, 32) && map_2d(ctx, m + MAP_DU_K, du, rows, F, 32) &&
            map_2d(ctx, m + MAP_X, f.x, rows, H, 64) && map_2d(ctx, m + MAP_DG, dg, rows, F, 64) &&
            map_2d(ctx, m + MAP_DU, du, rows, F, 64) && map_2d(ctx, m + MAP_DY, f.dy, rows, H, 64) &&
            map_2d(ctx, m + MAP_ACT, act, rows, F, 64) && map_out(ctx, m + MAP_OUT_G, f.dw_gate, n_experts * F, H) &&
@@ -702,7 +748,7 @@ bool describe(director_ctx* ctx, const FfnGrad& f, uint64_t n_experts, int F, vo
 template <int PHASE>
 bool grad_opt_in() {
     return cudaFuncSetAttribute(grouped_grad_kernel<PHASE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                grad_smem_bytes(kMaxG + 1, kMaxE + 1)) == cudaSuccess;
+                                grad_smem_bytes(PHASE, kMaxG + 1, kMaxE + 1)) == cudaSuccess;
 }
 
 }  // namespace
