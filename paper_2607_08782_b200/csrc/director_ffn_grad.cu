@@ -43,8 +43,13 @@ namespace {
 enum GradKind { GRAD_ACT = 0, GRAD_DX = 1, GRAD_GATEUP = 2, GRAD_DOWN = 3 };
 
 constexpr int G_STAGES = 6;
+// GRAD_ACT with tiles of at most 64 tokens needs 20 KB a stage (one box of tokens): nine fit into the same ring.  Such a launch
+// streams weights, and a stage comes back about 2500 cycles after it was asked for: what counts is how many are under way.
+constexpr int G_FEW_STAGES = 9;
 constexpr int G_BOX_BYTES = 64 * 128;                  // 64 rows of 64 bf16 columns
 constexpr int G_STAGE_BYTES = 4 * G_BOX_BYTES;         // 16 KB of each operand
+constexpr int G_FEW_STAGE_BYTES = 2 * G_BOX_BYTES + G_BOX_BYTES / 2;
+static_assert(G_FEW_STAGES * G_FEW_STAGE_BYTES <= G_STAGES * G_STAGE_BYTES, "the deeper ring fits into the ordinary one");
 // Epilogue warps, a multiple of the four TMEM lane quadrants; each takes every second or third chunk of 32 columns.  GRAD_ACT's epilogue (a
 // sigmoid, two kept values in and three outputs an element) bounds contractions shorter than about 2048: at H = 1536, F = 640,
 // 120 432 rows, the launch took 320 us with 8 warps, 291 with 12 and 293 with 16, at H = 4096 780, 754 and 766 us.
@@ -57,7 +62,7 @@ constexpr int G_CLAIM_LEAD = 32;                       // k-steps of claimed wor
 constexpr int G_OUT_BYTES = 32 * 64;                   // per epilogue warp: 32 rows x 32 bf16 columns of a weight gradient
 
 struct GradHeader {
-    uint64_t full[G_STAGES], empty[G_STAGES];
+    uint64_t full[G_FEW_STAGES], empty[G_FEW_STAGES];
     uint64_t part[G_STAGES];                           // this CTA's loads of a step that still has rows to be zeroed
     uint64_t tfull[2], tempty[2], sched_full[G_SLOTS], sched_empty[G_SLOTS];
     int4 item[G_SLOTS];
@@ -134,6 +139,12 @@ __device__ __forceinline__ float sigmoid(float g) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
     return s;
 }
+// a load that does not go through L1
+__device__ __forceinline__ int ld_relaxed(const int32_t* p) {
+    int v;
+    asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint64_t offset_by(const void* base, uint32_t bytes) {
     uint64_t r;
     asm("mad.wide.u32 %0, %1, 1, %2;" : "=l"(r) : "r"(bytes), "l"(reinterpret_cast<uint64_t>(base)));
@@ -177,15 +188,18 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     const int h_blocks = p.H / 256;
     auto problem_of = [&](int e) -> int { return e >= p.E ? 1 : 0; };
 
-    // ---- barriers, tensor memory and tensor maps: nothing here depends on the kernels before, so it comes before the wait ----
+    // ---- set-up.  Under programmatic dependent launch this runs while the kernel before is still ending.  Phase 0 waits for that
+    // kernel before it reads the segment table, and lets phase 1 start only after its wait: when a CTA of phase 1 runs, all that came
+    // before phase 0 - the segment table's writer among it - has ended, so phase 1 builds its tables ahead of its own wait (2.5 us
+    // of a small batch's time).  Without the launch attribute the instructions do nothing. ----
     if (tid == 0) {
         *abort_flag = 0;
         *prod_k = 0;
-        for (int s = 0; s < G_STAGES; ++s) {
+        for (int s = 0; s < G_FEW_STAGES; ++s) {
             mbar_init(smem_u32(&hd.full[s]), 2);
             mbar_init(smem_u32(&hd.empty[s]), 1);
-            mbar_init(smem_u32(&hd.part[s]), 1);
         }
+        for (int s = 0; s < G_STAGES; ++s) mbar_init(smem_u32(&hd.part[s]), 1);
         for (int a = 0; a < 2; ++a) {
             mbar_init(smem_u32(&hd.tfull[a]), 1);
             mbar_init(smem_u32(&hd.tempty[a]), 2 * G_EPI_WARPS);
@@ -205,26 +219,32 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     if (warp == 2)
         for (int i = lane; i < (p.experts > p.E ? 2 : 1) * GRAD_MAPS; i += 32)
             asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.m[0][0] + i)) : "memory");
-    chain_prologue();
+    if constexpr (PHASE == 0) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
 
     // ---- tables ----
     for (int r = tid; r < p.n_rep; r += G_THREADS) {
         int lo = 0, hi = p.prob[1].rows;
         if (r < p.n_rep - (experts - p.E)) {
-            const int g = __ldg(p.rep_slot + r);
-            lo = min(max(__ldg(p.seg_offsets + g), 0), p.prob[0].rows);
-            hi = min(max(__ldg(p.seg_offsets + g + 1), lo), p.prob[0].rows);
+            const int g = ld_relaxed(p.rep_slot + r);
+            lo = min(max(ld_relaxed(p.seg_offsets + g), 0), p.prob[0].rows);
+            hi = min(max(ld_relaxed(p.seg_offsets + g + 1), lo), p.prob[0].rows);
         }
         s_lo[r] = lo;
         s_hi[r] = hi;
     }
-    for (int e = tid; e <= experts; e += G_THREADS) s_rep[e] = e <= p.E ? __ldg(p.rep_start + e) : p.n_rep;
-    if (tid == 0 && blockIdx.x == 0) *p.other_counter = 0u;   // its launch has ended (chain_prologue), or has not begun
+    for (int e = tid; e <= experts; e += G_THREADS) s_rep[e] = e <= p.E ? ld_relaxed(p.rep_start + e) : p.n_rep;
     __syncthreads();
     {
         int steps = 0;                                  // 64-row steps of expert tid
+        bool long_one = false;                          // a segment of more than 64 rows
         if (tid < experts) {
-            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r) steps += (s_hi[r] - s_lo[r] + 63) / 64;
+            for (int r = s_rep[tid]; r < s_rep[tid + 1]; ++r) {
+                steps += (s_hi[r] - s_lo[r] + 63) / 64;
+                long_one |= s_hi[r] - s_lo[r] > 64;
+            }
             s_steps[tid] = steps;
         }
         // Token tiles are 256 rows; where that leaves fewer items than CTA pairs, 128 or 64: the same products on more SMs, each tile
@@ -243,11 +263,11 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
             const int in_warp = __reduce_add_sync(0xFFFFFFFFu, tiles[k] * blocks);
             if (lane == 0) hd.warp_sum[k][warp] = in_warp;
         }
-        __syncthreads();
+        const bool any_long = __syncthreads_or(long_one ? 1 : 0) != 0;
         int total[2] = {0, 0};
         for (int w = 0; w < G_THREADS / 32; ++w) { total[0] += hd.warp_sum[0][w]; total[1] += hd.warp_sum[1][w]; }
         __syncthreads();
-        const int pairs = (int)(gridDim.x >> 1), shift = total[0] >= pairs ? 0 : total[1] >= pairs ? 1 : 2;
+        const int pairs = (int)(gridDim.x >> 1), shift = !any_long ? 2 : total[0] >= pairs ? 0 : total[1] >= pairs ? 1 : 2;
         const int tile = G_TILE >> shift;
         int items = (shift == 0 ? tiles[0] : shift == 1 ? tiles[1] : tiles[2]) * blocks;
         if (tid == 0) hd.tile = tile;
@@ -277,7 +297,14 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     __syncthreads();
     cluster_sync_all();
     tc_fence_after();
+    if constexpr (PHASE == 1) {
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+    }
+    if (tid == 0 && blockIdx.x == 0) *p.other_counter = 0u;   // its launch has ended (waited for above), or has not begun
     const uint32_t tmem_base = hd.tmem;
+    const bool few = PHASE == 0 && hd.tile <= 64;
+    const int n_stages = few ? G_FEW_STAGES : G_STAGES, stage_bytes = few ? G_FEW_STAGE_BYTES : G_STAGE_BYTES;
 
     // ---- work items: claimed by one thread of the leader CTA, read by every role of both ----
     auto take_item = [&](int i, GradItem& it) -> bool {
@@ -342,7 +369,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     for (int k0 = s_lo[r]; k0 < hi; k0 += 64) {
                         // a step whose last MMA reaches past the segment is reported to this CTA's tail warp first
                         const bool tail = hi - k0 < 64 && ((hi - k0) & 15) != 0;
-                        const uint32_t dst = ring + stage * G_STAGE_BYTES;
+                        const uint32_t dst = ring + stage * stage_bytes;
                         const uint32_t bar = tail ? map_to_cta(smem_u32(&hd.part[stage]), rank) : map_to_cta(smem_u32(&hd.full[stage]), 0);
                         bad = mbar_wait_conv(smem_u32(&hd.empty[stage]), phase ^ 1u, abort_addr, bad, lead_lane);
                         ++issued_k;
@@ -354,7 +381,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                             if (half > 64) tma_load_2d_pair(dst + 3 * G_BOX_BYTES, mb, bar, n_col + 64, k0);
                             if (leader) *prod_k = issued_k;
                         }
-                        if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
                     }
                 }
             } else {
@@ -369,7 +396,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     const int w_row = e * (PHASE == 0 ? p.H : p.prob[pr].F) + k;
                     const CUtensorMap* ma = map + (PHASE == 0 ? MAP_WD : second ? MAP_WU : MAP_WG);
                     const CUtensorMap* mb = map + (PHASE == 0 ? MAP_DY_K : second ? MAP_DU_K : MAP_DG_K);
-                    const uint32_t dst = ring + stage * G_STAGE_BYTES;
+                    const uint32_t dst = ring + stage * stage_bytes;
                     const uint32_t bar = map_to_cta(smem_u32(&hd.full[stage]), 0);
                     bad = mbar_wait_conv(smem_u32(&hd.empty[stage]), phase ^ 1u, abort_addr, bad, lead_lane);
                     ++issued_k;
@@ -382,7 +409,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                             if (x < boxes) tma_load_2d_pair(dst + 2 * G_BOX_BYTES + x * (G_BOX_BYTES / 2), mb, bar, k, x_row + 32 * x);
                         if (leader) *prod_k = issued_k;
                     }
-                    if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                    if (++stage == n_stages) { stage = 0; phase ^= 1u; }
                 }
             }
             if (__any_sync(0xFFFFFFFFu, bad != 0u)) break;
@@ -405,7 +432,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                         const int hi = s_hi[r];
                         for (int k0 = s_lo[r]; k0 < hi; k0 += 64) {
                             const int rows = hi - k0;                  // MMAs of 16 rows each, up to four
-                            const uint32_t src = ring + stage * G_STAGE_BYTES;
+                            const uint32_t src = ring + stage * stage_bytes;
                             const uint64_t a_desc = smem_desc_mn(src), b_desc = smem_desc_mn(src + 2 * G_BOX_BYTES);
                             bad = mbar_wait_conv(smem_u32(&hd.full[stage]), phase, abort_addr, bad, lead_lane);
                             tc_fence_after();
@@ -417,13 +444,13 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                                 umma_commit_both(smem_u32(&hd.empty[stage]));
                             }
                             first = false;
-                            if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                            if (++stage == n_stages) { stage = 0; phase ^= 1u; }
                         }
                     }
                 } else {
                     const int k_steps = token_steps(it.e);
                     for (int kb = 0; kb < k_steps; ++kb) {
-                        const uint32_t src = ring + stage * G_STAGE_BYTES;
+                        const uint32_t src = ring + stage * stage_bytes;
                         const uint64_t a_desc = smem_desc_mn(src), b_desc = smem_desc(src + 2 * G_BOX_BYTES);
                         bad = mbar_wait_conv(smem_u32(&hd.full[stage]), phase, abort_addr, bad, lead_lane);
                         tc_fence_after();
@@ -433,7 +460,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                                 umma_pair_n(d_tmem, a_desc + 128u * k, b_desc + 2u * k, idesc, (kb | k) != 0 ? 1u : 0u);
                             umma_commit_both(smem_u32(&hd.empty[stage]));
                         }
-                        if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
                     }
                 }
                 if (__any_sync(0xFFFFFFFFu, bad != 0u)) break;
@@ -457,7 +484,8 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     }
                     if (give_up) { *abort_flag = 1; break; }
                 }
-                const unsigned int c = atomicAdd(p.counter, 1u);
+                // a pair's first item is the one of its number, the others come from the counter
+                const unsigned int c = i == 0 ? blockIdx.x >> 1 : (gridDim.x >> 1) + atomicAdd(p.counter, 1u);
                 const int w = c < (unsigned)total ? (int)c : total;
                 const int q = i & (G_SLOTS - 1);
                 if (!mbar_wait(smem_u32(&hd.sched_empty[q]), (((uint32_t)i / G_SLOTS) & 1u) ^ 1u, abort_flag)) break;

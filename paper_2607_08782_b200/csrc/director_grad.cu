@@ -22,7 +22,8 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 //
 // One warp per assignment (t, s): it reads dy[t] and the row of yp once, writes the row of dyp, and the dot product is a sum
 // over its lanes - no atomics, so dw has the same bits on every run.  The K warps of a token sit next to each other in a CTA,
-// so that dy[t] comes from HBM once and from L1 after that.
+// so that dy[t] comes from HBM once and from L1 after that.  T = 32768, H = 2048, K = 8: 372 us, 6.1 TB/s; with four pieces of a row
+// per lane asked for together the registers cost occupancy (390 us), and a small batch is no faster, its call being launch-bound.
 constexpr int kRowWarps = 8;
 
 __global__ void __launch_bounds__(kRowWarps * 32)
