@@ -8,7 +8,7 @@
 // order and writes 16 bytes.  HBM-bound gather: 2HK + 8K (+2H) bytes read, 2H written per token.
 //
 // With topk_w == nullptr all weights are one: the gradient of the dispatch (a token's row was copied to its K assignments, so
-// its gradient is the sum of theirs, plus the shared experts').
+// its gradient is the sum of theirs, plus the shared experts').  T = 16384, H = 2048, K = 4 with the shared experts': 66 us, 6.1 TB/s.
 #include "director_common.cuh"
 
 #include <cuda_bf16.h>

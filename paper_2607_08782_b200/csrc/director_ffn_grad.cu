@@ -26,9 +26,14 @@
 //     zeroes the rows behind the end inside the last one, in both operands (a zero times another expert's infinity would be
 //     NaN).  Experts are taken by descending length, so that the longest contractions do not end the launch.
 //     A tile goes out through shared memory and TMA stores: a lane holds 32 consecutive columns of one row, which as plain
-//     stores would touch 32 lines an instruction.  An expert without rows gets its zeros the same way, from a cleared buffer.
+//     stores would touch 32 lines an instruction.  An expert without rows gets its zeros the same way.
 // Work items are claimed from a global counter and handed to all roles through a small ring, as in the forward kernel.
 // Every wait is bounded; an expired one raises DIRECTOR_ERR_TIMEOUT.
+//
+// What bounds it: long segments, the tensor pipe - a 64-deep step takes 508-520 cycles, the pipe's four MMAs 512 - at the clock the
+// power cap leaves (8192 rows, eight experts, H = 4096, F = 14336: 0.73-0.85 and 3.65-3.95 ms for the two launches, 1.2-1.3
+// PFLOP/s); few rows per expert, HBM (8168 rows, 128 experts, H = 2048, F = 768: 77 and 307 us, 5.3 TB/s of weights read and
+// gradients written); a handful of rows, the launches' own latencies (8 us each).
 #include "director_common.cuh"
 #include "director_umma.cuh"
 
@@ -57,6 +62,7 @@ constexpr int grad_epi_warps(int phase) { return phase == 0 ? 12 : 8; }
 constexpr int grad_threads(int phase) { return 128 + 32 * grad_epi_warps(phase); }   // producer, MMA, scheduler and tail warps + epilogue
 constexpr int G_TILE = 256;                            // most tokens per tile; accumulators are this many columns apart
 constexpr int G_SLOTS = 4;                             // ring of work items
+constexpr int G_PACED_STEPS = 128;                     // contractions this long are paced
 constexpr int G_CLAIM_LEAD = 32;                       // k-steps of claimed work ahead of the producer
 
 constexpr int G_OUT_BYTES = 32 * 64;                   // per epilogue warp: 32 rows x 32 bf16 columns of a weight gradient
@@ -449,12 +455,20 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     }
                 } else {
                     const int k_steps = token_steps(it.e);
+                    // The ragged end of a segment in a long contraction is held to a full tile's speed, as in the forward's down
+                    // projection: pairs that run ahead stop meeting their neighbours' operands in L2.  F = 14336, H = 4096 (448
+                    // steps): DRAM reads of the launch 2.74 -> 1.90 GB on four experts, a call 4.89 -> 4.75 ms on eight; no
+                    // difference at 252 steps (F = 8064) or at 44 and 128 (F = 1408, 4096).
+                    const bool paced = PHASE == 1 && k_steps >= G_PACED_STEPS && it.valid < G_TILE && hd.tile == G_TILE;
+                    const uint32_t c_pace = (uint32_t)clock();
                     for (int kb = 0; kb < k_steps; ++kb) {
                         const uint32_t src = ring + stage * stage_bytes;
                         const uint64_t a_desc = smem_desc_mn(src), b_desc = smem_desc(src + 2 * G_BOX_BYTES);
                         bad = mbar_wait_conv(smem_u32(&hd.full[stage]), phase, abort_addr, bad, lead_lane);
                         tc_fence_after();
                         if (lead_lane && !bad) {
+                            if (paced)
+                                while ((uint32_t)clock() - c_pace < 512u * (uint32_t)kb) {}
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 umma_pair_n(d_tmem, a_desc + 128u * k, b_desc + 2u * k, idesc, (kb | k) != 0 ? 1u : 0u);

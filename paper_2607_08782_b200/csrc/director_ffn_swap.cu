@@ -192,7 +192,9 @@ struct SwapWalker {
 // input x through row_token - tm_x then describes x with a one-row box and the whole producer warp issues the
 // loads, four rows per lane - so the dispatch step needs no row copies at all.
 // GEMM-1, ALT_CHECKPOINT: the forward pass of training - besides the SwiGLU activations the epilogue writes every gate and up
-// value in 8 bits (see checkpoint_exponent), which is what the backward pass reads instead of repeating this GEMM.
+// value in 8 bits (director_checkpoint.cuh), which is what the backward pass reads instead of repeating this GEMM.  The epilogue
+// drains a tile in 12.9k cycles then (3.9k without), still less than its products take from a contraction of about 1700 on
+// (8192 tokens, 64 experts top-6 and two shared, H = 2048, F = 1408: 568 us, without 565).
 constexpr int ALT_NONE = 0, ALT_FUSED = 1, ALT_CHECKPOINT = 2;
 
 template <int MODE, int EPI_GROUPS, int ALT, int S_STAGES>

@@ -11,6 +11,7 @@ import argparse
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from .layer import MoELayer
 
@@ -27,6 +28,7 @@ class _Layer(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         layer = ctx.layer
         if getattr(layer, "step", None) is not ctx.step:

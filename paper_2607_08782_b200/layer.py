@@ -27,6 +27,7 @@ class MoELayer:
         self.dims = dict(T_max=T_max, H=H, F=F, E=E, K=K, S=S, R=R, C_max=C_max)
         self.d = Director(T_max, H, F, E, K, S, R, C_max)
         self.ffn_variant = 2
+        self.trained = None        # (T, x) of the training forward whose buffers are intact: its backward pass may run
         self.w = (w_gate, w_up, w_down)
         self.ws = (ws_gate, ws_up, ws_down)
         A, G = T_max * K, R * C_max
@@ -56,6 +57,7 @@ class MoELayer:
         self.ffn_variant = variant
 
     def route(self, T, logits):
+        self.trained = None
         self.d.route(T, logits, self.topk_idx, self.topk_w)
 
     def set_replica_policy(self, policy: int):
@@ -63,6 +65,7 @@ class MoELayer:
         self.d.set_replica_policy(policy)
 
     def dispatch(self, T, x, indices_only=False, token_src_rank=None):
+        self.trained = None
         xp = None if indices_only else self.xp
         if token_src_rank is None:
             self.d.dispatch(T, x, self.topk_idx, xp, self.row_token, self.inv_row, self.dest_rank, self.seg_offsets)
@@ -81,11 +84,13 @@ class MoELayer:
     def expert_ffn_gather(self, T, x):
         """The routed experts read their rows from x through row_token (no permuted copy)."""
         S = self.dims["S"]
+        self.trained = None
         self.d.expert_ffn_gather(T, x, self.row_token, self.seg_offsets, *self.w, self.yp,
                                  *(self.ws if S > 0 else (None, None, None)), self.y_shared if S > 0 else None)
 
     def expert_ffn(self, T, x=None):
         S = self.dims["S"]
+        self.trained = None
         self.d.expert_ffn(T, self.xp, self.seg_offsets, *self.w, self.yp,
                           x if S > 0 else None, *(self.ws if S > 0 else (None, None, None)),
                           self.y_shared if S > 0 else None)
@@ -126,7 +131,6 @@ class MoELayer:
                                 torch.empty((SF // 16, T, 2), dtype=torch.uint8, device=dev))
             self.dx_shared = torch.empty_like(grads["x"])
             grads.update({n: torch.empty_like(w) for n, w in zip(("ws_gate", "ws_up", "ws_down"), self.ws)})
-        self.trained = None                    # (T, x) of the forward pass whose backward pass is due
         self.grads = grads
 
     def forward_train(self, T, logits, x):
@@ -144,8 +148,8 @@ class MoELayer:
     def backward(self, T, dy):
         """Gradients of the forward_train() before, given dy = dL/dy [T,H] (bf16): a dict of x [T,H], logits [T,E], w_gate, w_up,
         w_down and, with shared experts, ws_gate, ws_up, ws_down - views of the layer's buffers, overwritten by the next call."""
-        if getattr(self, "trained", None) is None or self.trained[0] != T:
-            raise RuntimeError("backward() without a forward_train() of the same batch")
+        if self.trained is None or self.trained[0] != T:
+            raise RuntimeError("backward() needs the buffers of a forward_train() of the same batch size, with no pass of the layer in between")
         (_, x), self.trained = self.trained, None
         g = self.grads
         self.d.combine_backward(T, dy, self.yp, self.inv_row, self.topk_w, self.dyp, self.dtopk_w)
@@ -169,6 +173,7 @@ class MoELayer:
         # a batch small enough for the weight-streaming FFN kernels needs no permuted copy either: they stage a
         # segment's few rows from x themselves
         gather = (fused and self.ffn_variant == 2) or (self.d.batch_streams_weights(T) and not fused_combine)
+        self.trained = None
         if with_cost:          # front end in one call (a single launch for decode-sized batches)
             self.d.route_dispatch_cost(T, logits, x, self.topk_idx, self.topk_w, None if gather else self.xp,
                                        self.row_token, self.inv_row, self.dest_rank, self.seg_offsets, self.workload,

@@ -531,6 +531,23 @@ def test_ffn_backward_of_random_layouts(seed):
     _check_backward(f)
 
 
+def test_ffn_backward_with_the_largest_tables():
+    """256 experts on 64 ranks, every one of the 1024 slots taken (four replicas an expert) and most segments empty or one row long;
+    a shared expert beside them."""
+    rng = np.random.default_rng(77)
+    E, R, C = 256, 64, 16
+    X = np.zeros((E, R), dtype=np.uint8)
+    for e in range(E):
+        X[e, (e // 16 + 16 * np.arange(4)) % R] = 1
+    assert (X.sum(0) == C).all()
+    lengths = [int(v) for v in rng.choice([0, 0, 0, 0, 0, 0, 1, 1, 2, 17], size=R * C)]
+    f = FfnGradient(77, lengths, X, C, 256, 128, S=1)
+    f.d.reserve_training()
+    f.backward()
+    assert f.d.last_status() == 0
+    _check_backward(f)
+
+
 def test_what_is_not_finite_stays_with_its_expert():
     """An expert's rows full of NaN and infinity, next to another's in the permuted order: a step of the other's contraction
     that reads past its segment must not pick them up."""

@@ -117,6 +117,9 @@ def test_only_what_needs_a_gradient_gets_one_and_order_is_checked():
     layer.forward_train(8, logits.detach(), x)
     with pytest.raises(RuntimeError):
         layer.backward(7, x[:7])
+    layer.forward(8, logits.detach(), x)                  # a serving pass in between has taken the buffers
+    with pytest.raises(RuntimeError):
+        layer.backward(8, x)
     with pytest.raises(TypeError):
         moe_layer(layer, x.float(), logits)
     with pytest.raises(ValueError):
