@@ -130,6 +130,7 @@ struct GradParams {
 
 struct GradItem {
     int a, valid, e, b, kind;      // tokens: first row, rows (0: end), expert, block;   weights: h block, 1, expert, f block
+    int later;                     // tokens: not the first tile of its segment
 };
 
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
@@ -157,7 +158,7 @@ __device__ __forceinline__ uint64_t offset_by(const void* base, uint32_t bytes) 
     return r;
 }
 __device__ __forceinline__ void store_u32(uint64_t addr, uint32_t v) {
-    *reinterpret_cast<uint32_t*>(addr) = v;
+    asm volatile("st.global.b32 [%0], %1;" ::"l"(addr), "r"(v) : "memory");
 }
 
 // 16 bytes into the shared memory of a CTA of the cluster, counted on an mbarrier there when they have arrived
@@ -319,7 +320,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
         const bool ok = mbar_wait(bar, par, abort_flag);
         if (ok) {
             const int4 v = hd.item[q];
-            it = GradItem{v.x, v.y, v.z, v.w & 0x0FFFFFFF, v.w >> 28};
+            it = GradItem{v.x, v.y, v.z, v.w & 0x07FFFFFF, v.w >> 28, (v.w >> 27) & 1};
         }
         return ok;
     };
@@ -335,6 +336,7 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
         it.e = __shfl_sync(0xFFFFFFFFu, it.e, 0);
         it.b = __shfl_sync(0xFFFFFFFFu, it.b, 0);
         it.kind = PHASE == 0 ? GRAD_ACT : __shfl_sync(0xFFFFFFFFu, it.kind, 0);
+        it.later = __shfl_sync(0xFFFFFFFFu, it.later, 0);
         if (ok && lane == 0) release_item(i);
         return ok && it.valid != 0;
     };
@@ -458,8 +460,9 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     // The ragged end of a segment in a long contraction is held to a full tile's speed, as in the forward's down
                     // projection: pairs that run ahead stop meeting their neighbours' operands in L2.  F = 14336, H = 4096 (448
                     // steps): DRAM reads of the launch 2.74 -> 1.90 GB on four experts, a call 4.89 -> 4.75 ms on eight; no
-                    // difference at 252 steps (F = 8064) or at 44 and 128 (F = 1408, 4096).
-                    const bool paced = PHASE == 1 && k_steps >= G_PACED_STEPS && it.valid < G_TILE && hd.tile == G_TILE;
+                    // difference at 252 steps (F = 8064) or at 44 and 128 (F = 1408, 4096).  Not where a segment has no full tile:
+                    // few rows per expert stream weights and lose by waiting.
+                    const bool paced = PHASE == 1 && k_steps >= G_PACED_STEPS && it.later && it.valid < G_TILE && hd.tile == G_TILE;
                     const uint32_t c_pace = (uint32_t)clock();
                     for (int kb = 0; kb < k_steps; ++kb) {
                         const uint32_t src = ring + stage * stage_bytes;
@@ -517,7 +520,8 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                             nth -= n;
                         }
                         const int row0 = s_lo[r] + nth * tile;
-                        item = make_int4(row0, min(tile, s_hi[r] - row0), e, wb | ((PHASE == 0 ? GRAD_ACT : GRAD_DX) << 28));
+                        item = make_int4(row0, min(tile, s_hi[r] - row0), e,
+                                         wb | ((nth > 0 ? 1 : 0) << 27) | ((PHASE == 0 ? GRAD_ACT : GRAD_DX) << 28));
                         pub_k += token_steps(e);
                     } else if (PHASE == 1) {
                         const int v = w - token_items;
