@@ -584,6 +584,18 @@ def test_ffn_backward_is_the_derivative():
             assert abs((value[0] - value[1]) / 2e-4 - size) <= 0.02 * size, (e, name)
 
 
+def test_without_x_the_shared_experts_are_left_out():
+    lengths, X, C = _layout("ragged")
+    f = FfnGradient(12, lengths, X, C, 256, 128, S=1)
+    f.d.reserve_training()
+    f.codes.fill_(99)
+    f.d.expert_ffn_checkpoint(f.T, f.xp, f.seg, f.wg, f.wu, f.wd, f.codes, f.exps, f.yp)
+    f.d.expert_ffn_backward(f.T, f.xp, f.dyp, f.seg, f.codes, f.exps, f.wg, f.wu, f.wd, f.dxp, *f.dw)
+    assert f.d.last_status() == 0 and bool((f.dx_s == 7).all()) and all(bool((w == 7).all()) for w in f.dws)
+    f.S = 0
+    _check_backward(f)
+
+
 def test_refusals_of_the_ffn_gradient():
     import torch
     from paper_2607_08782_b200.binding import DirectorError
