@@ -70,6 +70,9 @@ constexpr int TOKEN_STEP = 32;                                 // granularity of
 // and store; one warp per quadrant with a large register budget (all 32 stores of a chunk in flight) is faster.
 constexpr int EPI_GROUPS_GEMM1 = 2;
 constexpr int EPI_GROUPS_GEMM2 = 1;
+// With the 8-bit values to write as well, three (8192 tokens, 64 experts top-6, F = 1408: H = 512 300 -> 278 us, H = 1024 374 -> 354,
+// H = 2048 566 -> 556).
+constexpr int EPI_GROUPS_CHECKPOINT = 3;
 
 // kind::f16 descriptor for the pair without the N field: D=f32, A=B=bf16, K-major, M=256.
 constexpr uint32_t S_IDESC_BASE = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(256 >> 4) << 24);
@@ -193,8 +196,9 @@ struct SwapWalker {
 // loads, four rows per lane - so the dispatch step needs no row copies at all.
 // GEMM-1, ALT_CHECKPOINT: the forward pass of training - besides the SwiGLU activations the epilogue writes every gate and up
 // value in 8 bits (director_checkpoint.cuh), which is what the backward pass reads instead of repeating this GEMM.  The epilogue
-// drains a tile in 12.9k cycles then (3.9k without), still less than its products take from a contraction of about 1700 on
-// (8192 tokens, 64 experts top-6 and two shared, H = 2048, F = 1408: 568 us, without 565).
+// drains a tile in some 12k cycles then (3.9k without; 35 of its 67 instructions per two tokens are integer and select
+// instructions, which bound it), less than the products take from a contraction of about 1600 on (8192 tokens, 64 experts
+// top-6 and two shared, H = 2048, F = 1408: 568 us, without 565).
 constexpr int ALT_NONE = 0, ALT_FUSED = 1, ALT_CHECKPOINT = 2;
 
 template <int MODE, int EPI_GROUPS, int ALT, int S_STAGES>
@@ -220,7 +224,8 @@ grouped_gemm_swap_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + HX + 224);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + HX + 228);
     int4* sched_item = reinterpret_cast<int4*>(gen + HX + 304);    // [4] decoded work items {row0, valid, w_row, wb}
-    int32_t* warp_sum = reinterpret_cast<int32_t*>(gen + HX + 248);     // [11]
+    // [warps] per-warp tile counts of the prologue; for more than eleven warps in the ring of work items, which is used later
+    int32_t* warp_sum = reinterpret_cast<int32_t*>(gen + HX + (EPI_GROUPS > 2 ? 304 : 248));
     volatile int* prod_k = reinterpret_cast<volatile int*>(gen + HX + 292);  // k-steps the scheduler CTA's producer has issued so far
     const int G = p.G;
     int32_t* s_seg = reinterpret_cast<int32_t*>(gen + HEADER_BYTES);
@@ -794,7 +799,7 @@ bool swap_opt_in() {
 
 int ffn_swap_init(director_ctx*) {
     if (!swap_opt_in<0, EPI_GROUPS_GEMM1, ALT_NONE>() || !swap_opt_in<0, EPI_GROUPS_GEMM1, ALT_FUSED>() ||
-        !swap_opt_in<0, EPI_GROUPS_GEMM1, ALT_CHECKPOINT>() || !swap_opt_in<1, EPI_GROUPS_GEMM2, ALT_NONE>() ||
+        !swap_opt_in<0, EPI_GROUPS_CHECKPOINT, ALT_CHECKPOINT>() || !swap_opt_in<1, EPI_GROUPS_GEMM2, ALT_NONE>() ||
         !swap_opt_in<1, EPI_GROUPS_GEMM2, ALT_FUSED>())
         return DIRECTOR_ERR_CUDA;
     return DIRECTOR_OK;
@@ -858,7 +863,7 @@ int ffn_pass_swap(director_ctx* ctx, const void* in, uint64_t in_rows, const int
                   counters, gather_rows, nullptr, d_rows, d_Fw / 128, H / BLOCK_K, d_Fw, id.gate_first ? 1 : 0,
                   dense ? dense->hidden : nullptr, clk, kept ? *kept : Checkpoint{}, dense && dense_kept ? *dense_kept : Checkpoint{}};
     int rc = gather_rows ? launch_swap<0, EPI_GROUPS_GEMM1, ALT_FUSED>(ctx, "grouped_gemm_swiglu_kernel", m_gu, m_in, d_gu, d_in, p1, false, st)
-             : kept ? launch_swap<0, EPI_GROUPS_GEMM1, ALT_CHECKPOINT>(ctx, "grouped_gemm_checkpoint_kernel", m_gu, m_in, d_gu, d_in, p1, small, st)
+             : kept ? launch_swap<0, EPI_GROUPS_CHECKPOINT, ALT_CHECKPOINT>(ctx, "grouped_gemm_checkpoint_kernel", m_gu, m_in, d_gu, d_in, p1, small, st)
                     : launch_swap<0, EPI_GROUPS_GEMM1, ALT_NONE>(ctx, "grouped_gemm_swiglu_kernel", m_gu, m_in, d_gu, d_in, p1, small, st);
     if (rc != DIRECTOR_OK) return rc;
     // with fc the routed experts' output is not Yp but the fp32 accumulator of y (pitch H floats), see the kernel's ALT
