@@ -23,7 +23,8 @@
  *   - Every pointer marked "dev" is caller-owned device memory on the context's device,
  *     16-byte aligned, valid until the stream has reached the call.  "host" pointers are
  *     ordinary host memory.  The context owns only its internal workspace, sized at create
- *     time; no entry point allocates after director_create (except director_reserve_placements).
+ *     time; no entry point allocates after director_create (except director_reserve_placements and
+ *     director_reserve_training).
  *   - bf16 tensors are passed as void* (raw 16-bit patterns), row-major, innermost last.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).
  *   - Calls are asynchronous on `stream` and never synchronise unless stated.  Every function
@@ -64,8 +65,8 @@ typedef struct {
     int32_t H, F, E, K, S, R, C_max;
 } director_shape;
 
-/* Life cycle.  director_create allocates the workspace on the current device (it is the only
- * call that allocates) and binds the context to that device. */
+/* Life cycle.  director_create allocates the workspace on the current device (besides the two
+ * director_reserve_* calls it is the only one that allocates) and binds the context to that device. */
 int director_create(const director_shape* shape, director_ctx** out);
 int director_destroy(director_ctx* ctx);
 
@@ -78,8 +79,8 @@ int director_set_placement(director_ctx* ctx, const uint8_t* X_host, void* strea
 
 /* Several placements on one context (the placement map P(l, i) of Section VI-A has one placement per layer l;
  * a model's layers can share one context's workspace and differ only in their tables).
- * director_reserve_placements makes room for n table sets (slots 0..n-1; slot 0 exists from creation; this is the
- * one call besides director_create that allocates).  director_select_placement makes a slot the current one: a
+ * director_reserve_placements makes room for n table sets (slots 0..n-1; slot 0 exists from creation; this call
+ * allocates).  director_select_placement makes a slot the current one: a
  * host-side switch, no copy, no stream work; kernels already launched keep the tables they were launched with.
  * director_set_placement fills the current slot; every entry point uses the current slot.  Selecting a slot that
  * was never filled leaves the context without a placement (DIRECTOR_ERR_PLACEMENT from the calls that need one). */
@@ -257,7 +258,7 @@ int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const
                                void* gate, void* up, void* stream);
 
 /* Workspace of director_expert_ffn_backward: two bf16 arrays [T_max*K,F] (and two [T_max,S*F]) on the context.  Allocates on
- * the first call, does nothing on later ones; serving contexts never pay for it. */
+ * the first call (and may synchronise the device), does nothing on later ones; serving contexts never pay for it. */
 int director_reserve_training(director_ctx* ctx);
 
 /* Gradients of director_expert_ffn_checkpoint at the gate and up values that it kept (s = sigmoid(g), e the row's expert):

@@ -8,7 +8,8 @@
 // order and writes 16 bytes.  HBM-bound gather: 2HK + 8K (+2H) bytes read, 2H written per token.
 //
 // With topk_w == nullptr all weights are one: the gradient of the dispatch (a token's row was copied to its K assignments, so
-// its gradient is the sum of theirs, plus the shared experts').  T = 16384, H = 2048, K = 4 with the shared experts': 66 us, 6.1 TB/s.
+// its gradient is the sum of theirs, plus the shared experts').  T = 16384, H = 2048, K = 4 with the shared experts': 64 us, 6.3 TB/s
+// (with streaming loads, evict first, 66; T = 32768, K = 8: 180 against 187).
 #include "director_common.cuh"
 
 #include <cuda_bf16.h>
@@ -71,7 +72,7 @@ combine_kernel(const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row
 #pragma unroll
             for (int i = 0; i < kVecPerLane; ++i) {
                 v[s][i] = make_uint4(0u, 0u, 0u, 0u);
-                if (rows[s] >= 0 && v0 + 32 * i < row_vec) v[s][i] = __ldcs(yp + (size_t)rows[s] * row_vec + v0 + 32 * i);
+                if (rows[s] >= 0 && v0 + 32 * i < row_vec) v[s][i] = __ldg(yp + (size_t)rows[s] * row_vec + v0 + 32 * i);
             }
         }
 #pragma unroll
@@ -85,13 +86,13 @@ combine_kernel(const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row
             if (row < 0) continue;
 #pragma unroll
             for (int i = 0; i < kVecPerLane; ++i)
-                if (v0 + 32 * i < row_vec) fma_bf16x8(acc[i], __ldcs(yp + (size_t)row * row_vec + v0 + 32 * i), w);
+                if (v0 + 32 * i < row_vec) fma_bf16x8(acc[i], __ldg(yp + (size_t)row * row_vec + v0 + 32 * i), w);
         }
     }
 #pragma unroll
     for (int i = 0; i < kVecPerLane; ++i) {
         if (v0 + 32 * i >= row_vec) continue;
-        if (y_shared) fma_bf16x8(acc[i], __ldcs(y_shared + (size_t)t * row_vec + v0 + 32 * i), 1.0f);
+        if (y_shared) fma_bf16x8(acc[i], __ldg(y_shared + (size_t)t * row_vec + v0 + 32 * i), 1.0f);
         uint4 o;
         o.x = pack_bf16x2(acc[i][0], acc[i][1]);
         o.y = pack_bf16x2(acc[i][2], acc[i][3]);

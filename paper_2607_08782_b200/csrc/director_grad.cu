@@ -22,9 +22,10 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 //
 // One warp per assignment (t, s): it reads dy[t] and the row of yp once, writes the row of dyp, and the dot product is a sum
 // over its lanes - no atomics, so dw has the same bits on every run.  The K warps of a token sit next to each other in a CTA,
-// so that dy[t] comes from HBM once and from L1 after that.  T = 32768, H = 2048, K = 8: 372 us, 6.1 TB/s; with four pieces of a row
-// per lane asked for together the registers cost occupancy (390 us), and a small batch is no faster, its call being launch-bound.
-constexpr int kRowWarps = 8;
+// so that dy[t] comes from HBM once and from L1 or L2 after that.  T = 32768, H = 2048, K = 8: 360 us, 6.3 TB/s.  Tried there: CTAs
+// of 8 warps + 1 %, 16 + 4 %; rows of yp loaded as streaming (evict first) + 4 %, dyp stored so + 11 %; four pieces of a row per
+// lane asked for together + 4 % (registers cost occupancy), and no faster for a small batch, whose call is launch-bound.
+constexpr int kRowWarps = 4;
 
 __global__ void __launch_bounds__(kRowWarps * 32)
 combine_backward_kernel(const uint4* __restrict__ dy, const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row,
@@ -49,7 +50,7 @@ combine_backward_kernel(const uint4* __restrict__ dy, const uint4* __restrict__ 
     uint4* o = dyp + (size_t)row * row_vec;
     float dot = 0.0f;
     for (int v = lane; v < row_vec; v += 32) {
-        const uint4 a = __ldg(g + v), b = __ldcs(y + v);
+        const uint4 a = __ldg(g + v), b = __ldg(y + v);
         const uint32_t ga[4] = {a.x, a.y, a.z, a.w}, yb[4] = {b.x, b.y, b.z, b.w};
         uint32_t r[4];
 #pragma unroll
