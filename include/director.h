@@ -224,7 +224,8 @@ int director_combine_backward(director_ctx* ctx, int32_t T, const void* dy, cons
 
 /* Gradient of director_dispatch's row copies:  dx[t,:] = bf16( sum_s dxp[inv_row[t,s],:] (+ dx_shared[t,:]) ), summed in
  * slot order.  dxp: dev bf16 [T*K,H].  inv_row: dev int32 [T,K].  dx_shared: dev bf16 [T,H], the shared experts' (or any
- * other branch's) gradient of x, or NULL.  dx: dev bf16 [T,H]. */
+ * other branch's) gradient of x, or NULL.  dx: dev bf16 [T,H].
+ * An assignment with inv_row < 0 adds nothing; a row >= T*K is skipped the same way and reported as DIRECTOR_ERR_BAD_INDEX. */
 int director_dispatch_backward(director_ctx* ctx, int32_t T, const void* dxp, const int32_t* inv_row,
                                const void* dx_shared, void* dx, void* stream);
 

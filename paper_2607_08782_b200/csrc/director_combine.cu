@@ -40,7 +40,7 @@ template <int K_T>   // K_T > 0: compile-time top-k (fully unrolled gathers); 0:
 __global__ void __launch_bounds__(kCombineWarps * 32)
 combine_kernel(const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row, const float* __restrict__ topk_w,
                const uint4* __restrict__ y_shared, uint4* __restrict__ y, int T, int K_rt, int row_vec,
-               int slices_per_row) {
+               int slices_per_row, int rows_end, int32_t* status) {
     chain_prologue();
     const int K = K_T > 0 ? K_T : K_rt;
     const int lane = threadIdx.x & 31;
@@ -54,6 +54,10 @@ combine_kernel(const uint4* __restrict__ yp, const int32_t* __restrict__ inv_row
     if (lane < K) {
         my_row = __ldg(inv_row + (size_t)t * K + lane);
         my_w = topk_w ? __ldg(topk_w + (size_t)t * K + lane) : 1.0f;
+        if (my_row >= rows_end) {                   // no row of this batch: skipped, as in the combine's gradient
+            my_row = -1;
+            director_set_status(status, DIRECTOR_ERR_BAD_INDEX);
+        }
     }
     float acc[kVecPerLane][8];
 #pragma unroll
@@ -112,11 +116,14 @@ int launch_combine(director_ctx* ctx, int T, const void* yp, const int32_t* inv_
     const int slices = (row_vec + kCombineSliceVec - 1) / kCombineSliceVec;
     const long long items = (long long)T * slices;
     const unsigned grid = (unsigned)((items + kCombineWarps - 1) / kCombineWarps);
+    // The gradient reads rows [0, T*K) alone.  The forward puts no end to them: with a whole batch's yp it may be given some of
+    // the batch's tokens.
+    const int rows_end = topk_w ? INT32_MAX : T * s.K;
     LaunchScope scope(ctx, st, topk_w ? "combine_kernel" : "dispatch_backward_kernel");
 #define COMBINE_LAUNCH(KT)                                                                                      \
     launch_chained(combine_kernel<KT>, dim3(grid), dim3(kCombineWarps * 32), 0, st, static_cast<const uint4*>(yp),  \
                    inv_row, topk_w, static_cast<const uint4*>(y_shared), static_cast<uint4*>(y), T, (int)s.K, row_vec,  \
-                   slices)
+                   slices, rows_end, ctx->d_status)
     switch (s.K) {
         case 1: COMBINE_LAUNCH(1); break;
         case 2: COMBINE_LAUNCH(2); break;
