@@ -259,7 +259,7 @@ int director_checkpoint_decode(director_ctx* ctx, int32_t rows, int32_t F, const
                                void* gate, void* up, void* stream);
 
 /* Workspace of director_expert_ffn_backward: two bf16 arrays [T_max*K,F] (and two [T_max,S*F]) on the context.  Allocates on
- * the first call (and may synchronise the device), does nothing on later ones; serving contexts never pay for it. */
+ * the first call (and waits for the legacy default stream), does nothing on later ones; serving contexts never pay for it. */
 int director_reserve_training(director_ctx* ctx);
 
 /* Gradients of director_expert_ffn_checkpoint at the gate and up values that it kept (s = sigmoid(g), e the row's expert):

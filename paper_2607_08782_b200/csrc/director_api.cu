@@ -21,6 +21,10 @@ bool dev_alloc(T** p, size_t count) {
     return cudaMalloc(reinterpret_cast<void**>(p), count * sizeof(T)) == cudaSuccess;
 }
 
+// cudaMemset is work on the legacy default stream like any other: it may still be queued there when the call returns, and a
+// stream made with cudaStreamNonBlocking does not wait for it.
+bool zeros_written() { return cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess; }
+
 bool shape_supported(const director_shape& s) {
     if (s.T_max < 1 || s.H < 256 || s.F < 128 || s.E < 1 || s.K < 1 || s.S < 0 || s.R < 1 || s.C_max < 1) return false;
     if (s.K > kMaxK || s.K > s.E || s.E > kMaxE || s.R > kMaxR || s.C_max > kMaxC) return false;
@@ -529,7 +533,7 @@ int director_reserve_training(director_ctx* ctx) {
     uint16_t *dgu = nullptr, *dgu_shared = nullptr;
     unsigned int* sched = nullptr;
     if (!dev_alloc(&dgu, 2 * (size_t)s.T_max * s.K * s.F) || !dev_alloc(&dgu_shared, 2 * (size_t)s.T_max * s.S * s.F) ||
-        !dev_alloc(&sched, 2) || cudaMemset(sched, 0, 2 * sizeof(unsigned int)) != cudaSuccess) {
+        !dev_alloc(&sched, 2) || cudaMemset(sched, 0, 2 * sizeof(unsigned int)) != cudaSuccess || !zeros_written()) {
         cudaGetLastError();
         void* ptrs[] = {dgu, dgu_shared, sched};
         for (void* p : ptrs)

@@ -6,6 +6,26 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 
+def _layer(S=1, F=256, seed=3):
+    from paper_2607_08782_b200.finetune import make_layer
+    return make_layer(64, 256, F, 8, 2, S, 4, 3, _placement(0), seed)
+
+
+def _placement(which):
+    """Eight experts on four ranks, expert `which` with a replica on another rank."""
+    X = np.zeros((8, 4), dtype=np.uint8)
+    X[np.arange(8), np.arange(8) // 2] = 1
+    X[which, 3 - which // 2] = 1
+    return X
+
+
+def _inputs(seed=0, T=64):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn((T, 8), generator=g, device="cuda"), torch.randn((T, 256), generator=g, device="cuda").bfloat16(),
+            torch.randn((T, 256), generator=g, device="cuda").bfloat16())
+
+
 @pytest.mark.parametrize("K", [1, 2, 3, 6, 8])
 @pytest.mark.parametrize("H", [256, 768])
 def test_dispatch_backward_skips_and_reports_a_row_past_the_end(K, H):
@@ -30,3 +50,56 @@ def test_dispatch_backward_skips_and_reports_a_row_past_the_end(K, H):
     table[4, K - 1] = -1                                                          # nothing there is no error
     d.dispatch_backward(T, room, table, None, dx)
     assert d.last_status() == 0
+
+
+# ---- the workspace -------------------------------------------------------------------------------------------------
+
+
+def _freed_garbage():
+    """Leaves small pieces of device memory behind that are not zero, for the next small allocations to find."""
+    import ctypes
+    import torch
+    cuda = ctypes.CDLL("libcudart.so.12")
+    pieces = []                                           # 4 MB of them: every hole in the small blocks is filled once
+    for _ in range(8192):
+        p = ctypes.c_void_p()
+        assert cuda.cudaMalloc(ctypes.byref(p), ctypes.c_size_t(512)) == 0
+        assert cuda.cudaMemset(p, 0x01, ctypes.c_size_t(512)) == 0
+        pieces.append(p)
+    torch.cuda.synchronize()
+    for p in pieces:
+        assert cuda.cudaFree(p) == 0
+
+
+def _busy(stream, ms):
+    """Ordinary work for about `ms` milliseconds."""
+    import torch
+    with torch.cuda.stream(stream):
+        a = torch.zeros(1 << 28, device="cuda")            # 1 GB: about 0.3 ms a pass
+        for _ in range(int(ms / 0.3)):
+            a.add_(1.0)
+
+
+def _train_once(layer, logits, x, dy):
+    layer.forward_train(64, logits, x)
+    return {n: t.clone() for n, t in layer.backward(64, dy).items()}
+
+
+def test_the_first_training_step_runs_beside_a_busy_default_stream():
+    """The training workspace is ready when the call that makes it returns, whatever the default stream still has to do: torch's
+    side streams do not wait for it."""
+    import torch
+    logits, x, dy = _inputs()
+    want = _train_once(_layer(F=4096), logits, x, dy)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        layer = _layer(F=4096)                           # more work items than the GPU has SMs: the counters matter
+        torch.cuda.synchronize()
+        _freed_garbage()
+        _busy(torch.cuda.default_stream(), 200)
+        with torch.cuda.stream(side):
+            got = _train_once(layer, logits, x, dy)
+        side.synchronize()
+        assert all(torch.equal(want[n], got[n]) for n in want)
+        torch.cuda.synchronize()
+        assert layer.d.last_status() == 0
