@@ -66,7 +66,8 @@ typedef struct {
 } director_shape;
 
 /* Life cycle.  director_create allocates the workspace on the current device (besides the two
- * director_reserve_* calls it is the only one that allocates) and binds the context to that device. */
+ * director_reserve_* calls it is the only one that allocates), binds the context to that device and waits for the legacy
+ * default stream: the context is ready for any stream when it returns. */
 int director_create(const director_shape* shape, director_ctx** out);
 int director_destroy(director_ctx* ctx);
 

@@ -153,7 +153,8 @@ int director_create(const director_shape* shape, director_ctx** out) {
     ok = cudaMemset(c->d_ticket, 0, 4 * sizeof(unsigned int)) == cudaSuccess &&
          cudaMemset(c->d_status, 0, sizeof(int32_t)) == cudaSuccess &&
          cudaMemset(c->d_zero_expert, 0, sizeof(int32_t)) == cudaSuccess &&
-         cudaMemset(c->d_gemm_clock, 0, sizeof(unsigned long long) * 2 * kGemmClockWords * kGemmClockCtas) == cudaSuccess;
+         cudaMemset(c->d_gemm_clock, 0, sizeof(unsigned long long) * 2 * kGemmClockWords * kGemmClockCtas) == cudaSuccess &&
+         zeros_written();
 
     cudaDriverEntryPointQueryResult qres;
     if (ok) {

@@ -103,3 +103,24 @@ def test_the_first_training_step_runs_beside_a_busy_default_stream():
         assert all(torch.equal(want[n], got[n]) for n in want)
         torch.cuda.synchronize()
         assert layer.d.last_status() == 0
+
+
+def test_a_context_made_beside_a_busy_default_stream_is_ready():
+    import torch
+    from paper_2607_08782_b200.layer import MoELayer
+    logits, x, dy = _inputs()
+    quiet = _layer(F=4096)
+    want = _train_once(quiet, logits, x, dy)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        _freed_garbage()
+        _busy(torch.cuda.default_stream(), 200)
+        with torch.cuda.stream(side):
+            layer = MoELayer(64, 256, 4096, 8, 2, 1, 4, 3, *quiet.w, *quiet.ws)
+            layer.set_placement(_placement(0))
+            got = _train_once(layer, logits, x, dy)
+            assert layer.d.last_status() == 0
+        side.synchronize()
+        assert all(torch.equal(want[n], got[n]) for n in want)
+        torch.cuda.synchronize()
