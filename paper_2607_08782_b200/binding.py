@@ -169,6 +169,7 @@ class Director:
         self.shape = DirectorShape(T_max, H, F, E, K, S, R, C_max)
         self._ctx = c_void_p()
         _check(self.lib.director_create(ctypes.byref(self.shape), ctypes.byref(self._ctx)), "director_create")
+        self._slot, self._fills = 0, {}
 
     def close(self):
         if getattr(self, "_ctx", None) is not None and self._ctx.value:
@@ -188,6 +189,12 @@ class Director:
         X = np.ascontiguousarray(X, dtype=np.uint8)
         assert X.shape == (self.shape.E, self.shape.R)
         _check(self.lib.director_set_placement(self._ctx, X.ctypes.data, _stream()), "director_set_placement")
+        self._fills[self._slot] = self._fills.get(self._slot, 0) + 1
+
+    def placement_id(self):
+        """Names the current placement's tables: another value once set_placement() has filled the slot anew, or while
+        another slot is selected."""
+        return self._slot, self._fills.get(self._slot, 0)
 
     # -- stages --------------------------------------------------------------------------------
     def route(self, T, logits, topk_idx, topk_w):
@@ -216,6 +223,7 @@ class Director:
 
     def select_placement(self, slot: int):
         _check(self.lib.director_select_placement(self._ctx, slot), "director_select_placement")
+        self._slot = slot
 
     def set_replica_policy(self, policy: int):
         _check(self.lib.director_set_replica_policy(self._ctx, policy), "director_set_replica_policy")

@@ -27,7 +27,7 @@ class MoELayer:
         self.dims = dict(T_max=T_max, H=H, F=F, E=E, K=K, S=S, R=R, C_max=C_max)
         self.d = Director(T_max, H, F, E, K, S, R, C_max)
         self.ffn_variant = 2
-        self.trained = None        # (T, x) of the training forward whose buffers are intact: its backward pass may run
+        self.trained = None        # (T, x, placement) of the training forward whose buffers are intact: its backward pass may run
         self.w = (w_gate, w_up, w_down)
         self.ws = (ws_gate, ws_up, ws_down)
         A, G = T_max * K, R * C_max
@@ -142,15 +142,19 @@ class MoELayer:
         shared = (x, *self.ws, *self.kept_shared, self.y_shared) if self.dims["S"] > 0 else ()
         self.d.expert_ffn_checkpoint(T, self.xp, self.seg_offsets, *self.w, *self.kept, self.yp, *shared)
         self.combine(T)
-        self.trained = (T, x)
+        self.trained = (T, x, self.d.placement_id())
         return self.y[:T]
 
     def backward(self, T, dy):
         """Gradients of the forward_train() before, given dy = dL/dy [T,H] (bf16): a dict of x [T,H], logits [T,E], w_gate, w_up,
-        w_down and, with shared experts, ws_gate, ws_up, ws_down - views of the layer's buffers, overwritten by the next call."""
+        w_down and, with shared experts, ws_gate, ws_up, ws_down - views of the layer's buffers, overwritten by the next call.
+        Under another placement than forward_train()'s, or after another pass of the layer, it raises a RuntimeError."""
         if self.trained is None or self.trained[0] != T:
             raise RuntimeError("backward() needs the buffers of a forward_train() of the same batch size, with no pass of the layer in between")
-        (_, x), self.trained = self.trained, None
+        _, x, placement = self.trained
+        if self.d.placement_id() != placement:            # the rows lie in its segments, and the gradients read its tables
+            raise RuntimeError("backward() needs the placement that forward_train() ran under, which has been changed since")
+        self.trained = None
         g = self.grads
         self.d.combine_backward(T, dy, self.yp, self.inv_row, self.topk_w, self.dyp, self.dtopk_w)
         with_shared = self.dims["S"] > 0

@@ -124,3 +124,49 @@ def test_a_context_made_beside_a_busy_default_stream_is_ready():
         side.synchronize()
         assert all(torch.equal(want[n], got[n]) for n in want)
         torch.cuda.synchronize()
+
+
+# ---- the layer's passes --------------------------------------------------------------------------------------------
+
+
+def test_backward_notices_another_placement():
+    import torch
+    layer = _layer()
+    logits, x, dy = _inputs()
+    layer.forward_train(64, logits, x)
+    want = {n: t.clone() for n, t in layer.backward(64, dy).items()}
+    layer.forward_train(64, logits, x)
+    layer.set_placement(_placement(5))
+    with pytest.raises(RuntimeError, match="placement"):
+        layer.backward(64, dy)
+    layer.set_placement(_placement(0))                    # filled anew: not the tables that the forward pass ran with
+    with pytest.raises(RuntimeError, match="placement"):
+        layer.backward(64, dy)
+    with pytest.raises(Exception):
+        layer.set_placement(np.zeros((8, 4), dtype=np.uint8))       # refused: the placement stays
+    layer.forward_train(64, logits, x)
+    with pytest.raises(Exception):
+        layer.set_placement(np.zeros((8, 4), dtype=np.uint8))
+    got = layer.backward(64, dy)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    layer.d.check_device_status()
+
+
+def test_backward_notices_another_placement_slot():
+    import torch
+    layer = _layer()
+    logits, x, dy = _inputs()
+    layer.d.reserve_placements(2)
+    layer.forward_train(64, logits, x)
+    want = {n: t.clone() for n, t in layer.backward(64, dy).items()}
+    layer.d.select_placement(1)
+    layer.set_placement(_placement(5))
+    layer.d.select_placement(0)
+    layer.forward_train(64, logits, x)
+    layer.d.select_placement(1)
+    with pytest.raises(RuntimeError, match="placement"):
+        layer.backward(64, dy)
+    layer.d.select_placement(0)                           # back at the forward pass's tables
+    got = layer.backward(64, dy)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    layer.d.check_device_status()
