@@ -18,6 +18,15 @@ def tensor_to_bf16_bits(t: torch.Tensor) -> np.ndarray:
     return t.detach().contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
 
 
+class LayerGraph(torch.cuda.CUDAGraph):
+    """A captured pass of a layer.  Its replays write to the layer's buffers, as the pass itself does."""
+    layer = None
+
+    def replay(self):
+        self.layer.trained = None
+        super().replay()
+
+
 class MoELayer:
     """Routed experts w_gate/w_up [E,F,H], w_down [E,H,F]; optional shared experts ws_gate/ws_up [S*F,H],
     ws_down [H,S*F] (all torch.bfloat16 CUDA tensors, kept by reference)."""
@@ -135,7 +144,9 @@ class MoELayer:
 
     def forward_train(self, T, logits, x):
         """The layer's forward pass, keeping what backward() needs (xp, yp, the gate's weights, the 8-bit gate and up values) in the
-        layer's buffers; returns y[:T].  x has to stay as it is until backward()."""
+        layer's buffers; returns y[:T].  x has to stay as it is until backward(), and so have the weights.  Another pass of the layer
+        takes the buffers, and so does a replay of capture()'s graph; replays of a graph that was captured in some other way go
+        unnoticed, and must not come between the two passes."""
         self.enable_training()
         self.route(T, logits)
         self.dispatch(T, x)
@@ -204,7 +215,8 @@ class MoELayer:
         with torch.cuda.stream(side):                      # first pass outside the capture: lazy module loading
             self.forward(T, logits, x, with_cost, fused, fused_combine)
         torch.cuda.current_stream().wait_stream(side)
-        graph = torch.cuda.CUDAGraph()
+        graph = LayerGraph()
+        graph.layer = self
         with torch.cuda.graph(graph):
             self.forward(T, logits, x, with_cost, fused, fused_combine)
         return graph

@@ -170,3 +170,20 @@ def test_backward_notices_another_placement_slot():
     got = layer.backward(64, dy)
     assert all(torch.equal(want[n], got[n]) for n in want)
     layer.d.check_device_status()
+
+
+def test_a_replayed_serving_pass_takes_the_buffers():
+    import torch
+    layer = _layer()
+    logits, x, dy = _inputs()
+    other = _inputs(seed=1)
+    graph = layer.capture(64, other[0], other[1])
+    layer.forward_train(64, logits, x)
+    graph.replay()
+    with pytest.raises(RuntimeError):
+        layer.backward(64, dy)
+    y = layer.y[:64].clone()
+    assert torch.equal(y, layer.forward(64, other[0], other[1])), "the replay is the pass that was captured"
+    layer.forward_train(64, logits, x)
+    layer.backward(64, dy)
+    layer.d.check_device_status()
