@@ -22,18 +22,16 @@ class _Layer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, layer, x, logits, *weights):
         T = x.shape[0]
-        ctx.layer, ctx.step = layer, object()
         y = layer.forward_train(T, logits.contiguous(), x.contiguous()).clone()
-        layer.step = ctx.step
+        ctx.layer, ctx.kept = layer, layer.trained
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         layer = ctx.layer
-        if getattr(layer, "step", None) is not ctx.step:
-            raise RuntimeError("the layer keeps one forward pass: run its backward before its next forward")
-        layer.step = None
+        if layer.trained is not ctx.kept:
+            raise RuntimeError("the layer keeps one forward pass: run its backward before the layer's next pass")
         g = layer.backward(dy.shape[0], dy.contiguous())
         weights = [g[n] for n in _WEIGHTS if n in g]
         return (None, *(t.clone() if need else None for t, need in zip([g["x"], g["logits"], *weights], ctx.needs_input_grad[1:])))

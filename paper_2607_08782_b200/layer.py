@@ -36,7 +36,9 @@ class MoELayer:
         self.dims = dict(T_max=T_max, H=H, F=F, E=E, K=K, S=S, R=R, C_max=C_max)
         self.d = Director(T_max, H, F, E, K, S, R, C_max)
         self.ffn_variant = 2
-        self.trained = None        # (T, x, placement) of the training forward whose buffers are intact: its backward pass may run
+        # (T, x, placement) of the training forward whose buffers are intact, an object of its own for every pass: its backward pass
+        # may run
+        self.trained = None
         self.w = (w_gate, w_up, w_down)
         self.ws = (ws_gate, ws_up, ws_down)
         A, G = T_max * K, R * C_max

@@ -187,3 +187,18 @@ def test_a_replayed_serving_pass_takes_the_buffers():
     layer.forward_train(64, logits, x)
     layer.backward(64, dy)
     layer.d.check_device_status()
+
+
+def test_autograd_notices_a_training_pass_of_the_layer_itself():
+    """The buffers then hold another pass's values, of the same size."""
+    from paper_2607_08782_b200.finetune import moe_layer
+    layer = _layer()
+    logits, x, dy = _inputs()
+    logits.requires_grad_()
+    y = moe_layer(layer, x, logits)
+    other = _inputs(seed=1)
+    layer.forward_train(64, other[0], other[1])
+    with pytest.raises(RuntimeError):
+        y.float().sum().backward()
+    layer.backward(64, dy)                                # which is still there for its own backward pass
+    layer.d.check_device_status()
