@@ -24,11 +24,15 @@ class _Layer(torch.autograd.Function):
         T = x.shape[0]
         y = layer.forward_train(T, logits.contiguous(), x.contiguous()).clone()
         ctx.layer, ctx.kept = layer, layer.trained
+        # what the backward pass reads of the caller's: autograd then notices where it was changed in place (x itself is read by
+        # the shared experts alone, the routed experts' rows are copies)
+        ctx.save_for_backward(*weights, *((x,) if layer.dims["S"] > 0 else ()))
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
+        ctx.saved_tensors                                 # raises if one of them was changed
         layer = ctx.layer
         if layer.trained is not ctx.kept:
             raise RuntimeError("the layer keeps one forward pass: run its backward before the layer's next pass")
@@ -40,7 +44,8 @@ class _Layer(torch.autograd.Function):
 def moe_layer(layer: MoELayer, x: torch.Tensor, logits: torch.Tensor) -> torch.Tensor:
     """y [T,H] of the layer for x [T,H] (bf16) and the router's logits [T,E] (fp32), differentiable in both and in the layer's
     weights (those that require a gradient).  The layer's placement has to be set.  One forward pass at a time is kept: the
-    backward pass of a call has to run before the layer's next call."""
+    backward pass of a call has to run before the layer's next call, and before the weights (with shared experts, x too) are changed
+    in place."""
     if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
         raise TypeError(f"x has to be bf16 and logits fp32, got {x.dtype} and {logits.dtype}")
     T, d = x.shape[0], layer.dims

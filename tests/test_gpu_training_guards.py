@@ -202,3 +202,36 @@ def test_autograd_notices_a_training_pass_of_the_layer_itself():
         y.float().sum().backward()
     layer.backward(64, dy)                                # which is still there for its own backward pass
     layer.d.check_device_status()
+
+
+@pytest.mark.parametrize("what", ["x", "expert", "shared"])
+def test_autograd_notices_what_was_changed_in_place(what):
+    import torch
+    from paper_2607_08782_b200.finetune import moe_layer
+    layer = _layer(S=1)
+    logits, x, _ = _inputs()
+    logits.requires_grad_()
+    for w in layer.w + layer.ws:
+        w.requires_grad_()
+    y = moe_layer(layer, x, logits)
+    with torch.no_grad():
+        {"x": x, "expert": layer.w[1], "shared": layer.ws[2]}[what].mul_(0.5)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.float().sum().backward()
+    moe_layer(layer, x, logits).float().sum().backward()
+    assert logits.grad is not None
+
+
+def test_without_shared_experts_x_may_be_written_to():
+    """The routed experts' rows are copies: a residual connection in place is as good as any other."""
+    import torch
+    from paper_2607_08782_b200.finetune import moe_layer
+    layer = _layer(S=0)
+    logits, x, dy = _inputs()
+    for w in layer.w:
+        w.requires_grad_()
+    want = torch.autograd.grad(moe_layer(layer, x, logits), layer.w, dy)
+    stream = x.clone()
+    y = moe_layer(layer, stream, logits)
+    stream += y.detach()
+    assert all(torch.equal(a, b) for a, b in zip(want, torch.autograd.grad(y, layer.w, dy)))
