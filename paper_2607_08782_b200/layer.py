@@ -155,7 +155,7 @@ class MoELayer:
         shared = (x, *self.ws, *self.kept_shared, self.y_shared) if self.dims["S"] > 0 else ()
         self.d.expert_ffn_checkpoint(T, self.xp, self.seg_offsets, *self.w, *self.kept, self.yp, *shared)
         self.combine(T)
-        self.trained = (T, x, self.d.placement_id())
+        self.trained = (T, x.detach(), self.d.placement_id())     # x without the graph that made it
         return self.y[:T]
 
     def backward(self, T, dy):

@@ -235,3 +235,27 @@ def test_without_shared_experts_x_may_be_written_to():
     y = moe_layer(layer, stream, logits)
     stream += y.detach()
     assert all(torch.equal(a, b) for a, b in zip(want, torch.autograd.grad(y, layer.w, dy)))
+
+
+def test_a_pass_without_a_backward_pass_keeps_no_graph_alive():
+    import gc
+    import weakref
+    import torch
+    from paper_2607_08782_b200.finetune import moe_layer
+
+    class Probe(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, t):
+            return t * 1
+
+        @staticmethod
+        def backward(ctx, g):
+            return g
+    layer = _layer()
+    logits, leaf, _ = _inputs()
+    x = Probe.apply(leaf.requires_grad_())
+    node = weakref.ref(x.grad_fn)
+    y = moe_layer(layer, x, logits)
+    del x, y
+    gc.collect()
+    assert node() is None, "the layer holds on to the graph of its input"
