@@ -5,7 +5,7 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from .binding import Director
+from .binding import Director, _need
 
 
 def bf16_bits_to_tensor(bits: np.ndarray, device="cuda") -> torch.Tensor:
@@ -149,6 +149,7 @@ class MoELayer:
         layer's buffers; returns y[:T].  x has to stay as it is until backward(), and so have the weights.  Another pass of the layer
         takes the buffers, and so does a replay of capture()'s graph; replays of a graph that was captured in some other way go
         unnoticed, and must not come between the two passes."""
+        _need("forward_train", ("logits", logits, torch.float32, T * self.dims["E"]), ("x", x, torch.bfloat16, T * self.dims["H"]))
         self.enable_training()
         self.route(T, logits)
         self.dispatch(T, x)

@@ -259,3 +259,26 @@ def test_a_pass_without_a_backward_pass_keeps_no_graph_alive():
     del x, y
     gc.collect()
     assert node() is None, "the layer holds on to the graph of its input"
+
+
+def test_forward_train_refuses_what_it_would_misread():
+    import torch
+    from paper_2607_08782_b200.finetune import moe_layer
+    layer = _layer()
+    logits, x, dy = _inputs()
+    for bad in (dict(logits=logits.double()), dict(x=x.float()), dict(x=x.half())):
+        with pytest.raises(TypeError):
+            layer.forward_train(64, **{"logits": logits, "x": x, **bad})
+    for bad in (dict(logits=logits[:63]), dict(x=x[:63]), dict(logits=logits.t().contiguous().t()), dict(x=x.t().contiguous().t()),
+                dict(logits=logits.cpu()), dict(x=x.cpu())):
+        with pytest.raises(ValueError):
+            layer.forward_train(64, **{"logits": logits, "x": x, **bad})
+    with pytest.raises(ValueError):
+        moe_layer(layer, x, logits.cpu())
+    with pytest.raises(ValueError):
+        moe_layer(layer, x.cpu(), logits)
+    with pytest.raises(RuntimeError):                     # no pass has run
+        layer.backward(64, dy)
+    layer.forward_train(64, logits, x)
+    layer.backward(64, dy)
+    layer.d.check_device_status()
