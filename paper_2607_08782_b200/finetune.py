@@ -20,9 +20,9 @@ _WEIGHTS = ("w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
 
 class _Layer(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, layer, x, logits, *weights):
+    def forward(ctx, layer, token_src_rank, x, logits, *weights):
         T = x.shape[0]
-        y = layer.forward_train(T, logits.contiguous(), x.contiguous()).clone()
+        y = layer.forward_train(T, logits.contiguous(), x.contiguous(), token_src_rank).clone()
         ctx.layer, ctx.kept = layer, layer.trained
         # what the backward pass reads of the caller's: autograd then notices where it was changed in place (x itself is read by
         # the shared experts alone, the routed experts' rows are copies)
@@ -38,21 +38,21 @@ class _Layer(torch.autograd.Function):
             raise RuntimeError("the layer keeps one forward pass: run its backward before the layer's next pass")
         g = layer.backward(dy.shape[0], dy.contiguous())
         weights = [g[n] for n in _WEIGHTS if n in g]
-        return (None, *(t.clone() if need else None for t, need in zip([g["x"], g["logits"], *weights], ctx.needs_input_grad[1:])))
+        return (None, None, *(t.clone() if need else None for t, need in zip([g["x"], g["logits"], *weights], ctx.needs_input_grad[2:])))
 
 
-def moe_layer(layer: MoELayer, x: torch.Tensor, logits: torch.Tensor) -> torch.Tensor:
+def moe_layer(layer: MoELayer, x: torch.Tensor, logits: torch.Tensor, token_src_rank: torch.Tensor | None = None) -> torch.Tensor:
     """y [T,H] of the layer for x [T,H] (bf16) and the router's logits [T,E] (fp32), differentiable in both and in the layer's
     weights (those that require a gradient).  The layer's placement has to be set.  One forward pass at a time is kept: the
     backward pass of a call has to run before the layer's next call, and before the weights (with shared experts, x too) are changed
-    in place."""
+    in place.  token_src_rank (int32 [T]): the tokens' home ranks, for the locality-first choice of replicas (see MoELayer.dispatch)."""
     if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
         raise TypeError(f"x has to be bf16 and logits fp32, got {x.dtype} and {logits.dtype}")
     T, d = x.shape[0], layer.dims
     if x.shape != (T, d["H"]) or logits.shape != (T, d["E"]) or not 1 <= T <= d["T_max"]:
         raise ValueError(f"x {tuple(x.shape)} and logits {tuple(logits.shape)} do not fit the layer {d}")
     weights = layer.w + (layer.ws if d["S"] > 0 else ())
-    return _Layer.apply(layer, x, logits, *weights)
+    return _Layer.apply(layer, token_src_rank, x, logits, *weights)
 
 
 def make_layer(T, H, F, E, K, S, R, C, X, seed, scale=0.05) -> MoELayer:

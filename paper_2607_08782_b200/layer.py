@@ -144,15 +144,17 @@ class MoELayer:
             grads.update({n: torch.empty_like(w) for n, w in zip(("ws_gate", "ws_up", "ws_down"), self.ws)})
         self.grads = grads
 
-    def forward_train(self, T, logits, x):
+    def forward_train(self, T, logits, x, token_src_rank=None):
         """The layer's forward pass, keeping what backward() needs (xp, yp, the gate's weights, the 8-bit gate and up values) in the
         layer's buffers; returns y[:T].  x has to stay as it is until backward(), and so have the weights.  Another pass of the layer
         takes the buffers, and so does a replay of capture()'s graph; replays of a graph that was captured in some other way go
-        unnoticed, and must not come between the two passes."""
+        unnoticed, and must not come between the two passes.  token_src_rank (int32 [T]): see dispatch()."""
         _need("forward_train", ("logits", logits, torch.float32, T * self.dims["E"]), ("x", x, torch.bfloat16, T * self.dims["H"]))
+        if token_src_rank is not None:
+            _need("forward_train", ("token_src_rank", token_src_rank, torch.int32, T))
         self.enable_training()
         self.route(T, logits)
-        self.dispatch(T, x)
+        self.dispatch(T, x, token_src_rank=token_src_rank)
         shared = (x, *self.ws, *self.kept_shared, self.y_shared) if self.dims["S"] > 0 else ()
         self.d.expert_ffn_checkpoint(T, self.xp, self.seg_offsets, *self.w, *self.kept, self.yp, *shared)
         self.combine(T)

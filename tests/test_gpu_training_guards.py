@@ -282,3 +282,36 @@ def test_forward_train_refuses_what_it_would_misread():
     layer.forward_train(64, logits, x)
     layer.backward(64, dy)
     layer.d.check_device_status()
+
+
+def test_training_under_locality_first_takes_the_tokens_home_ranks():
+    """Which replica serves a token plays no part in what is learnt: a token's own gradients have the same bits, the weights' sums
+    come in another order (two roundings to bf16 of fp32 sums)."""
+    import torch
+    from paper_2607_08782_b200.finetune import moe_layer
+    layer = _layer()
+    layer.set_replica_policy(1)
+    logits, x, dy = _inputs()
+    layer.forward_train(64, logits, x)
+    seg = layer.seg_offsets.clone()
+    want = {n: t.clone() for n, t in layer.backward(64, dy).items()}
+    home = (3 - torch.arange(64, device="cuda") // 16).int()
+    layer.forward_train(64, logits, x, token_src_rank=home)
+    tables = [t.clone() for t in (layer.dest_rank, layer.inv_row, layer.seg_offsets)]
+    got = {n: t.clone() for n, t in layer.backward(64, dy).items()}
+    assert not torch.equal(seg, tables[2]), "the home ranks count"
+    layer.dispatch(64, x, token_src_rank=home)
+    assert all(torch.equal(a, b) for a, b in zip(tables, (layer.dest_rank, layer.inv_row, layer.seg_offsets)))
+    for n in want:
+        if n in ("x", "logits"):
+            assert torch.equal(want[n], got[n]), n
+        else:
+            assert (got[n].double() - want[n].double()).norm() <= 2.0 ** -7 * want[n].double().norm(), n
+    logits.requires_grad_()
+    y = moe_layer(layer, x, logits, home)
+    assert torch.equal(torch.autograd.grad(y, logits, dy)[0], got["logits"])
+    with pytest.raises(TypeError):
+        layer.forward_train(64, logits.detach(), x, token_src_rank=home.long())
+    with pytest.raises(ValueError):
+        layer.forward_train(64, logits.detach(), x, token_src_rank=home[:63])
+    layer.d.check_device_status()
