@@ -821,7 +821,10 @@ int launch_expert_ffn_backward(director_ctx* ctx, const int32_t* seg_offsets, co
     if (rc != DIRECTOR_OK) return rc;
     p.counter = ctx->d_grad_sched + 1;
     p.other_counter = ctx->d_grad_sched;
-    return launch_grad<1>(ctx, "grouped_grad_weights_kernel", maps, p, st);
+    const int rc2 = launch_grad<1>(ctx, "grouped_grad_weights_kernel", maps, p, st);
+    // it would have cleared the first launch's counter, at whose end the next call would find its items claimed
+    if (rc2 != DIRECTOR_OK) cudaMemsetAsync(ctx->d_grad_sched, 0, 2 * sizeof(unsigned int), st);
+    return rc2;
 }
 
 }  // namespace director
