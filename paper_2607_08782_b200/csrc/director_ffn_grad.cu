@@ -62,7 +62,7 @@ constexpr int grad_epi_warps(int phase) { return phase == 0 ? 12 : 8; }
 constexpr int grad_threads(int phase) { return 128 + 32 * grad_epi_warps(phase); }   // producer, MMA, scheduler and tail warps + epilogue
 constexpr int G_TILE = 256;                            // most tokens per tile; accumulators are this many columns apart
 constexpr int G_SLOTS = 4;                             // ring of work items
-constexpr int G_PACED_STEPS = 128;                     // contractions this long are paced
+constexpr int G_PACED_STEPS = 256;                     // contractions this long are paced
 constexpr int G_CLAIM_LEAD = 32;                       // k-steps of claimed work ahead of the producer
 
 constexpr int G_OUT_BYTES = 32 * 64;                   // per epilogue warp: 32 rows x 32 bf16 columns of a weight gradient
@@ -458,10 +458,10 @@ grouped_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                 } else {
                     const int k_steps = token_steps(it.e);
                     // The ragged end of a segment in a long contraction is held to a full tile's speed, as in the forward's down
-                    // projection: pairs that run ahead stop meeting their neighbours' operands in L2.  F = 14336, H = 4096 (448
-                    // steps): DRAM reads of the launch 2.74 -> 1.90 GB on four experts, a call 4.89 -> 4.75 ms on eight; no
-                    // difference at 252 steps (F = 8064) or at 44 and 128 (F = 1408, 4096).  Not where a segment has no full tile:
-                    // few rows per expert stream weights and lose by waiting.
+                    // projection: pairs that run ahead stop meeting their neighbours' operands in L2.  A call on 4096 tokens, eight
+                    // experts top-2, H = 4096, without and with: F = 4096 (128 steps) 1399 and 1402 us, 6144 2090 and 2098, 8192 (256)
+                    // 2793 and 2768, 12288 4205 and 4138, 14336 4927 and 4829; 8192 tokens, F = 14336: 9721 and 9208.  Not where a
+                    // segment has no full tile: few rows per expert stream weights and lose by waiting.
                     const bool paced = PHASE == 1 && k_steps >= G_PACED_STEPS && it.later && it.valid < G_TILE && hd.tile == G_TILE;
                     const uint32_t c_pace = (uint32_t)clock();
                     for (int kb = 0; kb < k_steps; ++kb) {

@@ -38,3 +38,17 @@ def test_ffn_backward_with_full_tiles(H, F, S, tiles):
     first = [t.clone() for t in f.outputs()]
     f.backward()
     assert all(_same_bits(a, b) for a, b in zip(first, f.outputs()))
+
+
+def test_ffn_backward_with_paced_segment_ends():
+    """A contraction of 256 steps (F = 8192), segments with a ragged end behind full tiles."""
+    lengths = [2800, 700, 1100, 1]
+    assert _tile(lengths, 1024 // 256) == 256
+    f = FfnGradient(5, lengths, np.ones((4, 1), dtype=np.uint8), 4, 1024, 8192, scale=0.02)
+    f.d.reserve_training()
+    f.backward()
+    assert f.d.last_status() == 0
+    _check_backward(f)
+    first = [t.clone() for t in f.outputs()]
+    f.backward()
+    assert all(_same_bits(a, b) for a, b in zip(first, f.outputs()))
