@@ -23,18 +23,18 @@ class _Layer(torch.autograd.Function):
     def forward(ctx, layer, token_src_rank, x, logits, *weights):
         T = x.shape[0]
         y = layer.forward_train(T, logits.contiguous(), x.contiguous(), token_src_rank).clone()
-        ctx.layer, ctx.kept = layer, layer.trained
-        # what the backward pass reads of the caller's: autograd then notices where it was changed in place (x itself is read by
-        # the shared experts alone, the routed experts' rows are copies)
-        ctx.save_for_backward(*weights, *((x,) if layer.dims["S"] > 0 else ()))
+        ctx.layer = layer
+        # What the backward pass reads of the caller's: autograd then notices where it was changed in place (x itself is read by
+        # the shared experts alone, the routed experts' rows are copies).  The pass's number goes the same way, so that under
+        # activation checkpointing it comes back as that of the pass that was run again.
+        ctx.save_for_backward(torch.tensor(layer.passes, device="cpu"), *weights, *((x,) if layer.dims["S"] > 0 else ()))
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        ctx.saved_tensors                                 # raises if one of them was changed
-        layer = ctx.layer
-        if layer.trained is not ctx.kept:
+        kept, layer = int(ctx.saved_tensors[0]), ctx.layer         # the first access raises if a tensor was changed
+        if layer.trained is None or layer.trained[3] != kept:
             raise RuntimeError("the layer keeps one forward pass: run its backward before the layer's next pass")
         g = layer.backward(dy.shape[0], dy.contiguous())
         weights = [g[n] for n in _WEIGHTS if n in g]
@@ -44,7 +44,8 @@ class _Layer(torch.autograd.Function):
 def moe_layer(layer: MoELayer, x: torch.Tensor, logits: torch.Tensor, token_src_rank: torch.Tensor | None = None) -> torch.Tensor:
     """y [T,H] of the layer for x [T,H] (bf16) and the router's logits [T,E] (fp32), differentiable in both and in the layer's
     weights (those that require a gradient).  The layer's placement has to be set.  One forward pass at a time is kept: the
-    backward pass of a call has to run before the layer's next call, and before the weights (with shared experts, x too) are changed
+    backward pass of a call has to run before the layer's next call (torch.utils.checkpoint lifts this: it runs the call again
+    when its backward pass comes), and before the weights (with shared experts, x too) are changed
     in place.  token_src_rank (int32 [T]): the tokens' home ranks, for the locality-first choice of replicas (see MoELayer.dispatch)."""
     if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
         raise TypeError(f"x has to be bf16 and logits fp32, got {x.dtype} and {logits.dtype}")

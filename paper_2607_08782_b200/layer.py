@@ -36,9 +36,10 @@ class MoELayer:
         self.dims = dict(T_max=T_max, H=H, F=F, E=E, K=K, S=S, R=R, C_max=C_max)
         self.d = Director(T_max, H, F, E, K, S, R, C_max)
         self.ffn_variant = 2
-        # (T, x, placement) of the training forward whose buffers are intact, an object of its own for every pass: its backward pass
-        # may run
+        # (T, x, placement, pass) of the training forward whose buffers are intact: its backward pass may run.  No two passes of
+        # the layer have the same number.
         self.trained = None
+        self.passes = 0
         self.w = (w_gate, w_up, w_down)
         self.ws = (ws_gate, ws_up, ws_down)
         A, G = T_max * K, R * C_max
@@ -158,7 +159,8 @@ class MoELayer:
         shared = (x, *self.ws, *self.kept_shared, self.y_shared) if self.dims["S"] > 0 else ()
         self.d.expert_ffn_checkpoint(T, self.xp, self.seg_offsets, *self.w, *self.kept, self.yp, *shared)
         self.combine(T)
-        self.trained = (T, x.detach(), self.d.placement_id())     # x without the graph that made it
+        self.passes += 1
+        self.trained = (T, x.detach(), self.d.placement_id(), self.passes)     # x without the graph that made it
         return self.y[:T]
 
     def backward(self, T, dy):
@@ -167,7 +169,7 @@ class MoELayer:
         Under another placement than forward_train()'s, or after another pass of the layer, it raises a RuntimeError."""
         if self.trained is None or self.trained[0] != T:
             raise RuntimeError("backward() needs the buffers of a forward_train() of the same batch size, with no pass of the layer in between")
-        _, x, placement = self.trained
+        _, x, placement, _ = self.trained
         if self.d.placement_id() != placement:            # the rows lie in its segments, and the gradients read its tables
             raise RuntimeError("backward() needs the placement that forward_train() ran under, which has been changed since")
         self.trained = None

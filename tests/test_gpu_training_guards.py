@@ -315,3 +315,36 @@ def test_training_under_locality_first_takes_the_tokens_home_ranks():
     with pytest.raises(ValueError):
         layer.forward_train(64, logits.detach(), x, token_src_rank=home[:63])
     layer.d.check_device_status()
+
+
+def test_under_activation_checkpointing_calls_may_overlap():
+    """The forward pass runs again before the backward pass needs its buffers, inside a block of other operations or alone."""
+    import torch
+    from torch.utils.checkpoint import checkpoint
+    from paper_2607_08782_b200.finetune import moe_layer
+    layer = _layer()
+    for w in layer.w + layer.ws:
+        w.requires_grad_()
+
+    def alone(x, logits):
+        return moe_layer(layer, x, logits)
+
+    def block(x, logits):
+        return x + torch.tanh(moe_layer(layer, torch.sin(x), logits * 2))
+    batches = [_inputs(seed=k) for k in range(3)]
+    for fn in (alone, block):
+        want, got = [], []
+        for logits, x, dy in batches:
+            leaves = [x.clone().requires_grad_(), logits.clone().requires_grad_()]
+            want.append(torch.autograd.grad(fn(*leaves), [*leaves, *layer.w, *layer.ws], dy))
+        for reentrant in (False, True):
+            leaves = [[x.clone().requires_grad_(), logits.clone().requires_grad_()] for logits, x, _ in batches]
+            ys = [checkpoint(fn, *lv, use_reentrant=reentrant) for lv in leaves]
+            if reentrant:                                 # which hands gradients to .grad alone
+                for (_, _, dy), y in zip(batches, ys):
+                    y.backward(dy)
+                assert all(torch.equal(a.grad, b) for lv, w in zip(leaves, want) for a, b in zip(lv, w))
+            else:
+                for (_, _, dy), y, lv, w in zip(batches, ys, leaves, want):
+                    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, [*lv, *layer.w, *layer.ws], dy), w))
+    layer.d.check_device_status()
