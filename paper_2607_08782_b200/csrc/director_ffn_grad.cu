@@ -31,8 +31,8 @@
 // Every wait is bounded; an expired one raises DIRECTOR_ERR_TIMEOUT.
 //
 // What bounds it: long segments, the tensor pipe - a 64-deep step takes 508-520 cycles, the pipe's four MMAs 512 - at the clock the
-// power cap leaves (8192 rows, eight experts, H = 4096, F = 14336: 0.73-0.85 and 3.65-3.95 ms for the two launches, 1.2-1.3
-// PFLOP/s); few rows per expert, HBM (8168 rows, 128 experts, H = 2048, F = 768: 77 and 307 us, 5.3 TB/s of weights read and
+// power cap leaves (8192 rows, eight experts, H = 4096, F = 14336: 0.73-0.85 and 3.65-4.0 ms for the two launches, 1.2-1.3
+// PFLOP/s); few rows per expert, HBM (8168 rows, 128 experts, H = 2048, F = 768: 77-80 and 307 us, 5.3 TB/s of weights read and
 // gradients written); a handful of rows, the launches' own latencies (8 us each).
 #include "director_common.cuh"
 #include "director_umma.cuh"

@@ -70,8 +70,8 @@ constexpr int TOKEN_STEP = 32;                                 // granularity of
 // and store; one warp per quadrant with a large register budget (all 32 stores of a chunk in flight) is faster.
 constexpr int EPI_GROUPS_GEMM1 = 2;
 constexpr int EPI_GROUPS_GEMM2 = 1;
-// With the 8-bit values to write as well, three (8192 tokens, 64 experts top-6, F = 1408: H = 512 300 -> 278 us, H = 1024 374 -> 354,
-// H = 2048 566 -> 556).
+// With the 8-bit values to write as well, three (8192 tokens, 64 experts top-6 and two shared, F = 1408: H = 512 300 -> 278 us,
+// H = 1024 374 -> 354, H = 2048 566 -> 556; below H = 1600 or so the epilogue is still the longer side, at H = 512 twice the products).
 constexpr int EPI_GROUPS_CHECKPOINT = 3;
 
 // kind::f16 descriptor for the pair without the N field: D=f32, A=B=bf16, K-major, M=256.

@@ -22,7 +22,7 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 //
 // One warp per assignment (t, s): it reads dy[t] and the row of yp once, writes the row of dyp, and the dot product is a sum
 // over its lanes - no atomics, so dw has the same bits on every run.  The K warps of a token sit next to each other in a CTA,
-// so that dy[t] comes from HBM once and from L1 or L2 after that.  T = 32768, H = 2048, K = 8: 360 us, 6.3 TB/s.  Tried there: CTAs
+// so that dy[t] comes from HBM once and from L1 or L2 after that.  T = 32768, H = 2048, K = 8: 352-358 us, 6.4-6.5 TB/s.  Tried there: CTAs
 // of 8 warps + 1 %, 16 + 4 %; rows of yp loaded as streaming (evict first) + 4 %, dyp stored so + 11 %; four pieces of a row per
 // lane asked for together + 4 % (registers cost occupancy), and no faster for a small batch, whose call is launch-bound.
 constexpr int kRowWarps = 4;

@@ -43,7 +43,8 @@ class _Layer(torch.autograd.Function):
 
 def moe_layer(layer: MoELayer, x: torch.Tensor, logits: torch.Tensor, token_src_rank: torch.Tensor | None = None) -> torch.Tensor:
     """y [T,H] of the layer for x [T,H] (bf16) and the router's logits [T,E] (fp32), differentiable in both and in the layer's
-    weights (those that require a gradient).  The layer's placement has to be set.  One forward pass at a time is kept: the
+    weights (those that require a gradient).  Between the passes the experts' gate and up values are kept in 8 bits, which moves the
+    gradients by under 1 %; the weights' come out in bf16.  The layer's placement has to be set.  One forward pass at a time is kept: the
     backward pass of a call has to run before the layer's next call (torch.utils.checkpoint lifts this: it runs the call again
     when its backward pass comes), and before the weights (with shared experts, x too) are changed
     in place.  token_src_rank (int32 [T]): the tokens' home ranks, for the locality-first choice of replicas (see MoELayer.dispatch)."""
