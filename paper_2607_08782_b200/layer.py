@@ -172,6 +172,7 @@ class MoELayer:
         _, x, placement, _ = self.trained
         if self.d.placement_id() != placement:            # the rows lie in its segments, and the gradients read its tables
             raise RuntimeError("backward() needs the placement that forward_train() ran under, which has been changed since")
+        _need("backward", ("dy", dy, torch.bfloat16, T * self.dims["H"]))
         self.trained = None
         g = self.grads
         self.d.combine_backward(T, dy, self.yp, self.inv_row, self.topk_w, self.dyp, self.dtopk_w)

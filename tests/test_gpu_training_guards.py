@@ -348,3 +348,17 @@ def test_under_activation_checkpointing_calls_may_overlap():
                 for (_, _, dy), y, lv, w in zip(batches, ys, leaves, want):
                     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, [*lv, *layer.w, *layer.ws], dy), w))
     layer.d.check_device_status()
+
+
+def test_a_refused_dy_leaves_the_pass_as_it_is():
+    import torch
+    layer = _layer()
+    logits, x, dy = _inputs()
+    want = _train_once(layer, logits, x, dy)
+    layer.forward_train(64, logits, x)
+    for bad, error in ((dy.float(), TypeError), (dy[:63], ValueError), (dy.t(), ValueError), (dy.cpu(), ValueError)):
+        with pytest.raises(error):
+            layer.backward(64, bad)
+    got = layer.backward(64, dy)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    layer.d.check_device_status()
