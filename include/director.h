@@ -282,6 +282,77 @@ int director_expert_ffn_backward(director_ctx* ctx, int32_t T, const void* xp, c
                                  const void* ws_down, void* dx_shared, void* dws_gate, void* dws_up, void* dws_down,
                                  void* stream);
 
+/* ---- What a training step needs besides the gradients ---- */
+
+/* The router's balance term (the paper spreads load by placement; a router in training spreads it by this loss).  Over the N tokens
+ * that token_mask leaves, with p_t = softmax(logits_t) over all E experts:
+ *   counts[e] = their assignments to e,  f_e = counts[e] / (K N),  P_e = sum_t p_te / N,   loss = E sum_e f_e P_e   (1 if even).
+ * logits: dev fp32 [T,E].  topk_idx: dev int32 [T,K], as director_route gives them.  token_mask: dev uint8 [T], 0 for a token that
+ * does not count (padding), or NULL.  loss: dev fp32 [1].  counts: dev int64 [E+1], the last entry is N.  N = 0: loss 0.
+ * A masked token's logits and indices are not looked at.  An index outside [0,E) is skipped and reported as
+ * DIRECTOR_ERR_BAD_INDEX.  A logit of -inf scores 0; a row with a NaN, a +inf or nothing but -inf adds no scores (its assignments
+ * and the token itself count) and is reported as DIRECTOR_ERR_NONFINITE.  The results have the same bits on every run. */
+int director_balance_loss(director_ctx* ctx, int32_t T, const float* logits, const int32_t* topk_idx, const uint8_t* token_mask,
+                          float* loss, int64_t* counts, void* stream);
+
+/* Its gradient, with the counts held fixed (they are piecewise constant):
+ *   dlogits[t,e] = added[t,e] + dloss E/N p_te (f_e - sum_j f_j p_tj),   added[t,e] alone where token_mask is 0 or the row is
+ * one that director_balance_loss reports.  counts: dev int64 [E+1], as director_balance_loss writes them (or their sums over
+ * several batches, which makes dlogits the gradient of the loss over all of them).  dloss: dev fp32 [1].  added: dev fp32 [T,E], the logits'
+ * gradient so far (director_route_backward's), or NULL for zeros; it may be dlogits itself.  dlogits: dev fp32 [T,E], written whole,
+ * apart from the logits. */
+int director_balance_loss_backward(director_ctx* ctx, int32_t T, const float* logits, const int64_t* counts,
+                                   const uint8_t* token_mask, const float* dloss, const float* added, float* dlogits,
+                                   void* stream);
+
+/* Norm, clipping and update of the gradients of a whole model: no context, any number of tensors, each contiguous, of any length
+ * (0 too) and at any address that is a multiple of its element's size.  The tables of tensors are host memory and may be reused when
+ * the call returns.  workspace: dev, director_grad_workspace_bytes() bytes, 16-byte aligned, contents irrelevant; calls that may
+ * overlap on the GPU need one each.  The results have the same bits on every run on the same kind of GPU.
+ * Errors: DIRECTOR_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, negative lengths, tensors that are written
+ * and overlap another of the call; DIRECTOR_ERR_UNSUPPORTED for more than 2^40 elements in a tensor. */
+enum { DIRECTOR_FP32 = 0, DIRECTOR_BF16 = 1 };
+typedef struct {
+    void* data;          /* dev */
+    int64_t numel;
+    int32_t type;        /* DIRECTOR_FP32 or DIRECTOR_BF16 */
+    int32_t reserved;    /* 0 */
+} director_tensor;
+int64_t director_grad_workspace_bytes(void);
+
+/* norm = sqrt of the sum of squares over all elements of all tensors.  norm: dev fp32 [1].  Squares that leave fp32's range
+ * do not harm it; an infinity or a NaN among the elements does. */
+int director_grad_norm(int32_t n, const director_tensor* grads, float* norm, void* workspace, void* stream);
+
+/* out[i] = grads[i] * min(1, max_norm / norm), norm as above.  out: n tensors of the same lengths, fp32 or bf16 each, or NULL for
+ * the gradients themselves; out[i] may be grads[i] itself (same address and type).  max_norm > 0, infinity allowed (no clipping).
+ * Where norm is infinite or NaN nothing is scaled.  norm: dev fp32 [1], of the gradients before clipping. */
+int director_clip_grads(int32_t n, const director_tensor* grads, const director_tensor* out, float max_norm, float* norm,
+                        void* workspace, void* stream);
+
+/* One step of AdamW (Adam where weight_decay is 0) on the gradients g' = g * min(1, max_norm / norm), t = *steps + 1:
+ *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
+ *   w = w - lr weight_decay w - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
+ * in fp32.  A bf16 weight has an fp32 master, which is what w is above, and becomes the master rounded; an fp32 weight has none
+ * (master NULL).  grads: n tensors as long as the weights; one with data NULL and numel 0 leaves its weight and moments as they are.
+ * params: host.  lr: dev fp32 [1] that takes the place of h->lr (for captured steps), or NULL.  steps: dev int64 [1], the steps done
+ * so far, advanced by one.  norm: dev fp32 [1] or NULL.
+ * Where max_norm is finite or norm is not NULL the norm is taken, and where it is infinite or NaN the step is skipped: nothing
+ * changes, steps neither, and device_status (dev int32 [1] or NULL) receives DIRECTOR_ERR_NONFINITE if it was 0.
+ * 0 <= beta1, beta2 < 1, eps >= 0, max_norm > 0 (infinity: no clipping); lr and weight_decay finite. */
+typedef struct {
+    void* weight;                              /* dev bf16 or fp32 [numel] */
+    float *master, *exp_avg, *exp_avg_sq;      /* dev fp32 [numel] */
+    int64_t numel;
+    int32_t type;                              /* of the weight */
+    int32_t reserved;                          /* 0 */
+} director_param;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, max_norm;
+} director_adamw;
+int director_adamw_step(int32_t n, const director_tensor* grads, const director_param* params, const director_adamw* h,
+                        const float* lr, int64_t* steps, float* norm, int32_t* device_status, void* workspace, void* stream);
+
 /* (a5) Placement cost (Section VI-A): workload matrix W, per-rank load of Eq. 1 and dispatch
  * volume of Eq. 3 for the current placement, counted per executed assignment.
  * topk_idx: dev int32 [T,K].  token_src_rank: dev int32 [T] home rank of each token, or NULL for

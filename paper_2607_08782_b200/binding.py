@@ -30,7 +30,8 @@ EXPORTED = (
     "director_selftest_bounded_wait", "director_gemm_sm_mhz", "director_gemm_counters",
     "director_combine_backward", "director_dispatch_backward", "director_route_backward",
     "director_expert_ffn_checkpoint", "director_checkpoint_decode", "director_reserve_training",
-    "director_expert_ffn_backward",
+    "director_expert_ffn_backward", "director_balance_loss", "director_balance_loss_backward", "director_grad_workspace_bytes",
+    "director_grad_norm", "director_clip_grads", "director_adamw_step",
 )
 
 REPLICA_ROUND_ROBIN, REPLICA_LOCAL_FIRST = 0, 1
@@ -38,6 +39,22 @@ REPLICA_ROUND_ROBIN, REPLICA_LOCAL_FIRST = 0, 1
 
 class DirectorShape(ctypes.Structure):
     _fields_ = [(n, c_int32) for n in ("T_max", "H", "F", "E", "K", "S", "R", "C_max")]
+
+
+class DirectorTensor(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("numel", c_int64), ("type", c_int32), ("reserved", c_int32)]
+
+
+class DirectorParam(ctypes.Structure):
+    _fields_ = [("weight", c_void_p), ("master", c_void_p), ("exp_avg", c_void_p), ("exp_avg_sq", c_void_p), ("numel", c_int64),
+                ("type", c_int32), ("reserved", c_int32)]
+
+
+class DirectorAdamW(ctypes.Structure):
+    _fields_ = [(n, c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")]
+
+
+FP32, BF16 = 0, 1
 
 
 class DirectorError(RuntimeError):
@@ -98,6 +115,12 @@ def load_library(rebuild_if_stale: bool = True) -> ctypes.CDLL:
     lib.director_reserve_training.argtypes = [vp]
     lib.director_expert_ffn_backward.argtypes = [vp, c_int32] + [vp] * 24
     lib.director_checkpoint_decode.argtypes = [vp, c_int32, c_int32] + [vp] * 5
+    lib.director_balance_loss.argtypes = [vp, c_int32] + [vp] * 6
+    lib.director_balance_loss_backward.argtypes = [vp, c_int32] + [vp] * 7
+    lib.director_grad_workspace_bytes.argtypes = []
+    lib.director_grad_norm.argtypes = [c_int32] + [vp] * 4
+    lib.director_clip_grads.argtypes = [c_int32, vp, vp, c_float, vp, vp, vp]
+    lib.director_adamw_step.argtypes = [c_int32] + [vp] * 9
     lib.director_kernel_time.argtypes = [vp, c_char_p, POINTER(c_int64)]
     lib.director_kernel_time.restype = c_double
     lib.director_status_string.argtypes = [c_int]
@@ -105,6 +128,7 @@ def load_library(rebuild_if_stale: bool = True) -> ctypes.CDLL:
     for name in EXPORTED:
         if name not in ("director_launch_count", "director_kernel_time", "director_status_string", "director_gemm_sm_mhz"):
             getattr(lib, name).restype = c_int
+    lib.director_grad_workspace_bytes.restype = c_int64
     _lib = lib
     return lib
 
@@ -119,13 +143,14 @@ def _ptr(t):
 
 
 # torch's dtypes and its raw-stream query, looked up once by the first context (torch is imported no earlier than that)
-_BF16 = _F32 = _I32 = _I8 = _U8 = _raw_stream = _current_device = None
+_BF16 = _F32 = _I32 = _I64 = _I8 = _U8 = _BOOL = _raw_stream = _current_device = None
 
 
 def _bind_torch():
-    global _BF16, _F32, _I32, _I8, _U8, _raw_stream, _current_device
+    global _BF16, _F32, _I32, _I64, _I8, _U8, _BOOL, _raw_stream, _current_device
     import torch
-    _BF16, _F32, _I32, _I8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
+    _BF16, _F32, _I32, _I64, _I8, _U8, _BOOL = (torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.int8, torch.uint8,
+                                                torch.bool)
     _current_device = torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -143,6 +168,13 @@ def _need(where: str, *tensors):
             raise ValueError(f"{where}: {name} has {t.numel()} elements, {numel} are needed")
         addresses.append(t.data_ptr())
     return addresses
+
+
+def _mask(where: str, mask, T: int):
+    """Address of a token mask (uint8 or bool [T], a byte each), None for none."""
+    if mask is None:
+        return None
+    return _need(where, ("token_mask", mask, _BOOL if mask.dtype is _BOOL else _U8, T))[0]
 
 
 def _stream():
@@ -279,6 +311,26 @@ class Director:
         args = _need("route_backward", ("topk_idx", topk_idx, _I32, TK), ("topk_w", topk_w, _F32, TK), ("dtopk_w", dtopk_w, _F32, TK),
                      ("dlogits", dlogits, _F32, T * self.shape.E))
         _check(self.lib.director_route_backward(self._ctx, T, *args, _stream()), "director_route_backward")
+
+    # -- the router's balance term ---------------------------------------------------------------
+    def balance_loss(self, T, logits, topk_idx, token_mask, loss, counts):
+        """loss (fp32 [1]) and counts (int64 [E+1], the last entry the number of valid tokens) of a batch; token_mask: uint8 or
+        bool [T], or None."""
+        s = self.shape
+        logits, topk_idx, loss, counts = _need("balance_loss", ("logits", logits, _F32, T * s.E), ("topk_idx", topk_idx, _I32, T * s.K),
+                                               ("loss", loss, _F32, 1), ("counts", counts, _I64, s.E + 1))
+        _check(self.lib.director_balance_loss(self._ctx, T, logits, topk_idx, _mask("balance_loss", token_mask, T), loss, counts, _stream()),
+               "director_balance_loss")
+
+    def balance_loss_backward(self, T, logits, counts, token_mask, dloss, added, dlogits):
+        """dlogits = added (fp32 [T,E], may be dlogits itself, or None) + the balance term's gradient for dloss (fp32 [1])."""
+        TE = T * self.shape.E
+        logits, counts, dloss, dlogits = _need("balance_loss_backward", ("logits", logits, _F32, TE), ("counts", counts, _I64, self.shape.E + 1),
+                                               ("dloss", dloss, _F32, 1), ("dlogits", dlogits, _F32, TE))
+        if added is not None:
+            added, = _need("balance_loss_backward", ("added", added, _F32, TE))
+        _check(self.lib.director_balance_loss_backward(self._ctx, T, logits, counts, _mask("balance_loss_backward", token_mask, T), dloss,
+                                                       added, dlogits, _stream()), "director_balance_loss_backward")
 
     def expert_ffn_checkpoint(self, T, xp, seg_offsets, w_gate, w_up, w_down, codes, exps, yp, x=None, ws_gate=None,
                               ws_up=None, ws_down=None, codes_shared=None, exps_shared=None, y_shared=None):

@@ -47,7 +47,8 @@ void free_all(director_ctx* c) {
                     c->d_status, c->d_hidden, c->d_hidden_shared, c->d_one_seg, c->d_sched, c->d_gemm_clock,
                     c->d_zero_expert, c->e_logits2[0], c->e_logits2[1], c->e_x2[0], c->e_x2[1], c->e_topk_idx,
                     c->e_topk_w, c->e_xp, c->e_yp, c->e_y2[0], c->e_y2[1], c->e_y_shared, c->e_row_token, c->e_inv_row,
-                    c->e_dest_rank, c->e_cost2[0], c->e_cost2[1], c->d_dgu, c->d_dgu_shared, c->d_grad_sched};
+                    c->e_dest_rank, c->e_cost2[0], c->e_cost2[1], c->d_dgu, c->d_dgu_shared, c->d_grad_sched,
+                    c->d_balance};
     for (void* p : ptrs)
         if (p) cudaFree(p);
     for (int i = 0; i < 2; ++i) {
@@ -128,7 +129,7 @@ int director_create(const director_shape* shape, director_ctx** out) {
               dev_alloc(&c->d_seg_offsets, c->G + 1) && dev_alloc(&c->d_ticket, 4) && dev_alloc(&c->d_status, 1) &&
               dev_alloc(&c->d_host_mask, s.E) && dev_alloc(&c->d_tile_rep, (size_t)c->n_tiles_max * c->G) &&
               dev_alloc(&c->d_one_seg, 2) && dev_alloc(&c->d_sched, 4) &&
-              dev_alloc(&c->d_zero_expert, 1) &&
+              dev_alloc(&c->d_zero_expert, 1) && dev_alloc(reinterpret_cast<uint8_t**>(&c->d_balance), balance_workspace_bytes()) &&
               dev_alloc(&c->d_gemm_clock, 2 * (size_t)kGemmClockWords * kGemmClockCtas) &&
               dev_alloc(reinterpret_cast<uint16_t**>(&c->d_hidden), A * s.F) &&
               dev_alloc(reinterpret_cast<uint16_t**>(&c->d_hidden_shared), T * s.S * s.F) &&
@@ -152,6 +153,7 @@ int director_create(const director_shape* shape, director_ctx** out) {
     c->bank.push_back({c->d_rep_start, c->d_rep_slot, c->d_slot_expert, c->d_host_mask, 0, false});
     ok = cudaMemset(c->d_ticket, 0, 4 * sizeof(unsigned int)) == cudaSuccess &&
          cudaMemset(c->d_status, 0, sizeof(int32_t)) == cudaSuccess &&
+         cudaMemset(c->d_balance, 0, balance_workspace_bytes()) == cudaSuccess &&
          cudaMemset(c->d_zero_expert, 0, sizeof(int32_t)) == cudaSuccess &&
          cudaMemset(c->d_gemm_clock, 0, sizeof(unsigned long long) * 2 * kGemmClockWords * kGemmClockCtas) == cudaSuccess &&
          zeros_written();
@@ -493,6 +495,35 @@ int director_route_backward(director_ctx* ctx, int32_t T, const int32_t* topk_id
     REQUIRE_PTR(dtopk_w);
     REQUIRE_PTR(dlogits);
     return launch_route_backward(ctx, T, topk_idx, topk_w, dtopk_w, dlogits, as_stream(stream));
+}
+
+int director_balance_loss(director_ctx* ctx, int32_t T, const float* logits, const int32_t* topk_idx, const uint8_t* token_mask,
+                          float* loss, int64_t* counts, void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PTR(logits);
+    REQUIRE_PTR(topk_idx);
+    if (loss == nullptr || (reinterpret_cast<uintptr_t>(loss) & 3u)) return DIRECTOR_ERR_INVALID_ARG;
+    if (counts == nullptr || (reinterpret_cast<uintptr_t>(counts) & 7u)) return DIRECTOR_ERR_INVALID_ARG;
+    return launch_balance_loss(ctx, T, logits, topk_idx, token_mask, loss, counts, as_stream(stream));
+}
+
+int director_balance_loss_backward(director_ctx* ctx, int32_t T, const float* logits, const int64_t* counts,
+                                   const uint8_t* token_mask, const float* dloss, const float* added, float* dlogits,
+                                   void* stream) {
+    REQUIRE_CTX(ctx);
+    REQUIRE_T(ctx, T);
+    REQUIRE_PTR(logits);
+    if (counts == nullptr || (reinterpret_cast<uintptr_t>(counts) & 7u)) return DIRECTOR_ERR_INVALID_ARG;
+    if (dloss == nullptr || (reinterpret_cast<uintptr_t>(dloss) & 3u)) return DIRECTOR_ERR_INVALID_ARG;
+    if (added != nullptr && !aligned16(added)) return DIRECTOR_ERR_INVALID_ARG;
+    REQUIRE_PTR(dlogits);
+    const auto near_dlogits = [&](const float* p) {        // shares memory with dlogits
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(dlogits);
+        return (a < b ? b - a : a - b) < (uintptr_t)T * ctx->shape.E * sizeof(float);
+    };
+    if (near_dlogits(logits) || (added != nullptr && added != dlogits && near_dlogits(added))) return DIRECTOR_ERR_INVALID_ARG;
+    return launch_balance_backward(ctx, T, logits, counts, token_mask, dloss, added, dlogits, as_stream(stream));
 }
 
 int director_expert_ffn_checkpoint(director_ctx* ctx, int32_t T, const void* xp, const int32_t* seg_offsets, const void* w_gate,

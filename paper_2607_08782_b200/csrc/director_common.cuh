@@ -78,6 +78,7 @@ struct director_ctx {
     // backward pass, allocated by director_reserve_training
     void* d_dgu = nullptr;             // bf16 [2][T_max*K, F]     gradients of the gate and up values (act reuses d_hidden)
     void* d_dgu_shared = nullptr;      // bf16 [2][T_max, S*F]
+    void* d_balance = nullptr;         // sums of director_balance_loss over the CTAs of a launch, zeros between launches
     unsigned int* d_grad_sched = nullptr;   // [2] work-item counters of the two launches of a backward call, each cleared by the other
 
     // buffers of the host-buffer entry points; inputs, y and the histograms exist twice so that the
@@ -281,6 +282,11 @@ int launch_combine_backward(director_ctx*, int T, const void* dy, const void* yp
 int launch_route_backward(director_ctx*, int T, const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
                           float* dlogits, cudaStream_t);
 int launch_checkpoint_decode(director_ctx*, int rows, int F, const Checkpoint& kept, void* gate, void* up, cudaStream_t);
+size_t balance_workspace_bytes();
+int launch_balance_loss(director_ctx*, int T, const float* logits, const int32_t* topk_idx, const uint8_t* mask, float* loss,
+                        int64_t* counts, cudaStream_t);
+int launch_balance_backward(director_ctx*, int T, const float* logits, const int64_t* counts, const uint8_t* mask,
+                            const float* dloss, const float* added, float* dlogits, cudaStream_t);
 // topk_w == nullptr: all weights are one (the gradient of the dispatch)
 int launch_combine(director_ctx*, int T, const void* yp, const int32_t* inv_row, const float* topk_w,
                    const void* y_shared, void* y, cudaStream_t);

@@ -40,6 +40,7 @@ class MoELayer:
         # the layer have the same number.
         self.trained = None
         self.passes = 0
+        self.balanced = None         # (T, logits, token_mask, pass) of the balance_loss() whose counts are intact
         self.w = (w_gate, w_up, w_down)
         self.ws = (ws_gate, ws_up, ws_down)
         A, G = T_max * K, R * C_max
@@ -163,16 +164,34 @@ class MoELayer:
         self.trained = (T, x.detach(), self.d.placement_id(), self.passes)     # x without the graph that made it
         return self.y[:T]
 
-    def backward(self, T, dy):
+    def balance_loss(self, T, logits, token_mask=None):
+        """The router's balance term over the batch that forward_train() (or route()) just took, E sum_e f_e P_e, fp32 [1], and the
+        experts' counts, int64 [E+1], the last entry the number of valid tokens (see director_balance_loss): buffers of the layer,
+        overwritten by the next call.  logits: as for forward_train(); they and token_mask (uint8 or bool [T], 0 for padding) have
+        to stay as they are until backward()."""
+        if getattr(self, "balance", None) is None:
+            dev = self.y.device
+            self.balance = (torch.empty((1,), dtype=torch.float32, device=dev), torch.empty((self.dims["E"] + 1,), dtype=torch.int64, device=dev))
+        self.balanced = None
+        self.d.balance_loss(T, logits, self.topk_idx, token_mask, *self.balance)
+        self.balanced = (T, logits.detach(), token_mask, self.passes)
+        return self.balance
+
+    def backward(self, T, dy, dbalance=None):
         """Gradients of the forward_train() before, given dy = dL/dy [T,H] (bf16): a dict of x [T,H], logits [T,E], w_gate, w_up,
         w_down and, with shared experts, ws_gate, ws_up, ws_down - views of the layer's buffers, overwritten by the next call.
+        dbalance: dL/d balance_loss(), fp32 [1], whose part of the logits' gradient is added (after a balance_loss() of this pass).
         Under another placement than forward_train()'s, or after another pass of the layer, it raises a RuntimeError."""
         if self.trained is None or self.trained[0] != T:
             raise RuntimeError("backward() needs the buffers of a forward_train() of the same batch size, with no pass of the layer in between")
-        _, x, placement, _ = self.trained
+        _, x, placement, number = self.trained
         if self.d.placement_id() != placement:            # the rows lie in its segments, and the gradients read its tables
             raise RuntimeError("backward() needs the placement that forward_train() ran under, which has been changed since")
+        if dbalance is not None and (self.balanced is None or self.balanced[0] != T or self.balanced[3] != number):
+            raise RuntimeError("backward() with dbalance needs a balance_loss() of the pass")
         _need("backward", ("dy", dy, torch.bfloat16, T * self.dims["H"]))
+        if dbalance is not None:
+            _need("backward", ("dbalance", dbalance, torch.float32, 1))
         self.trained = None
         g = self.grads
         self.d.combine_backward(T, dy, self.yp, self.inv_row, self.topk_w, self.dyp, self.dtopk_w)
@@ -182,6 +201,9 @@ class MoELayer:
                                    g["w_down"], *shared)
         self.d.dispatch_backward(T, self.dxp, self.inv_row, self.dx_shared if with_shared else None, g["x"])
         self.d.route_backward(T, self.topk_idx, self.topk_w, self.dtopk_w, g["logits"])
+        if dbalance is not None:
+            _, logits, mask, _ = self.balanced
+            self.d.balance_loss_backward(T, logits, self.balance[1], mask, dbalance, g["logits"], g["logits"])
         return {n: t[:T] if n in ("x", "logits") else t for n, t in g.items()}
 
     def placement_cost(self, T, token_src_rank=None):

@@ -1,0 +1,192 @@
+"""From the gradients of a training step to the next weights: the global gradient norm, clipping by it, and AdamW with the clipping
+done on the way.  Any number of tensors, of a layer or of a whole model, bf16 or fp32 each.
+
+    grads = TensorList([layer.grads[n] for n in ("w_gate", "w_up", "w_down")])     # buffers that stay where they are
+    optimizer = AdamW(layer.w, lr=1e-4, max_norm=1.0)
+    ...
+    norm = optimizer.step(grads)                  # or step() for the weights' .grad, or step(list of tensors)
+
+Everything runs on the current stream and can be captured into a CUDA graph; nothing is read back.  Results have the same bits on
+every run.  Marshalling only: the work is done by the library's kernels (see include/director.h)."""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import binding
+from .binding import BF16, FP32, DirectorAdamW, DirectorError, DirectorParam, DirectorTensor, _check, load_library
+
+_TYPES = {torch.float32: FP32, torch.bfloat16: BF16}
+
+
+class TensorList:
+    """Tensors that calls take together: their addresses, looked up once.  Contiguous fp32 or bf16 CUDA tensors of one device, of any
+    size; None stands for a gradient that does not exist (AdamW.step leaves its weight as it is).  The list keeps the tensors; their
+    memory has to stay where it is (in-place changes are fine, set_() or resize_() are not)."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (DirectorTensor * max(1, len(self.tensors)))()
+        self.device = None
+        for i, t in enumerate(self.tensors):
+            if t is None:
+                continue
+            kind = _TYPES.get(t.dtype)
+            if kind is None:
+                raise TypeError(f"tensor {i} is {t.dtype}, fp32 or bf16 is needed")
+            if not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"tensor {i} has to be a contiguous CUDA tensor")
+            if self.device is None:
+                self.device = t.device
+            elif t.device != self.device:
+                raise ValueError(f"tensor {i} is on {t.device}, the ones before it on {self.device}")
+            a = self.array[i]
+            a.data, a.numel, a.type = t.data_ptr(), t.numel(), kind
+        if self.device is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def __iter__(self):
+        return iter(self.tensors)
+
+
+def _as_list(tensors) -> TensorList:
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def _begin(device: torch.device):
+    """The library and the current stream, which has to be one of the tensors' device."""
+    lib = load_library()
+    if binding._raw_stream is None:
+        binding._bind_torch()
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    return lib, binding._stream()
+
+
+def _workspace(lib, device) -> torch.Tensor:
+    # made anew by each call, on its stream: calls that overlap, captured ones too, never share one
+    return torch.empty((lib.director_grad_workspace_bytes(),), dtype=torch.uint8, device=device)
+
+
+def _changed(tensors):
+    """Tells autograd that the tensors were changed in place."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+
+
+def grad_norm(grads) -> torch.Tensor:
+    """The square root of the sum of squares over all elements of all tensors (a TensorList or a sequence): fp32, no dimensions."""
+    grads = _as_list(grads)
+    lib, stream = _begin(grads.device)
+    norm = torch.empty((), dtype=torch.float32, device=grads.device)
+    _check(lib.director_grad_norm(len(grads), grads.array, norm.data_ptr(), _workspace(lib, grads.device).data_ptr(), stream), "director_grad_norm")
+    return norm
+
+
+def clip_grads(grads, max_norm: float, out=None) -> torch.Tensor:
+    """Scales the gradients (a TensorList or a sequence) by min(1, max_norm / norm), in place or into `out` (tensors of the same
+    lengths, fp32 or bf16: fp32 gradients for an optimizer that takes those), and returns the norm before clipping (fp32, no
+    dimensions).  Where it is infinite or NaN nothing is scaled."""
+    grads = _as_list(grads)
+    out = grads if out is None else _as_list(out)
+    if len(out) != len(grads) or any((g is None) != (o is None) or (g is not None and g.numel() != o.numel()) for g, o in zip(grads, out)):
+        raise ValueError("clip_grads: out has to have a tensor of the same length for every gradient")
+    if not max_norm > 0:
+        raise ValueError(f"clip_grads: max_norm is {max_norm}, a positive number is needed")
+    if out.device != grads.device:
+        raise ValueError(f"clip_grads: the gradients are on {grads.device}, out is on {out.device}")
+    lib, stream = _begin(grads.device)
+    norm = torch.empty((), dtype=torch.float32, device=grads.device)
+    _check(lib.director_clip_grads(len(grads), grads.array, out.array, max_norm, norm.data_ptr(), _workspace(lib, grads.device).data_ptr(), stream),
+           "director_clip_grads")
+    _changed(out)
+    return norm
+
+
+class AdamW:
+    """AdamW over bf16 weights, each with an fp32 master, and fp32 weights (contiguous CUDA tensors, kept by reference and updated
+    in place); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to it.  A step whose norm is infinite or NaN is skipped
+    (with max_norm = infinity the norm is not taken, and such gradients reach the weights).  `lr` may be changed between steps; in a captured step, pass an
+    fp32 CUDA tensor of one element instead, which the step reads when it runs.  One optimizer serves one stream at a time."""
+
+    def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, max_norm=math.inf):
+        self.weights = list(weights)
+        listed = TensorList(self.weights)
+        if any(w is None for w in self.weights):
+            raise ValueError("AdamW: a weight is None")
+        self.device = listed.device
+        self.lr, self.betas, self.eps, self.weight_decay, self.max_norm = lr, tuple(betas), eps, weight_decay, max_norm
+        self.masters = [w.detach().float() if w.dtype is torch.bfloat16 else None for w in self.weights]
+        self.exp_avg = [torch.zeros_like(w, dtype=torch.float32, requires_grad=False) for w in self.weights]
+        self.exp_avg_sq = [torch.zeros_like(m) for m in self.exp_avg]
+        self.steps = torch.zeros((1,), dtype=torch.int64, device=self.device)
+        self.status = torch.zeros((1,), dtype=torch.int32, device=self.device)
+        self._params = (DirectorParam * max(1, len(self.weights)))()
+        for i, w in enumerate(self.weights):
+            p = self._params[i]
+            p.weight, p.numel, p.type = w.data_ptr(), w.numel(), listed.array[i].type
+            p.exp_avg, p.exp_avg_sq = self.exp_avg[i].data_ptr(), self.exp_avg_sq[i].data_ptr()
+            p.master = self.masters[i].data_ptr() if self.masters[i] is not None else None
+
+    def step(self, grads=None, lr=None) -> torch.Tensor | None:
+        """One step on `grads` (a TensorList or a sequence, a tensor or None for each weight; default: the weights' .grad), with
+        `lr` in place of the optimizer's if given (a number or an fp32 CUDA tensor of one element).  Returns the gradients' norm before
+        clipping (fp32, no dimensions), None where max_norm is infinite."""
+        grads = _as_list([w.grad for w in self.weights] if grads is None else grads)
+        if len(grads) != len(self.weights):
+            raise ValueError(f"AdamW.step: {len(grads)} gradients for {len(self.weights)} weights")
+        for i, (g, w) in enumerate(zip(grads.tensors, self.weights)):
+            if g is not None and g.shape != w.shape:
+                raise ValueError(f"AdamW.step: gradient {i} is {tuple(g.shape)}, its weight {tuple(w.shape)}")
+        if grads.device != self.device:
+            raise ValueError(f"AdamW.step: the gradients are on {grads.device}, the weights on {self.device}")
+        lib, stream = _begin(self.device)
+        lr = self.lr if lr is None else lr
+        lr_dev = None
+        if isinstance(lr, torch.Tensor):
+            if lr.dtype is not torch.float32 or lr.numel() != 1 or lr.device != self.device:
+                raise ValueError("AdamW.step: lr has to be a number or an fp32 tensor of one element on the weights' device")
+            lr_dev, lr = lr.data_ptr(), 0.0
+        h = DirectorAdamW(lr, *self.betas, self.eps, self.weight_decay, self.max_norm)
+        norm = torch.empty((), dtype=torch.float32, device=self.device) if math.isfinite(self.max_norm) else None
+        _check(lib.director_adamw_step(len(grads), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(),
+                                       norm.data_ptr() if norm is not None else None, self.status.data_ptr(),
+                                       _workspace(lib, self.device).data_ptr(), stream), "director_adamw_step")
+        _changed(self.weights)
+        return norm
+
+    def last_status(self) -> int:
+        """Waits for the current stream; 8 (DIRECTOR_ERR_NONFINITE) if a step was skipped since the last call, else 0."""
+        status = int(self.status.item())
+        self.status.zero_()
+        return status
+
+    def check_status(self):
+        """Raises a DirectorError if a step was skipped since the last call."""
+        status = self.last_status()
+        if status != 0:
+            raise DirectorError(status, "AdamW.step")
+
+    def state_dict(self) -> dict:
+        """The state, as it is (no copies): steps, masters, exp_avg, exp_avg_sq."""
+        return dict(steps=self.steps, masters=self.masters, exp_avg=self.exp_avg, exp_avg_sq=self.exp_avg_sq)
+
+    def load_state_dict(self, state: dict):
+        """Copies a state_dict() into this optimizer; the bf16 weights become their masters, rounded."""
+        for name in ("masters", "exp_avg", "exp_avg_sq"):
+            mine, theirs = getattr(self, name), list(state[name])
+            if len(theirs) != len(mine) or any(m is not None and (t is None or t.shape != m.shape) for m, t in zip(mine, theirs)):
+                raise ValueError(f"AdamW.load_state_dict: {name} does not fit the weights")
+        with torch.no_grad():
+            for name in ("masters", "exp_avg", "exp_avg_sq"):
+                for m, t in zip(getattr(self, name), state[name]):
+                    if m is not None:
+                        m.copy_(t)
+            for w, m in zip(self.weights, self.masters):
+                if m is not None:
+                    w.copy_(m)
+            self.steps.copy_(state["steps"])
