@@ -16,7 +16,11 @@ namespace director {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kVals = 16;
-constexpr int kForwardRows = 64;     // most rows of a lane's registers in one CTA of the forward: its fp32 sums stay short
+constexpr int kMostPasses = 64;      // rows that a lane sees in one CTA at most: the forward's fp32 sums stay short
+// CTAs of the forward that an SM holds, and that the batch is cut for: they all run at once (131072 x 256: 28 us; four and 64 registers
+// 28, five 41).  The backward sums nothing, and many small CTAs keep the addresses that are under way close together: 45 us with 16
+// an SM of which four run, 46 with 8, 50 with 4.
+constexpr int kForwardCtas = 3, kBackwardCtas = 16;
 
 // The sixteen values of lane `sub` of its row: groups of four, LPR groups apart.  -inf behind the last expert.
 template <int LPR, bool VEC>
@@ -54,7 +58,7 @@ __device__ __forceinline__ float softmax_terms(float (&x)[kVals]) {
     return s;
 }
 
-// Loss and counts.  A CTA sums its tokens' p in registers (fp32, at most kForwardRows rows a lane), then over lanes and warps (the
+// Loss and counts.  A CTA sums its tokens' p in registers (fp32, at most kMostPasses rows a lane), then over lanes and warps (the
 // latter in fp64), and adds the sums to the context's 64-bit integers as fixed point (2^`shift` to one; T 2^shift < 2^62), whose
 // order makes no difference: the loss has the same bits on every run.  The last CTA to arrive writes the results and leaves zeros.
 struct BalanceSums {
@@ -64,7 +68,7 @@ struct BalanceSums {
 };
 
 template <int LPR, bool VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kForwardCtas)
 balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk_idx, const uint8_t* __restrict__ mask, int T,
                     int E, int K, int rows, int shift, BalanceSums* __restrict__ sums, float* __restrict__ loss,
                     int64_t* __restrict__ counts, int32_t* status) {
@@ -79,28 +83,50 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
     __syncthreads();
     const int r0 = blockIdx.x * rows, n_rows = min(rows, T - r0);
 
-    for (unsigned a = tid; a < (unsigned)(n_rows * K); a += kThreads) {
-        if (mask != nullptr && __ldg(mask + r0 + a / (unsigned)K) == 0) continue;
-        const int e = __ldg(topk_idx + (size_t)r0 * K + a);
+    float acc[kVals] = {}, next[kVals] = {};
+    int valid = 0;
+    const auto fetch = [&](int base) {                     // the lane's part of its row of the pass at `base`
+        const int row = r0 + base + lane / LPR;
+        const bool live = base + lane / LPR < n_rows && (mask == nullptr || __ldg(mask + row) != 0);
+        if (live) load_row<LPR, VEC>(logits + (size_t)row * E, E, sub, next);
+        return live;
+    };
+    bool next_live = fetch(warp * kGroups);
+
+    // the counts, while the first rows are on their way; r0 is a multiple of four, so that a CTA's indices start on 16 bytes
+    const auto count_one = [&](unsigned a, int e) {
+        if (mask != nullptr && __ldg(mask + r0 + a / (unsigned)K) == 0) return;
         if ((unsigned)e < (unsigned)E) atomicAdd(&s_count[e], 1);
         else director_set_status(status, DIRECTOR_ERR_BAD_INDEX);
+    };
+    const unsigned n_chosen = (unsigned)n_rows * K;
+    const int32_t* const chosen = topk_idx + (size_t)r0 * K;
+    for (unsigned a = 4 * tid; a < n_chosen; a += 4 * kThreads) {
+        if (a + 4 <= n_chosen) {
+            const int4 e = __ldg(reinterpret_cast<const int4*>(chosen + a));
+            count_one(a, e.x), count_one(a + 1, e.y), count_one(a + 2, e.z), count_one(a + 3, e.w);
+        } else {
+            for (unsigned b = a; b < n_chosen; ++b) count_one(b, __ldg(chosen + b));
+        }
     }
 
-    float acc[kVals] = {};
-    int valid = 0;
     for (int base = warp * kGroups; base < n_rows; base += kWarps * kGroups) {
-        const bool here = base + lane / LPR < n_rows;
-        const int row = r0 + base + lane / LPR;
-        const bool live = here && (mask == nullptr || __ldg(mask + row) != 0);
-        float x[kVals] = {};
-        if (live) load_row<LPR, VEC>(logits + (size_t)row * E, E, sub, x);
-        const float s = softmax_terms<LPR>(x);
-        const bool good = live && s > 0.0f;
-        if (live && !good && sub == 0) director_set_status(status, DIRECTOR_ERR_NONFINITE);
-        valid += live && sub == 0;
-        const float inv = 1.0f / s;
+        const bool live = next_live;
+        float x[kVals];
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) acc[i] += good ? x[i] * inv : 0.0f;
+        for (int i = 0; i < kVals; ++i) x[i] = next[i];
+        next_live = fetch(base + kWarps * kGroups);
+        const float s = softmax_terms<LPR>(x);
+        const float inv = 1.0f / s;
+        if (live) {
+            valid += sub == 0;
+            if (s > 0.0f) {
+#pragma unroll
+                for (int i = 0; i < kVals; ++i) acc[i] = fmaf(x[i], inv, acc[i]);
+            } else if (sub == 0) {
+                director_set_status(status, DIRECTOR_ERR_NONFINITE);
+            }
+        }
     }
 #pragma unroll
     for (int o = LPR; o < 32; o <<= 1)
@@ -159,37 +185,45 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
 // The gradient.  f enters less its mean, (E counts_e - sum counts) / (E K N) from whole numbers: the difference f_e - sum_j f_j p_tj is
 // the same, and a router that is nearly balanced does not lose it to the rounding of two nearly equal numbers.
 template <int LPR, bool VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, VEC ? 4 : 3)
 balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restrict__ counts, const uint8_t* __restrict__ mask,
                         const float* __restrict__ dloss, const float* added, float* dlogits, int T, int E, int K, int rows,
                         int32_t* status) {
     constexpr int kGroups = 32 / LPR;
+    __shared__ float s_f[LPR * kVals];
+    __shared__ long long s_total[kWarps];
     chain_prologue();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LPR;
-    float f[kVals];
-    float factor;
-    {
-        long long c[kVals], total = 0;
-#pragma unroll
-        for (int i = 0; i < kVals; ++i) {
-            const int e = 4 * ((i / 4) * LPR + sub) + i % 4;
-            c[i] = e < E ? __ldg(counts + e) : 0;
-            total += c[i];
-        }
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-        const double n = (double)__ldg(counts + E), scale = n > 0 ? 1.0 / ((double)E * K * n) : 0.0;
-#pragma unroll
-        for (int i = 0; i < kVals; ++i) f[i] = (float)((double)(E * c[i] - total) * scale);
-        factor = n > 0 ? (float)((double)__ldg(dloss) * E / n) : 0.0f;
-    }
-    const int r0 = blockIdx.x * rows, n_rows = min(rows, T - r0);
-    for (int base = warp * kGroups; base < n_rows; base += kWarps * kGroups) {
-        const bool here = base + lane / LPR < n_rows;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % LPR;
+    const int r0 = (int)(gridDim.x - 1 - blockIdx.x) * rows, n_rows = min(rows, T - r0);
+    float x[kVals] = {};
+    const auto fetch = [&](int base) {                     // the lane's part of its row of the pass at `base`
         const int row = r0 + base + lane / LPR;
-        const bool live = here && (mask == nullptr || __ldg(mask + row) != 0);
-        float x[kVals] = {};
+        const bool live = base + lane / LPR < n_rows && (mask == nullptr || __ldg(mask + row) != 0);
         if (live) load_row<LPR, VEC>(logits + (size_t)row * E, E, sub, x);
+        return live;
+    };
+    bool live = fetch(warp * kGroups);
+
+    // f, while the first rows are on their way
+    const long long count = tid < E ? __ldg(counts + tid) : 0;
+    const double n = (double)__ldg(counts + E);
+    long long total = count;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    if (lane == 0) s_total[warp] = total;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) total += s_total[w];
+    if (tid < LPR * kVals) s_f[tid] = n > 0 ? (float)((double)(E * count - total) / ((double)E * K * n)) : 0.0f;
+    __syncthreads();
+    float f[kVals];
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) f[i] = s_f[4 * ((i / 4) * LPR + sub) + i % 4];
+    const float factor = n > 0 ? (float)((double)__ldg(dloss) * E / n) : 0.0f;
+
+    for (int base = warp * kGroups; base < n_rows; base += kWarps * kGroups) {
+        const int row = r0 + base + lane / LPR;
         const float s = softmax_terms<LPR>(x);
         const bool good = live && s > 0.0f;
         if (live && !good && sub == 0) director_set_status(status, DIRECTOR_ERR_NONFINITE);
@@ -200,25 +234,28 @@ balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restr
         for (int o = 1; o < LPR; o <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, o);
         const float inv = 1.0f / s, scale = factor * inv;
         mean *= inv;
+        float d[kVals];
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) d[i] = good ? scale * x[i] * (f[i] - mean) : 0.0f;
+        const bool here = base + lane / LPR < n_rows;
+        live = fetch(base + kWarps * kGroups);
         if (!here) continue;
 #pragma unroll
         for (int j = 0; j < kVals / 4; ++j) {
             const int e = 4 * (j * LPR + sub);
-            float d[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) d[i] = good ? scale * x[4 * j + i] * (f[4 * j + i] - mean) : 0.0f;
             const size_t at = (size_t)row * E + e;
             if (VEC) {
                 if (e >= E) continue;
+                float4 v = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
                 if (added != nullptr) {
                     const float4 a = *reinterpret_cast<const float4*>(added + at);
-                    d[0] += a.x, d[1] += a.y, d[2] += a.z, d[3] += a.w;
+                    v.x += a.x, v.y += a.y, v.z += a.z, v.w += a.w;
                 }
-                *reinterpret_cast<float4*>(dlogits + at) = make_float4(d[0], d[1], d[2], d[3]);
+                *reinterpret_cast<float4*>(dlogits + at) = v;
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (e + i < E) dlogits[at + i] = added != nullptr ? added[at + i] + d[i] : d[i];
+                    if (e + i < E) dlogits[at + i] = added != nullptr ? added[at + i] + d[4 * j + i] : d[4 * j + i];
             }
         }
     }
@@ -258,7 +295,7 @@ int launch_balance_loss(director_ctx* ctx, int T, const float* logits, const int
     for (int t = T; t > 0; t >>= 1) --shift;               // T 2^shift < 2^62
     return by_width(s.E, [&](auto lpr, auto vec) {
         constexpr int L = decltype(lpr)::value;
-        const int rows = rows_of_cta(T, L, 2 * ctx->sm_count, kForwardRows);
+        const int rows = rows_of_cta(T, L, kForwardCtas * ctx->sm_count, kMostPasses);
         LaunchScope scope(ctx, st, "balance_loss_kernel");
         return cuda_status(launch_chained(balance_loss_kernel<L, decltype(vec)::value>, dim3(ctas_of(T, rows)), dim3(kThreads), 0, st,
                                           logits, topk_idx, mask, T, (int)s.E, (int)s.K, rows, shift,
@@ -272,7 +309,7 @@ int launch_balance_backward(director_ctx* ctx, int T, const float* logits, const
     const director_shape& s = ctx->shape;
     return by_width(s.E, [&](auto lpr, auto vec) {
         constexpr int L = decltype(lpr)::value;
-        const int rows = rows_of_cta(T, L, 4 * ctx->sm_count, 32);
+        const int rows = rows_of_cta(T, L, kBackwardCtas * ctx->sm_count, kMostPasses);
         LaunchScope scope(ctx, st, "balance_backward_kernel");
         return cuda_status(launch_chained(balance_backward_kernel<L, decltype(vec)::value>, dim3(ctas_of(T, rows)), dim3(kThreads), 0, st,
                                           logits, counts, mask, dloss, added, dlogits, T, (int)s.E, (int)s.K, rows, ctx->d_status));

@@ -1,9 +1,13 @@
 // From a model's gradients to its next weights: the global norm, clipping by it, and AdamW with the clipping on the way (training; the
-// paper serves).  A call takes any number of tensors; their addresses and lengths travel as kernel parameters, up to kTensors to a
+// paper serves).  A call takes any number of tensors; their addresses and lengths travel as kernel parameters, a few hundred to a
 // launch, so that nothing has to be copied to the device ahead of a call and a captured call keeps its own table.
 //
-// All of it is HBM-bound elementwise work over the concatenation of the tensors.  That is cut into chunks which the CTAs of a grid
-// that fills the GPU once take in turn; the sums of squares are joined in a fixed order, so that a call gives the same bits again.
+// All of it is HBM-bound elementwise work over the concatenation of the tensors, which is cut into chunks.  A call is
+//   the sum of squares, by a grid that fills the GPU once;
+//   the norm: by one CTA that joins the partial sums, or, where the elementwise part has few CTAs (kFewChunks), by each of them;
+//   the elementwise part, a CTA to a chunk.
+// The norm alone of small tensors is one launch of one cluster (DIRECTOR_SMALL_BYTES).
+// Sums are joined in a fixed order, so that a call gives the same bits again.
 #include "director_common.cuh"
 
 #include <cuda_bf16.h>
@@ -17,18 +21,25 @@ namespace director {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kSlots = 1024;                     // CTAs of the norm's grid at most: one partial sum each
+constexpr int kThreads = 256;
+constexpr int kNormCtas = 5, kSlots = 1024;      // CTAs of the norm's grid: an SM's, and at most, one partial sum each
 constexpr int kNormUnroll = 4;                   // 16-byte loads of a thread and chunk of the norm
-constexpr int kVec = 8;                          // elements of a thread and chunk of the two others
-constexpr int kChunk = kThreads * kVec;
+constexpr int kClusterCtas = 16, kClusterThreads = 1024, kClusterUnroll = 8;
+constexpr int kChunk = kThreads * 8;             // elements of a chunk of the update
+constexpr int kClipUnroll = 4, kClipChunk = kThreads * 8 * kClipUnroll;
+constexpr int kFewChunks = 1200;
 constexpr long long kMostElements = 1ll << 40;
 
 // What a call keeps between its launches, in the caller's workspace.
 struct Workspace {
     double partial[kSlots];                      // sums of squares
-    double bias1, bias2;                         // 1 - beta^t of the step under way
+    // What all elements have in common.  Read as one vector through L1: with loads from L2, those of a few hundred thousand CTAs
+    // queue up at one line (an update of 603 M weights: 3157 instead of 2640 us).
+    float scale;                                 // the clipping factor, kNotFinite for a norm that is none
+    float decay, rate, root;                     // AdamW: lr * weight_decay, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
 };
+
+constexpr float kNotFinite = -1.0f;
 
 // The tensors of one launch: P arrays of CAP tensors, and the first chunk of each tensor.
 template <int P, int CAP>
@@ -39,7 +50,7 @@ struct Table {
     unsigned char kind[CAP];
     int n;
 };
-constexpr int kFewTensors = 16, kTensors = 160;
+constexpr int kFewTensors = DIRECTOR_SMALL_TENSORS, kNormTensors = 480, kClipTensors = 360, kUpdateTensors = 200;     // about 10 KB each
 
 // The tensor that chunk c lies in.
 template <typename TABLE>
@@ -61,15 +72,16 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 }
 
 // the sum over the CTA, in every thread; in a fixed order
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v) {
-    __shared__ double s_part[kWarps];
+    __shared__ double s_part[THREADS / 32];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
     __syncthreads();
     double sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) sum += s_part[w];
+    for (int w = 0; w < THREADS / 32; ++w) sum += s_part[w];
     return sum;
 }
 
@@ -101,16 +113,23 @@ __host__ __device__ inline long long head_of(const void* p, long long n) {
     return head < n ? head : n;
 }
 template <typename T>
-inline long long norm_chunks(const void* p, long long n) {
-    const long long vecs = (n - head_of<T>(p, n)) / (16 / (int)sizeof(T)), per = kThreads * kNormUnroll;
+inline long long norm_chunks(const void* p, long long n, int per) {
+    const long long vecs = (n - head_of<T>(p, n)) / (16 / (int)sizeof(T));
     return n == 0 ? 0 : vecs == 0 ? 1 : (vecs + per - 1) / per;
 }
 
-template <typename T>
+// What a thread of a CTA of THREADS adds for chunk `chunk` of a tensor: UNROLL 16-byte loads.
+template <typename T, int THREADS, int UNROLL>
 __device__ __forceinline__ double squares_of_chunk(const T* __restrict__ p, long long n, int chunk) {
     constexpr int kPer = 16 / sizeof(T);
     const int tid = threadIdx.x;
     const long long head = head_of<T>(p, n), vecs = (n - head) / kPer;
+    const uint4* q = reinterpret_cast<const uint4*>(p + head);
+    const long long v0 = (long long)chunk * (THREADS * UNROLL) + tid;
+    uint4 x[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+        x[u] = v0 + u * THREADS < vecs ? __ldg(q + v0 + u * THREADS) : make_uint4(0u, 0u, 0u, 0u);
     double sum = 0.0;
     if (chunk == 0) {                                      // the ragged ends: fewer than kPer elements each
         const int tail = (int)(n - head - vecs * kPer);
@@ -119,15 +138,9 @@ __device__ __forceinline__ double squares_of_chunk(const T* __restrict__ p, long
         else if (tid >= 32 && tid < 32 + tail) v = to_float(p[n - tail + tid - 32]);
         sum = (double)v * (double)v;
     }
-    const uint4* q = reinterpret_cast<const uint4*>(p + head);
-    const long long v0 = (long long)chunk * (kThreads * kNormUnroll) + tid;
-    uint4 x[kNormUnroll];
-#pragma unroll
-    for (int u = 0; u < kNormUnroll; ++u)
-        x[u] = v0 + u * kThreads < vecs ? __ldg(q + v0 + u * kThreads) : make_uint4(0u, 0u, 0u, 0u);
     float s = 0.0f;
 #pragma unroll
-    for (int u = 0; u < kNormUnroll; ++u)
+    for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const float v = element<T>(x[u], i);
@@ -135,7 +148,7 @@ __device__ __forceinline__ double squares_of_chunk(const T* __restrict__ p, long
         }
     if (s >= kSquaresLowest && s <= kSquaresHighest) return sum + (double)s;
 #pragma unroll
-    for (int u = 0; u < kNormUnroll; ++u)
+    for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const double v = (double)element<T>(x[u], i);
@@ -144,51 +157,103 @@ __device__ __forceinline__ double squares_of_chunk(const T* __restrict__ p, long
     return sum;
 }
 
-struct StepStart {                               // what the first launch of an AdamW step does besides
-    long long* steps;
-    double beta1, beta2;
+// What CTA `cta` of `ctas` has of the table: every ctas-th chunk.
+template <int THREADS, int UNROLL, typename TABLE>
+__device__ __forceinline__ double squares_of_table(const TABLE& t, int cta, int ctas) {
+    double sum = 0.0;
+    const int chunks = t.first[t.n];
+    for (int c = cta; c < chunks;) {
+        const int k = tensor_of(t, c), first = t.first[k], end = t.first[k + 1];
+        const long long n = t.numel[k];
+        if (t.kind[k] == DIRECTOR_BF16) {
+            const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(t.at[0][k]);
+            for (; c < end; c += ctas) sum += squares_of_chunk<__nv_bfloat16, THREADS, UNROLL>(p, n, c - first);
+        } else {
+            const float* p = static_cast<const float*>(t.at[0][k]);
+            for (; c < end; c += ctas) sum += squares_of_chunk<float, THREADS, UNROLL>(p, n, c - first);
+        }
+    }
+    return sum;
+}
+
+// What a call makes of the norm.  Its first launch starts the step (AdamW), one thread behind the norm finishes it.
+struct Call {
+    Workspace* ws;
+    float* norm;                 // or NULL
+    double max_norm;
+    long long* steps;            // AdamW; NULL: clipping
+    double lr, beta1, beta2, weight_decay;
+    const float* lr_dev;
+    int32_t* status;
 };
 
-__device__ __forceinline__ void start_step(const StepStart& s, Workspace* ws) {
-    const long long t = *s.steps + 1;
-    *s.steps = t;
-    ws->bias1 = 1.0 - pow(s.beta1, (double)t);
-    ws->bias2 = 1.0 - pow(s.beta2, (double)t);
+__device__ __forceinline__ void start_step(const Call& q) {
+    const long long t = *q.steps + 1;
+    *q.steps = t;
+    const double lr = q.lr_dev != nullptr ? (double)*q.lr_dev : q.lr;
+    q.ws->decay = (float)(lr * q.weight_decay);
+    q.ws->rate = (float)(lr / (1.0 - pow(q.beta1, (double)t)));
+    q.ws->root = (float)(1.0 / sqrt(1.0 - pow(q.beta2, (double)t)));
+}
+__device__ __forceinline__ float scale_of(const Call& q, double norm) {
+    return !isfinite((float)norm) ? kNotFinite : norm > q.max_norm ? (float)(q.max_norm / norm) : 1.0f;
+}
+__device__ __forceinline__ void finish(const Call& q, double norm) {
+    if (q.norm != nullptr) *q.norm = (float)norm;
+    if (q.steps != nullptr && !isfinite((float)norm)) {    // the step is not taken
+        *q.steps -= 1;
+        if (q.status != nullptr) director_set_status(q.status, DIRECTOR_ERR_NONFINITE);
+    }
 }
 
 // Partial sum blockIdx.x of the workspace, added to it where an earlier launch of the call has written it (blockIdx.x < filled).
 template <int CAP>
-__global__ void __launch_bounds__(kThreads, 4)
-norm_kernel(const __grid_constant__ Table<1, CAP> t, Workspace* ws, int filled, const StepStart start) {
+__global__ void __launch_bounds__(kThreads, kNormCtas)
+norm_kernel(const __grid_constant__ Table<1, CAP> t, const Call q, int filled) {
     chain_prologue();
-    if (start.steps != nullptr && blockIdx.x == 0 && threadIdx.x == 0) start_step(start, ws);
-    double sum = 0.0;
-    for (int c = blockIdx.x; c < t.first[t.n]; c += gridDim.x) {
-        const int k = tensor_of(t, c);
-        sum += t.kind[k] == DIRECTOR_BF16
-                   ? squares_of_chunk(static_cast<const __nv_bfloat16*>(t.at[0][k]), t.numel[k], c - t.first[k])
-                   : squares_of_chunk(static_cast<const float*>(t.at[0][k]), t.numel[k], c - t.first[k]);
-    }
-    sum = block_sum(sum);
-    if (threadIdx.x == 0) ws->partial[blockIdx.x] = (int)blockIdx.x < filled ? ws->partial[blockIdx.x] + sum : sum;
+    if (filled == 0 && q.steps != nullptr && blockIdx.x == gridDim.x - 1 && threadIdx.x == kThreads - 1) start_step(q);
+    const double sum = block_sum<kThreads>(squares_of_table<kThreads, kNormUnroll>(t, blockIdx.x, gridDim.x));
+    double* const mine = q.ws->partial + blockIdx.x;
+    if (threadIdx.x == 0) *mine = (int)blockIdx.x < filled ? *mine + sum : sum;
 }
 
-// The norm from the partial sums, in every thread of the CTA.
-__device__ __forceinline__ double norm_of(const Workspace* ws, int slots) {
+__device__ __forceinline__ double norm_of_slots(const Workspace* ws, int slots) {
     double v = 0.0;
     for (int i = threadIdx.x; i < slots; i += kThreads) v += __ldcg(&ws->partial[i]);
-    return sqrt(block_sum(v));
+    return sqrt(block_sum<kThreads>(v));
 }
 
-__global__ void __launch_bounds__(kThreads) norm_finish_kernel(const Workspace* ws, int slots, float* norm) {
+// The norm from the partial sums; with none of them: a norm of 0, and the step is started here.
+__global__ void __launch_bounds__(kThreads) finish_kernel(const Call q, int slots) {
     chain_prologue();
-    const double v = norm_of(ws, slots);
-    if (threadIdx.x == 0) *norm = (float)v;
+    const double norm = norm_of_slots(q.ws, slots);
+    if (threadIdx.x != 0) return;
+    if (slots == 0 && q.steps != nullptr) start_step(q);
+    q.ws->scale = scale_of(q, norm);
+    finish(q, norm);
 }
 
-__global__ void start_step_kernel(Workspace* ws, const StepStart start) {
+// The norm alone of small tensors: the CTAs of one cluster hand their sums to its first through distributed shared memory - one
+// launch instead of two, and no workspace.
+__global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterThreads, 1)
+norm_cluster_kernel(const __grid_constant__ Table<1, kFewTensors> t, float* norm) {
+    __shared__ double s_sums[kClusterCtas];
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     chain_prologue();
-    start_step(start, ws);
+    const double sum = block_sum<kClusterThreads>(squares_of_table<kClusterThreads, kClusterUnroll>(t, blockIdx.x, kClusterCtas));
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // every CTA of the cluster is there
+    if (threadIdx.x == 0) {
+        uint32_t at;
+        const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&s_sums[blockIdx.x]);
+        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(mine));
+        asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(at), "d"(sum) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        double v = 0.0;
+        for (int i = 0; i < kClusterCtas; ++i) v += s_sums[i];
+        *norm = (float)sqrt(v);
+    }
 }
 
 // ---- eight elements ------------------------------------------------------------------------------------------------
@@ -230,146 +295,161 @@ inline bool whole(const void* p) { return (reinterpret_cast<uintptr_t>(p) & (8 *
 // kind bits of a tensor: its types, and which addresses allow whole accesses
 enum { kGradBf16 = 1, kOutBf16 = 2, kGradWhole = 4, kOutWhole = 8 };
 
-// ---- clipping ------------------------------------------------------------------------------------------------------
-//
-// The chunks run backwards: the norm has read the last tensors last, and what of them is still in L2 is not fetched again.
-
-template <typename S, typename D>
-__device__ __forceinline__ void scale_chunk(const S* src, D* dst, long long n, int chunk, float scale, int kind) {
-    const long long at = (long long)chunk * kChunk + threadIdx.x * kVec;
-    if (at >= n) return;
-    float v[8];
-    const int some = (int)min(n - at, 8ll);
-    if (some == 8 && (kind & kGradWhole)) load8(src + at, v);
-    else load_some(src + at, some, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= scale;
-    if (some == 8 && (kind & kOutWhole)) store8(dst + at, v);
-    else store_some(dst + at, some, v);
+// (scale, decay, rate, root) of the workspace; with SLOTS the clipping factor is worked out from the partial sums instead, and one
+// thread of the launch, the call's only one, finishes.
+template <bool SLOTS>
+__device__ __forceinline__ float4 common_of(const Call& q, int slots) {
+    float4 c = *reinterpret_cast<const float4*>(&q.ws->scale);
+    if (SLOTS) {
+        const double norm = norm_of_slots(q.ws, slots);
+        if (blockIdx.x == 0 && threadIdx.x == 0) finish(q, norm);
+        c.x = scale_of(q, norm);
+    }
+    return c;
 }
 
-template <int CAP>
-__global__ void __launch_bounds__(kThreads, 4)
-clip_kernel(const __grid_constant__ Table<2, CAP> t, const Workspace* ws, int slots, float max_norm, float* norm) {
+// The chunks run backwards: the norm has read the last tensors last, and what of them is still in L2 is not fetched again.
+struct Place {
+    int k, kind;                 // tensor
+    long long at, left;          // the chunk's first element, and how many are left from there
+};
+template <typename TABLE>
+__device__ __forceinline__ Place place_of(const TABLE& t, int chunk) {
+    const int c = gridDim.x - 1 - blockIdx.x, k = tensor_of(t, c);
+    const long long at = (long long)(c - t.first[k]) * chunk;
+    return {k, t.kind[k], at, t.numel[k] - at};
+}
+
+// ---- clipping ------------------------------------------------------------------------------------------------------
+
+// A chunk: kClipUnroll x eight elements a thread, asked for together.  FULL: all of them exist; SW, DW: whole accesses.
+template <bool SLOTS, bool FULL, bool SW, bool DW, typename S, typename D>
+__device__ __forceinline__ void clip_chunk(const S* src, D* dst, long long left, const Call& q, int slots) {
+    float v[kClipUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kClipUnroll; ++u) {
+        const int e = (u * kThreads + threadIdx.x) * 8, some = FULL ? 8 : (int)max(0ll, min(8ll, left - e));
+        if (SW) load8(src + e, v[u]);
+        else load_some(src + e, some, v[u]);
+    }
+    const float scale = common_of<SLOTS>(q, slots).x;
+    const bool same = scale == kNotFinite || scale == 1.0f;
+    if (same && static_cast<const void*>(src) == dst) return;
+#pragma unroll
+    for (int u = 0; u < kClipUnroll; ++u) {
+        const int e = (u * kThreads + threadIdx.x) * 8, some = FULL ? 8 : (int)max(0ll, min(8ll, left - e));
+        if (!same)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] *= scale;
+        if (DW) store8(dst + e, v[u]);
+        else store_some(dst + e, some, v[u]);
+    }
+}
+template <bool SLOTS, typename S, typename D>
+__device__ __forceinline__ void clip_any(const void* src, void* dst, const Place& p, const Call& q, int slots) {
+    const S* s = static_cast<const S*>(src) + p.at;
+    D* d = static_cast<D*>(dst) + p.at;
+    const bool full = p.left >= kClipChunk;
+    if (full && (p.kind & kGradWhole) && (p.kind & kOutWhole)) clip_chunk<SLOTS, true, true, true>(s, d, p.left, q, slots);
+    else if (full && (p.kind & kOutWhole)) clip_chunk<SLOTS, true, false, true>(s, d, p.left, q, slots);
+    else clip_chunk<SLOTS, false, false, false>(s, d, p.left, q, slots);
+}
+
+template <int CAP, bool SLOTS>
+__global__ void __launch_bounds__(kThreads, SLOTS ? 3 : 4)
+clip_kernel(const __grid_constant__ Table<2, CAP> t, const Call q, int slots) {
     chain_prologue();
-    const double total = norm_of(ws, slots);
-    const float scale = total > (double)max_norm && isfinite((float)total) ? (float)((double)max_norm / total) : 1.0f;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
-    for (int c = t.first[t.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const int k = tensor_of(t, c), kind = t.kind[k], chunk = c - t.first[k];
-        const void* src = t.at[0][k];
-        void* dst = t.at[1][k];
-        if (scale == 1.0f && src == dst) continue;
-        const long long n = t.numel[k];
-        if (kind & kGradBf16) {
-            if (kind & kOutBf16) scale_chunk(static_cast<const __nv_bfloat16*>(src), static_cast<__nv_bfloat16*>(dst), n, chunk, scale, kind);
-            else scale_chunk(static_cast<const __nv_bfloat16*>(src), static_cast<float*>(dst), n, chunk, scale, kind);
-        } else {
-            if (kind & kOutBf16) scale_chunk(static_cast<const float*>(src), static_cast<__nv_bfloat16*>(dst), n, chunk, scale, kind);
-            else scale_chunk(static_cast<const float*>(src), static_cast<float*>(dst), n, chunk, scale, kind);
-        }
+    const Place p = place_of(t, kClipChunk);
+    const void* src = t.at[0][p.k];
+    void* dst = t.at[1][p.k];
+    if (!SLOTS && src == dst) {
+        const float scale = common_of<false>(q, 0).x;
+        if (scale == kNotFinite || scale == 1.0f) return;
+    }
+    if (p.kind & kGradBf16) {
+        if (p.kind & kOutBf16) clip_any<SLOTS, __nv_bfloat16, __nv_bfloat16>(src, dst, p, q, slots);
+        else clip_any<SLOTS, __nv_bfloat16, float>(src, dst, p, q, slots);
+    } else {
+        if (p.kind & kOutBf16) clip_any<SLOTS, float, __nv_bfloat16>(src, dst, p, q, slots);
+        else clip_any<SLOTS, float, float>(src, dst, p, q, slots);
     }
 }
 
 // ---- AdamW ---------------------------------------------------------------------------------------------------------
 
-struct AdamW {
-    float beta1, rest1, beta2, rest2, eps, decay;          // rest = 1 - beta, decay = lr * weight_decay
-    float scale, rate, root;                               // the clipping factor, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+struct Betas {
+    float beta1, rest1, beta2, rest2, eps;                 // rest = 1 - beta
+};
+struct Arrays {
+    const void* grad;
+    void* weight;
+    float *master, *exp_avg, *exp_avg_sq;
 };
 
-template <typename G, typename W>
-__device__ __forceinline__ void update_chunk(const G* grad, W* weight, float* master, float* exp_avg, float* exp_avg_sq, long long n,
-                                             int chunk, const AdamW& a, int kind) {
-    const long long at = (long long)chunk * kChunk + threadIdx.x * kVec;
-    if (at >= n) return;
-    const int some = (int)min(n - at, 8ll);
-    const bool all = some == 8 && (kind & kOutWhole);
+// A chunk: eight elements a thread.  FULL: all of them exist and the weight and its state allow whole accesses; GW: the gradient does.
+template <bool SLOTS, bool FULL, bool GW, typename G, typename W>
+__device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, const Call& q, const Betas& b, int slots) {
+    constexpr bool kMaster = sizeof(W) == 2;
+    const long long at = p.at + threadIdx.x * 8;
+    const int some = FULL ? 8 : (int)max(0ll, min(8ll, p.left - threadIdx.x * 8));
+    const G* const grad = static_cast<const G*>(a.grad) + at;
+    W* const weight = static_cast<W*>(a.weight) + at;
+    float* const w32 = kMaster ? a.master + at : reinterpret_cast<float*>(weight);
     float g[8], w[8], m[8], v[8];
-    if (some == 8 && (kind & kGradWhole)) load8(grad + at, g);
-    else load_some(grad + at, some, g);
-    float* const w32 = sizeof(W) == 2 ? master : reinterpret_cast<float*>(weight);
-    if (all) {
-        load8(exp_avg + at, m);
-        load8(exp_avg_sq + at, v);
-        load8(w32 + at, w);
+    if (FULL) {
+        load8(a.exp_avg + at, m);
+        load8(a.exp_avg_sq + at, v);
+        load8(w32, w);
     } else {
-        load_some(exp_avg + at, some, m);
-        load_some(exp_avg_sq + at, some, v);
-        load_some(w32 + at, some, w);
+        load_some(a.exp_avg + at, some, m);
+        load_some(a.exp_avg_sq + at, some, v);
+        load_some(w32, some, w);
     }
+    if (GW) load8(grad, g);
+    else load_some(grad, some, g);
+    const float4 common = common_of<SLOTS>(q, slots);
+    const float scale = common.x, decay = common.y, rate = common.z, root = common.w;
+    if (scale == kNotFinite) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float x = g[i] * a.scale;
-        m[i] = fmaf(a.beta1, m[i], a.rest1 * x);
-        v[i] = fmaf(a.beta2, v[i], a.rest2 * x * x);
-        w[i] = fmaf(-a.decay, w[i], w[i]) - a.rate * m[i] / fmaf(sqrtf(v[i]), a.root, a.eps);
+        const float x = g[i] * scale;
+        m[i] = fmaf(b.beta1, m[i], b.rest1 * x);
+        v[i] = fmaf(b.beta2, v[i], b.rest2 * x * x);
+        w[i] = fmaf(-decay, w[i], w[i]) - rate * m[i] / fmaf(sqrtf(v[i]), root, b.eps);
     }
-    if (all) {
-        store8(exp_avg + at, m);
-        store8(exp_avg_sq + at, v);
-        store8(w32 + at, w);
-        if (sizeof(W) == 2) store8(weight + at, w);
+    if (FULL) {
+        store8(a.exp_avg + at, m);
+        store8(a.exp_avg_sq + at, v);
+        store8(w32, w);
+        if (kMaster) store8(weight, w);
     } else {
-        store_some(exp_avg + at, some, m);
-        store_some(exp_avg_sq + at, some, v);
-        store_some(w32 + at, some, w);
-        if (sizeof(W) == 2) store_some(weight + at, some, w);
+        store_some(a.exp_avg + at, some, m);
+        store_some(a.exp_avg_sq + at, some, v);
+        store_some(w32, some, w);
+        if (kMaster) store_some(weight, some, w);
     }
 }
+template <bool SLOTS, typename G, typename W>
+__device__ __forceinline__ void update_any(const Arrays& a, const Place& p, const Call& q, const Betas& b, int slots) {
+    const bool full = p.left >= kChunk && (p.kind & kOutWhole);
+    if (full && (p.kind & kGradWhole)) update_chunk<SLOTS, true, true, G, W>(a, p, q, b, slots);
+    else if (full) update_chunk<SLOTS, true, false, G, W>(a, p, q, b, slots);
+    else update_chunk<SLOTS, false, false, G, W>(a, p, q, b, slots);
+}
 
-struct StepRest {
-    float beta1, rest1, beta2, rest2, eps;
-    double lr, weight_decay, max_norm;
-    const float* lr_dev;
-    float* norm;
-    long long* steps;
-    int32_t* status;
-    int slots;           // partial sums of the norm; 0: it was not taken
-    bool last;           // of the call's launches
-};
-
-template <int CAP>
-__global__ void __launch_bounds__(kThreads, 4)
-update_kernel(const __grid_constant__ Table<5, CAP> t, const Workspace* ws, const StepRest r) {
+template <int CAP, bool SLOTS>
+__global__ void __launch_bounds__(kThreads, SLOTS ? 3 : 4)
+update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas b, int slots) {
     chain_prologue();
-    AdamW a;
-    a.beta1 = r.beta1, a.rest1 = r.rest1, a.beta2 = r.beta2, a.rest2 = r.rest2, a.eps = r.eps;
-    a.scale = 1.0f;
-    const bool first = blockIdx.x == 0 && threadIdx.x == 0 && r.last;
-    if (r.slots > 0) {
-        const double total = norm_of(ws, r.slots);
-        if (first && r.norm != nullptr) *r.norm = (float)total;
-        if (!isfinite((float)total)) {
-            if (first) {
-                *r.steps -= 1;                             // no other thread of the launch reads it
-                if (r.status != nullptr) director_set_status(r.status, DIRECTOR_ERR_NONFINITE);
-            }
-            return;
-        }
-        if (total > r.max_norm) a.scale = (float)(r.max_norm / total);
-    }
-    const double lr = r.lr_dev != nullptr ? (double)__ldg(r.lr_dev) : r.lr;
-    a.decay = (float)(lr * r.weight_decay);
-    a.rate = (float)(lr / __ldcg(&ws->bias1));
-    a.root = (float)(1.0 / sqrt(__ldcg(&ws->bias2)));
-    for (int c = t.first[t.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const int k = tensor_of(t, c), kind = t.kind[k], chunk = c - t.first[k];
-        const long long n = t.numel[k];
-        const void* grad = t.at[0][k];
-        void* weight = t.at[1][k];
-        float* master = static_cast<float*>(t.at[2][k]);
-        float* exp_avg = static_cast<float*>(t.at[3][k]);
-        float* exp_avg_sq = static_cast<float*>(t.at[4][k]);
-        if (kind & kGradBf16) {
-            const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(grad);
-            if (kind & kOutBf16) update_chunk(g, static_cast<__nv_bfloat16*>(weight), master, exp_avg, exp_avg_sq, n, chunk, a, kind);
-            else update_chunk(g, static_cast<float*>(weight), master, exp_avg, exp_avg_sq, n, chunk, a, kind);
-        } else {
-            const float* g = static_cast<const float*>(grad);
-            if (kind & kOutBf16) update_chunk(g, static_cast<__nv_bfloat16*>(weight), master, exp_avg, exp_avg_sq, n, chunk, a, kind);
-            else update_chunk(g, static_cast<float*>(weight), master, exp_avg, exp_avg_sq, n, chunk, a, kind);
-        }
+    const Place p = place_of(t, kChunk);
+    const Arrays a{t.at[0][p.k], t.at[1][p.k], static_cast<float*>(t.at[2][p.k]), static_cast<float*>(t.at[3][p.k]),
+                   static_cast<float*>(t.at[4][p.k])};
+    if (p.kind & kGradBf16) {
+        if (p.kind & kOutBf16) update_any<SLOTS, __nv_bfloat16, __nv_bfloat16>(a, p, q, b, slots);
+        else update_any<SLOTS, __nv_bfloat16, float>(a, p, q, b, slots);
+    } else {
+        if (p.kind & kOutBf16) update_any<SLOTS, float, __nv_bfloat16>(a, p, q, b, slots);
+        else update_any<SLOTS, float, float>(a, p, q, b, slots);
     }
 }
 
@@ -422,11 +502,6 @@ int check_tensors(int32_t n, const director_tensor* g) {
     return DIRECTOR_OK;
 }
 
-bool sm_count(int* out) {
-    int dev = 0;
-    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
-}
-
 template <typename... KArgs>
 cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, unsigned threads, cudaStream_t st, const KArgs&... args) {
     cudaLaunchConfig_t cfg = {};
@@ -443,7 +518,7 @@ cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, unsigned threads, cu
 }
 
 // Puts the tensors i = 0 .. n-1 that have chunks (chunks_of(i)) into tables (fill(table, slot, i)) and launches each table that is
-// full, and the last one even if it is empty: run(table, chunks, last).
+// full, and the last one even if it is empty: run(table, chunks).
 template <typename TABLE, int CAP, typename Chunks, typename Fill, typename Run>
 int in_tables(int n, Chunks&& chunks_of, Fill&& fill, Run&& run) {
     TABLE t;
@@ -453,7 +528,7 @@ int in_tables(int n, Chunks&& chunks_of, Fill&& fill, Run&& run) {
         const long long chunks = chunks_of(i);
         if (chunks == 0) continue;
         if (t.n == CAP || t.first[t.n] + chunks > (1ll << 30)) {
-            const int rc = run(t, t.first[t.n], false);
+            const int rc = run(t, t.first[t.n]);
             if (rc != DIRECTOR_OK) return rc;
             t.n = 0;
         }
@@ -461,47 +536,73 @@ int in_tables(int n, Chunks&& chunks_of, Fill&& fill, Run&& run) {
         t.first[t.n + 1] = (int)(t.first[t.n] + chunks);
         ++t.n;
     }
-    return run(t, t.first[t.n], true);
+    return run(t, t.first[t.n]);
 }
 
-unsigned grid_of(int chunks, int sms) {
-    const int most = std::min(4 * sms, kSlots);
-    return (unsigned)std::max(1, std::min(chunks, most));
+// Whether one cluster takes the sum of squares.
+bool in_one_cluster(int n, const director_tensor* g) {
+    if (n > kFewTensors) return false;
+    long long bytes = 0;
+    for (int i = 0; i < n; ++i) {
+        if (g[i].numel > DIRECTOR_SMALL_BYTES) return false;
+        bytes += g[i].numel * (long long)width_of(g[i].type);
+    }
+    return bytes <= DIRECTOR_SMALL_BYTES;
 }
 
-// The launches that leave the partial sums in the workspace; *slots: how many.
-template <int CAP>
-int norm_launches(int n, const director_tensor* g, Workspace* ws, const StepStart& start, int sms, int* slots, cudaStream_t st) {
-    *slots = 0;
-    StepStart s = start;
+template <int CAP, typename Run>
+int norm_tables(int n, const director_tensor* g, int per, Run&& run) {
     return in_tables<Table<1, CAP>, CAP>(
         n,
         [&](int i) {
-            return g[i].type == DIRECTOR_BF16 ? norm_chunks<__nv_bfloat16>(g[i].data, g[i].numel) : norm_chunks<float>(g[i].data, g[i].numel);
+            return g[i].type == DIRECTOR_BF16 ? norm_chunks<__nv_bfloat16>(g[i].data, g[i].numel, per)
+                                              : norm_chunks<float>(g[i].data, g[i].numel, per);
         },
         [&](Table<1, CAP>& t, int k, int i) {
             t.at[0][k] = g[i].data;
             t.numel[k] = g[i].numel;
             t.kind[k] = (unsigned char)g[i].type;
         },
-        [&](const Table<1, CAP>& t, int chunks, bool) {
-            const unsigned grid = grid_of(chunks, sms);
-            const cudaError_t e = launch(norm_kernel<CAP>, grid, kThreads, st, t, ws, *slots, s);
-            *slots = std::max(*slots, (int)grid);
-            s.steps = nullptr;
-            return cuda_status(e);
-        });
-}
-int take_norm(int n, const director_tensor* g, Workspace* ws, const StepStart& start, int sms, int* slots, cudaStream_t st) {
-    return n <= kFewTensors ? norm_launches<kFewTensors>(n, g, ws, start, sms, slots, st)
-                            : norm_launches<kTensors>(n, g, ws, start, sms, slots, st);
+        run);
 }
 
-template <int CAP>
-int clip_launches(int n, const director_tensor* g, const director_tensor* out, const Workspace* ws, int slots, float max_norm, float* norm,
-                  int sms, cudaStream_t st) {
+// Leaves *slots partial sums in the workspace.
+int sum_squares(int n, const director_tensor* g, const Call& q, int* slots, cudaStream_t st) {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return DIRECTOR_ERR_CUDA;
+    *slots = 0;
+    const auto run = [&](auto kernel, const auto& t, int chunks) {
+        const int grid = std::max(1, std::min({chunks, kNormCtas * sms, kSlots}));
+        const cudaError_t e = launch(kernel, (unsigned)grid, kThreads, st, t, q, *slots);
+        *slots = std::max(*slots, grid);
+        return cuda_status(e);
+    };
+    constexpr int kPer = kThreads * kNormUnroll;
+    return n <= kFewTensors
+        ? norm_tables<kFewTensors>(n, g, kPer, [&](const Table<1, kFewTensors>& t, int chunks) { return run(norm_kernel<kFewTensors>, t, chunks); })
+        : norm_tables<kNormTensors>(n, g, kPer, [&](const Table<1, kNormTensors>& t, int chunks) { return run(norm_kernel<kNormTensors>, t, chunks); });
+}
+
+int finish_call(const Call& q, int slots, cudaStream_t st) { return cuda_status(launch(finish_kernel, 1u, kThreads, st, q, slots)); }
+
+// Sums the squares for a call whose elementwise part has chunks of `chunk` elements, and joins the sums unless those do it; *slots: how many
+// they have to join.
+int norm_for(int n, const director_tensor* g, int chunk, const Call& q, int* slots, cudaStream_t st) {
+    long long chunks = 0;
+    for (int i = 0; i < n; ++i) chunks += (g[i].numel + chunk - 1) / chunk;
+    int rc = sum_squares(n, g, q, slots, st);
+    if (rc == DIRECTOR_OK && (n > kFewTensors || chunks == 0 || chunks > kFewChunks)) {
+        rc = finish_call(q, *slots, st);
+        *slots = 0;
+    }
+    return rc;
+}
+
+template <int CAP, bool SLOTS>
+int clip_launches(int n, const director_tensor* g, const director_tensor* out, const Call& q, int slots, cudaStream_t st) {
     return in_tables<Table<2, CAP>, CAP>(
-        n, [&](int i) { return (g[i].numel + kChunk - 1) / kChunk; },
+        n, [&](int i) { return (g[i].numel + kClipChunk - 1) / kClipChunk; },
         [&](Table<2, CAP>& t, int k, int i) {
             t.at[0][k] = g[i].data;
             t.at[1][k] = out[i].data;
@@ -511,13 +612,13 @@ int clip_launches(int n, const director_tensor* g, const director_tensor* out, c
                                         ((sb ? whole<__nv_bfloat16>(g[i].data) : whole<float>(g[i].data)) ? kGradWhole : 0) |
                                         ((db ? whole<__nv_bfloat16>(out[i].data) : whole<float>(out[i].data)) ? kOutWhole : 0));
         },
-        [&](const Table<2, CAP>& t, int chunks, bool) {
-            return cuda_status(launch(clip_kernel<CAP>, grid_of(chunks, sms), kThreads, st, t, ws, slots, max_norm, norm));
+        [&](const Table<2, CAP>& t, int chunks) {
+            return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(clip_kernel<CAP, SLOTS>, (unsigned)chunks, kThreads, st, t, q, slots));
         });
 }
 
-template <int CAP>
-int update_launches(int n, const director_tensor* g, const director_param* p, const Workspace* ws, StepRest rest, int sms, cudaStream_t st) {
+template <int CAP, bool SLOTS>
+int update_launches(int n, const director_tensor* g, const director_param* p, const Call& q, const Betas& b, int slots, cudaStream_t st) {
     return in_tables<Table<5, CAP>, CAP>(
         n, [&](int i) { return (g[i].numel + kChunk - 1) / kChunk; },
         [&](Table<5, CAP>& t, int k, int i) {
@@ -533,9 +634,8 @@ int update_launches(int n, const director_tensor* g, const director_param* p, co
             t.kind[k] = (unsigned char)((gb ? kGradBf16 : 0) | (wb ? kOutBf16 : 0) | (state ? kOutWhole : 0) |
                                         ((gb ? whole<__nv_bfloat16>(g[i].data) : whole<float>(g[i].data)) ? kGradWhole : 0));
         },
-        [&](const Table<5, CAP>& t, int chunks, bool last) {
-            rest.last = last;
-            return cuda_status(launch(update_kernel<CAP>, grid_of(chunks, sms), kThreads, st, t, ws, rest));
+        [&](const Table<5, CAP>& t, int chunks) {
+            return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(update_kernel<CAP, SLOTS>, (unsigned)chunks, kThreads, st, t, q, b, slots));
         });
 }
 
@@ -554,14 +654,21 @@ int64_t director_grad_workspace_bytes(void) { return (int64_t)sizeof(Workspace);
 int director_grad_norm(int32_t n, const director_tensor* grads, float* norm, void* workspace, void* stream) {
     const int rc = check_tensors(n, grads);
     if (rc != DIRECTOR_OK) return rc;
-    if (norm == nullptr || !aligned4(norm) || workspace == nullptr || !aligned16(workspace)) return DIRECTOR_ERR_INVALID_ARG;
-    int sms = 0, slots = 0;
-    if (!sm_count(&sms)) return DIRECTOR_ERR_CUDA;
+    if (norm == nullptr || !aligned4(norm) || !aligned16(workspace) || (workspace == nullptr && !in_one_cluster(n, grads)))
+        return DIRECTOR_ERR_INVALID_ARG;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    Workspace* ws = static_cast<Workspace*>(workspace);
-    const int done = take_norm(n, grads, ws, StepStart{}, sms, &slots, st);
-    if (done != DIRECTOR_OK) return done;
-    return cuda_status(launch(norm_finish_kernel, 1u, kThreads, st, static_cast<const Workspace*>(ws), slots, norm));
+    if (in_one_cluster(n, grads)) {
+        if (cudaFuncSetAttribute(norm_cluster_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return DIRECTOR_ERR_CUDA;
+        return norm_tables<kFewTensors>(n, grads, kClusterThreads * kClusterUnroll, [&](const Table<1, kFewTensors>& t, int) {
+            return cuda_status(launch(norm_cluster_kernel, kClusterCtas, kClusterThreads, st, t, norm));
+        });
+    }
+    Call q = {};
+    q.ws = static_cast<Workspace*>(workspace);
+    q.norm = norm;
+    int slots = 0;
+    const int done = sum_squares(n, grads, q, &slots, st);
+    return done != DIRECTOR_OK ? done : finish_call(q, slots, st);
 }
 
 int director_clip_grads(int32_t n, const director_tensor* grads, const director_tensor* out, float max_norm, float* norm,
@@ -582,14 +689,17 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
     extents.add(norm, 1, DIRECTOR_FP32, true);
     extents.add(workspace, sizeof(Workspace) / 4, DIRECTOR_FP32, true);
     if (!extents.apart()) return DIRECTOR_ERR_INVALID_ARG;
-    int sms = 0, slots = 0;
-    if (!sm_count(&sms)) return DIRECTOR_ERR_CUDA;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    Workspace* ws = static_cast<Workspace*>(workspace);
-    rc = take_norm(n, grads, ws, StepStart{}, sms, &slots, st);
+    Call q = {};
+    q.ws = static_cast<Workspace*>(workspace);
+    q.norm = norm;
+    q.max_norm = max_norm;
+    int slots = 0;
+    rc = norm_for(n, grads, kClipChunk, q, &slots, st);
     if (rc != DIRECTOR_OK) return rc;
-    return n <= kFewTensors ? clip_launches<kFewTensors>(n, grads, out, ws, slots, max_norm, norm, sms, st)
-                            : clip_launches<kTensors>(n, grads, out, ws, slots, max_norm, norm, sms, st);
+    return slots > 0          ? clip_launches<kFewTensors, true>(n, grads, out, q, slots, st)
+           : n <= kFewTensors ? clip_launches<kFewTensors, false>(n, grads, out, q, 0, st)
+                              : clip_launches<kClipTensors, false>(n, grads, out, q, 0, st);
 }
 
 int director_adamw_step(int32_t n, const director_tensor* grads, const director_param* params, const director_adamw* h,
@@ -624,25 +734,25 @@ int director_adamw_step(int32_t n, const director_tensor* grads, const director_
     if (device_status != nullptr) extents.add(device_status, 1, DIRECTOR_FP32, true);
     extents.add(workspace, sizeof(Workspace) / 4, DIRECTOR_FP32, true);
     if (!extents.apart()) return DIRECTOR_ERR_INVALID_ARG;
-    int sms = 0;
-    if (!sm_count(&sms)) return DIRECTOR_ERR_CUDA;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    Workspace* ws = static_cast<Workspace*>(workspace);
-    StepRest rest = {};
-    rest.beta1 = (float)h->beta1, rest.rest1 = (float)(1.0 - h->beta1);
-    rest.beta2 = (float)h->beta2, rest.rest2 = (float)(1.0 - h->beta2);
-    rest.eps = (float)h->eps;
-    rest.lr = h->lr, rest.weight_decay = h->weight_decay, rest.max_norm = h->max_norm;
-    rest.lr_dev = lr;
-    rest.norm = norm;
-    rest.steps = reinterpret_cast<long long*>(steps);
-    rest.status = device_status;
-    const StepStart start{rest.steps, h->beta1, h->beta2};
-    if (norm != nullptr || std::isfinite(h->max_norm)) rc = take_norm(n, grads, ws, start, sms, &rest.slots, st);
-    else rc = cuda_status(launch(start_step_kernel, 1u, 1u, st, ws, start));
+    Call q = {};
+    q.ws = static_cast<Workspace*>(workspace);
+    q.norm = norm;
+    q.max_norm = h->max_norm;
+    q.steps = reinterpret_cast<long long*>(steps);
+    q.lr = h->lr, q.beta1 = h->beta1, q.beta2 = h->beta2, q.weight_decay = h->weight_decay;
+    q.lr_dev = lr;
+    q.status = device_status;
+    int slots = 0;
+    rc = norm != nullptr || std::isfinite(h->max_norm) ? norm_for(n, grads, kChunk, q, &slots, st) : finish_call(q, 0, st);
     if (rc != DIRECTOR_OK) return rc;
-    return n <= kFewTensors ? update_launches<kFewTensors>(n, grads, params, ws, rest, sms, st)
-                            : update_launches<kTensors>(n, grads, params, ws, rest, sms, st);
+    Betas b = {};
+    b.beta1 = (float)h->beta1, b.rest1 = (float)(1.0 - h->beta1);
+    b.beta2 = (float)h->beta2, b.rest2 = (float)(1.0 - h->beta2);
+    b.eps = (float)h->eps;
+    return slots > 0          ? update_launches<kFewTensors, true>(n, grads, params, q, b, slots, st)
+           : n <= kFewTensors ? update_launches<kFewTensors, false>(n, grads, params, q, b, 0, st)
+                              : update_launches<kUpdateTensors, false>(n, grads, params, q, b, 0, st);
 }
 
 }  // extern "C"

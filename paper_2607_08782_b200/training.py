@@ -29,6 +29,7 @@ class TensorList:
     def __init__(self, tensors):
         self.tensors = list(tensors)
         self.array = (DirectorTensor * max(1, len(self.tensors)))()
+        self.shapes = [None if t is None else t.shape for t in self.tensors]
         self.device = None
         for i, t in enumerate(self.tensors):
             if t is None:
@@ -44,6 +45,9 @@ class TensorList:
                 raise ValueError(f"tensor {i} is on {t.device}, the ones before it on {self.device}")
             a = self.array[i]
             a.data, a.numel, a.type = t.data_ptr(), t.numel(), kind
+        self.numels = [a.numel for a in self.array[:len(self.tensors)]]
+        # what the library's norm needs no workspace for
+        self.small = len(self.tensors) <= 16 and sum(a.numel * (4 if a.type == FP32 else 2) for a in self.array) <= 4 << 20
         if self.device is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
 
@@ -70,7 +74,7 @@ def _begin(device: torch.device):
 
 def _workspace(lib, device) -> torch.Tensor:
     # made anew by each call, on its stream: calls that overlap, captured ones too, never share one
-    return torch.empty((lib.director_grad_workspace_bytes(),), dtype=torch.uint8, device=device)
+    return torch.empty(lib.director_grad_workspace_bytes(), dtype=torch.uint8, device=device)
 
 
 def _changed(tensors):
@@ -83,7 +87,9 @@ def grad_norm(grads) -> torch.Tensor:
     grads = _as_list(grads)
     lib, stream = _begin(grads.device)
     norm = torch.empty((), dtype=torch.float32, device=grads.device)
-    _check(lib.director_grad_norm(len(grads), grads.array, norm.data_ptr(), _workspace(lib, grads.device).data_ptr(), stream), "director_grad_norm")
+    workspace = None if grads.small else _workspace(lib, grads.device)
+    _check(lib.director_grad_norm(len(grads), grads.array, norm.data_ptr(), None if workspace is None else workspace.data_ptr(), stream),
+           "director_grad_norm")
     return norm
 
 
@@ -93,17 +99,17 @@ def clip_grads(grads, max_norm: float, out=None) -> torch.Tensor:
     dimensions).  Where it is infinite or NaN nothing is scaled."""
     grads = _as_list(grads)
     out = grads if out is None else _as_list(out)
-    if len(out) != len(grads) or any((g is None) != (o is None) or (g is not None and g.numel() != o.numel()) for g, o in zip(grads, out)):
+    if out.numels != grads.numels:
         raise ValueError("clip_grads: out has to have a tensor of the same length for every gradient")
     if not max_norm > 0:
         raise ValueError(f"clip_grads: max_norm is {max_norm}, a positive number is needed")
     if out.device != grads.device:
         raise ValueError(f"clip_grads: the gradients are on {grads.device}, out is on {out.device}")
     lib, stream = _begin(grads.device)
-    norm = torch.empty((), dtype=torch.float32, device=grads.device)
-    _check(lib.director_clip_grads(len(grads), grads.array, out.array, max_norm, norm.data_ptr(), _workspace(lib, grads.device).data_ptr(), stream),
+    norm, workspace = torch.empty((), dtype=torch.float32, device=grads.device), _workspace(lib, grads.device)
+    _check(lib.director_clip_grads(len(grads), grads.array, out.array, max_norm, norm.data_ptr(), workspace.data_ptr(), stream),
            "director_clip_grads")
-    _changed(out)
+    _changed(out.tensors)
     return norm
 
 
@@ -111,7 +117,8 @@ class AdamW:
     """AdamW over bf16 weights, each with an fp32 master, and fp32 weights (contiguous CUDA tensors, kept by reference and updated
     in place); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to it.  A step whose norm is infinite or NaN is skipped
     (with max_norm = infinity the norm is not taken, and such gradients reach the weights).  `lr` may be changed between steps; in a captured step, pass an
-    fp32 CUDA tensor of one element instead, which the step reads when it runs.  One optimizer serves one stream at a time."""
+    fp32 CUDA tensor of one element instead, which the step reads when it runs.  One optimizer serves one stream at a time; its workspace
+    and the norm that a step returns are its own."""
 
     def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, max_norm=math.inf):
         self.weights = list(weights)
@@ -125,6 +132,9 @@ class AdamW:
         self.exp_avg_sq = [torch.zeros_like(m) for m in self.exp_avg]
         self.steps = torch.zeros((1,), dtype=torch.int64, device=self.device)
         self.status = torch.zeros((1,), dtype=torch.int32, device=self.device)
+        self._norm = torch.zeros((), dtype=torch.float32, device=self.device)
+        self._workspace = _workspace(load_library(), self.device)
+        self._hyper, self._shapes = DirectorAdamW(), listed.shapes
         self._params = (DirectorParam * max(1, len(self.weights)))()
         for i, w in enumerate(self.weights):
             p = self._params[i]
@@ -135,13 +145,14 @@ class AdamW:
     def step(self, grads=None, lr=None) -> torch.Tensor | None:
         """One step on `grads` (a TensorList or a sequence, a tensor or None for each weight; default: the weights' .grad), with
         `lr` in place of the optimizer's if given (a number or an fp32 CUDA tensor of one element).  Returns the gradients' norm before
-        clipping (fp32, no dimensions), None where max_norm is infinite."""
+        clipping (fp32, no dimensions, overwritten by the next step), None where max_norm is infinite."""
         grads = _as_list([w.grad for w in self.weights] if grads is None else grads)
-        if len(grads) != len(self.weights):
-            raise ValueError(f"AdamW.step: {len(grads)} gradients for {len(self.weights)} weights")
-        for i, (g, w) in enumerate(zip(grads.tensors, self.weights)):
-            if g is not None and g.shape != w.shape:
-                raise ValueError(f"AdamW.step: gradient {i} is {tuple(g.shape)}, its weight {tuple(w.shape)}")
+        if grads.shapes != self._shapes:
+            if len(grads) != len(self._shapes):
+                raise ValueError(f"AdamW.step: {len(grads)} gradients for {len(self._shapes)} weights")
+            for i, (g, w) in enumerate(zip(grads.shapes, self._shapes)):
+                if g is not None and g != w:
+                    raise ValueError(f"AdamW.step: gradient {i} is {tuple(g)}, its weight {tuple(w)}")
         if grads.device != self.device:
             raise ValueError(f"AdamW.step: the gradients are on {grads.device}, the weights on {self.device}")
         lib, stream = _begin(self.device)
@@ -151,11 +162,12 @@ class AdamW:
             if lr.dtype is not torch.float32 or lr.numel() != 1 or lr.device != self.device:
                 raise ValueError("AdamW.step: lr has to be a number or an fp32 tensor of one element on the weights' device")
             lr_dev, lr = lr.data_ptr(), 0.0
-        h = DirectorAdamW(lr, *self.betas, self.eps, self.weight_decay, self.max_norm)
-        norm = torch.empty((), dtype=torch.float32, device=self.device) if math.isfinite(self.max_norm) else None
-        _check(lib.director_adamw_step(len(grads), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(),
-                                       norm.data_ptr() if norm is not None else None, self.status.data_ptr(),
-                                       _workspace(lib, self.device).data_ptr(), stream), "director_adamw_step")
+        h = self._hyper
+        h.lr, (h.beta1, h.beta2), h.eps, h.weight_decay, h.max_norm = lr, self.betas, self.eps, self.weight_decay, self.max_norm
+        norm = self._norm if self.max_norm != math.inf else None
+        _check(lib.director_adamw_step(len(self._shapes), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(),
+                                       None if norm is None else norm.data_ptr(), self.status.data_ptr(), self._workspace.data_ptr(), stream),
+               "director_adamw_step")
         _changed(self.weights)
         return norm
 

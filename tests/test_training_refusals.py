@@ -49,7 +49,7 @@ def test_a_tensor_that_is_too_long():
 
 
 def test_missing_and_misaligned_buffers():
-    n, a = _tensors((A, 5, FP32))
+    n, a = _tensors((A, (1 << 20) + 1, FP32))                # one element more than what needs no workspace
     for bad in (None, NORM + 1):
         assert _norm(n, a, norm=bad) == INVALID and _clip(n, a, None, norm=bad) == INVALID
     for bad in (None, WORK + 8):
