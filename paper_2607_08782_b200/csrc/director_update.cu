@@ -4,12 +4,15 @@
 //
 // All of it is HBM-bound elementwise work over the concatenation of the tensors, which is cut into chunks.  A call is
 //   the sum of squares, by a grid that fills the GPU once;
-//   the norm: by one CTA that joins the partial sums, or, where the elementwise part has few CTAs (kFewChunks), by each of them;
-//   the elementwise part, a CTA to a chunk.
-// The norm alone of small tensors is one launch of one cluster (DIRECTOR_SMALL_BYTES).
+//   the norm, by one CTA that joins the partial sums;
+//   the elementwise part, a CTA to a chunk: handed out in order, the CTAs under way stay close together in memory (an update of 210 M
+//   weights 859 us; by a grid that fills the GPU and takes chunks in turns 1018, with three CTAs an SM instead of four 926).
+// Where the chunks are few (kSmallCtas) all of it is one cooperative launch, and the norm alone of small tensors is one cluster's
+// (DIRECTOR_SMALL_BYTES): launches are what those cost.
 // Sums are joined in a fixed order, so that a call gives the same bits again.
 #include "director_common.cuh"
 
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -27,7 +30,10 @@ constexpr int kNormUnroll = 4;                   // 16-byte loads of a thread an
 constexpr int kClusterCtas = 16, kClusterThreads = 1024, kClusterUnroll = 8;
 constexpr int kChunk = kThreads * 8;             // elements of a chunk of the update
 constexpr int kClipUnroll = 4, kClipChunk = kThreads * 8 * kClipUnroll;
-constexpr int kFewChunks = 1200;
+// CTAs of an SM, and so chunks, up to which norm and elementwise part are one cooperative launch.  Against two launches or three, four
+// tensors: a step of 0.26 M weights 8.2 and 11.8 us a call, of 0.5 M 10.3 and 11.8, of 1 M (512 chunks) 12.3 and 11.7; clipping of
+// 1 M 11.4 and 15.7, of 4 M (512 chunks) 13.5 and 15.8, but 12.4 and 9.3 without the host, in a graph.
+constexpr int kSmallCtas = 2;
 constexpr long long kMostElements = 1ll << 40;
 
 // What a call keeps between its launches, in the caller's workspace.
@@ -91,6 +97,17 @@ __device__ __forceinline__ double block_sum(double v) {
 // left the range - it is infinite, or so small that some may have vanished - the same elements are summed in fp64.
 
 constexpr float kSquaresLowest = 1e-26f, kSquaresHighest = 3e38f;
+
+__device__ __forceinline__ double squares_of(const float (&v)[8]) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
+    if (s >= kSquaresLowest && s <= kSquaresHighest) return (double)s;
+    double d = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d = fma((double)v[i], (double)v[i], d);
+    return d;
+}
 
 template <typename T>
 __device__ __forceinline__ float element(uint4 v, int i);
@@ -295,18 +312,8 @@ inline bool whole(const void* p) { return (reinterpret_cast<uintptr_t>(p) & (8 *
 // kind bits of a tensor: its types, and which addresses allow whole accesses
 enum { kGradBf16 = 1, kOutBf16 = 2, kGradWhole = 4, kOutWhole = 8 };
 
-// (scale, decay, rate, root) of the workspace; with SLOTS the clipping factor is worked out from the partial sums instead, and one
-// thread of the launch, the call's only one, finishes.
-template <bool SLOTS>
-__device__ __forceinline__ float4 common_of(const Call& q, int slots) {
-    float4 c = *reinterpret_cast<const float4*>(&q.ws->scale);
-    if (SLOTS) {
-        const double norm = norm_of_slots(q.ws, slots);
-        if (blockIdx.x == 0 && threadIdx.x == 0) finish(q, norm);
-        c.x = scale_of(q, norm);
-    }
-    return c;
-}
+// What all elements have in common: (scale, decay, rate, root) of the workspace.
+__device__ __forceinline__ float4 common_of(const Call& q) { return *reinterpret_cast<const float4*>(&q.ws->scale); }
 
 // The chunks run backwards: the norm has read the last tensors last, and what of them is still in L2 is not fetched again.
 struct Place {
@@ -314,17 +321,46 @@ struct Place {
     long long at, left;          // the chunk's first element, and how many are left from there
 };
 template <typename TABLE>
-__device__ __forceinline__ Place place_of(const TABLE& t, int chunk) {
-    const int c = gridDim.x - 1 - blockIdx.x, k = tensor_of(t, c);
+__device__ __forceinline__ Place place_of(const TABLE& t, int c, int chunk) {
+    const int k = tensor_of(t, c);
     const long long at = (long long)(c - t.first[k]) * chunk;
     return {k, t.kind[k], at, t.numel[k] - at};
+}
+
+// The norm inside a cooperative launch: a CTA sums the squares of its chunk, and every CTA joins the partial sums behind the grid's
+// barrier.  Array 0 of the table holds the gradients.
+template <typename TABLE>
+__device__ __forceinline__ double norm_in_launch(const TABLE& t, const Call& q, const Place& p, int chunk) {
+    double sum = 0.0;
+    for (long long e = threadIdx.x * 8; e < chunk && e < p.left; e += kThreads * 8) {
+        const int some = (int)min(8ll, p.left - e);
+        const bool one = some == 8 && (p.kind & kGradWhole);
+        float v[8];
+        if (p.kind & kGradBf16) {
+            const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.at[0][p.k]) + p.at + e;
+            if (one) load8(g, v);
+            else load_some(g, some, v);
+        } else {
+            const float* g = static_cast<const float*>(t.at[0][p.k]) + p.at + e;
+            if (one) load8(g, v);
+            else load_some(g, some, v);
+        }
+        sum += squares_of(v);
+    }
+    if (q.steps != nullptr && blockIdx.x == gridDim.x - 1 && threadIdx.x == kThreads - 1) start_step(q);
+    sum = block_sum<kThreads>(sum);
+    if (threadIdx.x == 0) q.ws->partial[blockIdx.x] = sum;
+    cooperative_groups::this_grid().sync();
+    const double norm = norm_of_slots(q.ws, gridDim.x);
+    if (blockIdx.x == 0 && threadIdx.x == 0) finish(q, norm);
+    return norm;
 }
 
 // ---- clipping ------------------------------------------------------------------------------------------------------
 
 // A chunk: kClipUnroll x eight elements a thread, asked for together.  FULL: all of them exist; SW, DW: whole accesses.
-template <bool SLOTS, bool FULL, bool SW, bool DW, typename S, typename D>
-__device__ __forceinline__ void clip_chunk(const S* src, D* dst, long long left, const Call& q, int slots) {
+template <bool FULL, bool SW, bool DW, typename S, typename D>
+__device__ __forceinline__ void clip_chunk(const S* src, D* dst, long long left, float scale) {
     float v[kClipUnroll][8];
 #pragma unroll
     for (int u = 0; u < kClipUnroll; ++u) {
@@ -332,7 +368,6 @@ __device__ __forceinline__ void clip_chunk(const S* src, D* dst, long long left,
         if (SW) load8(src + e, v[u]);
         else load_some(src + e, some, v[u]);
     }
-    const float scale = common_of<SLOTS>(q, slots).x;
     const bool same = scale == kNotFinite || scale == 1.0f;
     if (same && static_cast<const void*>(src) == dst) return;
 #pragma unroll
@@ -345,34 +380,43 @@ __device__ __forceinline__ void clip_chunk(const S* src, D* dst, long long left,
         else store_some(dst + e, some, v[u]);
     }
 }
-template <bool SLOTS, typename S, typename D>
-__device__ __forceinline__ void clip_any(const void* src, void* dst, const Place& p, const Call& q, int slots) {
+template <typename S, typename D>
+__device__ __forceinline__ void clip_any(const void* src, void* dst, const Place& p, float scale) {
     const S* s = static_cast<const S*>(src) + p.at;
     D* d = static_cast<D*>(dst) + p.at;
     const bool full = p.left >= kClipChunk;
-    if (full && (p.kind & kGradWhole) && (p.kind & kOutWhole)) clip_chunk<SLOTS, true, true, true>(s, d, p.left, q, slots);
-    else if (full && (p.kind & kOutWhole)) clip_chunk<SLOTS, true, false, true>(s, d, p.left, q, slots);
-    else clip_chunk<SLOTS, false, false, false>(s, d, p.left, q, slots);
+    if (full && (p.kind & kGradWhole) && (p.kind & kOutWhole)) clip_chunk<true, true, true>(s, d, p.left, scale);
+    else if (full && (p.kind & kOutWhole)) clip_chunk<true, false, true>(s, d, p.left, scale);
+    else clip_chunk<false, false, false>(s, d, p.left, scale);
 }
 
-template <int CAP, bool SLOTS>
-__global__ void __launch_bounds__(kThreads, SLOTS ? 3 : 4)
-clip_kernel(const __grid_constant__ Table<2, CAP> t, const Call q, int slots) {
-    chain_prologue();
-    const Place p = place_of(t, kClipChunk);
+template <typename TABLE>
+__device__ __forceinline__ void clip_place(const TABLE& t, const Place& p, float scale) {
     const void* src = t.at[0][p.k];
     void* dst = t.at[1][p.k];
-    if (!SLOTS && src == dst) {
-        const float scale = common_of<false>(q, 0).x;
-        if (scale == kNotFinite || scale == 1.0f) return;
-    }
     if (p.kind & kGradBf16) {
-        if (p.kind & kOutBf16) clip_any<SLOTS, __nv_bfloat16, __nv_bfloat16>(src, dst, p, q, slots);
-        else clip_any<SLOTS, __nv_bfloat16, float>(src, dst, p, q, slots);
+        if (p.kind & kOutBf16) clip_any<__nv_bfloat16, __nv_bfloat16>(src, dst, p, scale);
+        else clip_any<__nv_bfloat16, float>(src, dst, p, scale);
     } else {
-        if (p.kind & kOutBf16) clip_any<SLOTS, float, __nv_bfloat16>(src, dst, p, q, slots);
-        else clip_any<SLOTS, float, float>(src, dst, p, q, slots);
+        if (p.kind & kOutBf16) clip_any<float, __nv_bfloat16>(src, dst, p, scale);
+        else clip_any<float, float>(src, dst, p, scale);
     }
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads, 4)
+clip_kernel(const __grid_constant__ Table<2, CAP> t, const Call q, bool in_place) {
+    chain_prologue();
+    const float scale = common_of(q).x;
+    if (in_place && (scale == kNotFinite || scale == 1.0f)) return;
+    clip_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kClipChunk), scale);
+}
+
+// Few chunks: norm and clipping in one cooperative launch.
+__global__ void __launch_bounds__(kThreads, kSmallCtas)
+clip_small_kernel(const __grid_constant__ Table<2, kFewTensors> t, const Call q) {
+    const Place p = place_of(t, blockIdx.x, kClipChunk);
+    clip_place(t, p, scale_of(q, norm_in_launch(t, q, p, kClipChunk)));
 }
 
 // ---- AdamW ---------------------------------------------------------------------------------------------------------
@@ -387,8 +431,8 @@ struct Arrays {
 };
 
 // A chunk: eight elements a thread.  FULL: all of them exist and the weight and its state allow whole accesses; GW: the gradient does.
-template <bool SLOTS, bool FULL, bool GW, typename G, typename W>
-__device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, const Call& q, const Betas& b, int slots) {
+template <bool FULL, bool GW, typename G, typename W>
+__device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, float4 common, const Betas& b) {
     constexpr bool kMaster = sizeof(W) == 2;
     const long long at = p.at + threadIdx.x * 8;
     const int some = FULL ? 8 : (int)max(0ll, min(8ll, p.left - threadIdx.x * 8));
@@ -407,7 +451,6 @@ __device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, co
     }
     if (GW) load8(grad, g);
     else load_some(grad, some, g);
-    const float4 common = common_of<SLOTS>(q, slots);
     const float scale = common.x, decay = common.y, rate = common.z, root = common.w;
     if (scale == kNotFinite) return;
 #pragma unroll
@@ -429,28 +472,48 @@ __device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, co
         if (kMaster) store_some(weight, some, w);
     }
 }
-template <bool SLOTS, typename G, typename W>
-__device__ __forceinline__ void update_any(const Arrays& a, const Place& p, const Call& q, const Betas& b, int slots) {
+template <typename G, typename W>
+__device__ __forceinline__ void update_any(const Arrays& a, const Place& p, float4 common, const Betas& b) {
     const bool full = p.left >= kChunk && (p.kind & kOutWhole);
-    if (full && (p.kind & kGradWhole)) update_chunk<SLOTS, true, true, G, W>(a, p, q, b, slots);
-    else if (full) update_chunk<SLOTS, true, false, G, W>(a, p, q, b, slots);
-    else update_chunk<SLOTS, false, false, G, W>(a, p, q, b, slots);
+    if (full && (p.kind & kGradWhole)) update_chunk<true, true, G, W>(a, p, common, b);
+    else if (full) update_chunk<true, false, G, W>(a, p, common, b);
+    else update_chunk<false, false, G, W>(a, p, common, b);
 }
 
-template <int CAP, bool SLOTS>
-__global__ void __launch_bounds__(kThreads, SLOTS ? 3 : 4)
-update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas b, int slots) {
-    chain_prologue();
-    const Place p = place_of(t, kChunk);
+template <typename TABLE>
+__device__ __forceinline__ void update_place(const TABLE& t, const Place& p, float4 common, const Betas& b) {
     const Arrays a{t.at[0][p.k], t.at[1][p.k], static_cast<float*>(t.at[2][p.k]), static_cast<float*>(t.at[3][p.k]),
                    static_cast<float*>(t.at[4][p.k])};
     if (p.kind & kGradBf16) {
-        if (p.kind & kOutBf16) update_any<SLOTS, __nv_bfloat16, __nv_bfloat16>(a, p, q, b, slots);
-        else update_any<SLOTS, __nv_bfloat16, float>(a, p, q, b, slots);
+        if (p.kind & kOutBf16) update_any<__nv_bfloat16, __nv_bfloat16>(a, p, common, b);
+        else update_any<__nv_bfloat16, float>(a, p, common, b);
     } else {
-        if (p.kind & kOutBf16) update_any<SLOTS, float, __nv_bfloat16>(a, p, q, b, slots);
-        else update_any<SLOTS, float, float>(a, p, q, b, slots);
+        if (p.kind & kOutBf16) update_any<float, __nv_bfloat16>(a, p, common, b);
+        else update_any<float, float>(a, p, common, b);
     }
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads, 4)
+update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas b) {
+    chain_prologue();
+    update_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kChunk), common_of(q), b);
+}
+
+// Few chunks: norm and step in one cooperative launch, the state on its way to L2 while the norm is taken.
+__global__ void __launch_bounds__(kThreads, kSmallCtas)
+update_small_kernel(const __grid_constant__ Table<5, kFewTensors> t, const Call q, const Betas b) {
+    const Place p = place_of(t, blockIdx.x, kChunk);
+    if (threadIdx.x * 8 < p.left) {
+        const long long at = p.at + threadIdx.x * 8;
+        const int w32 = (p.kind & kOutBf16) ? 2 : 1;
+#pragma unroll
+        for (int i = 2; i < 5; ++i) asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const float*>(t.at[i == 2 ? w32 : i][p.k]) + at));
+    }
+    const double norm = norm_in_launch(t, q, p, kChunk);
+    float4 common = common_of(q);
+    common.x = scale_of(q, norm);
+    update_place(t, p, common, b);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -503,18 +566,27 @@ int check_tensors(int32_t n, const director_tensor* g) {
 }
 
 template <typename... KArgs>
-cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, unsigned threads, cudaStream_t st, const KArgs&... args) {
+cudaError_t launch_as(bool cooperative, void (*kernel)(KArgs...), unsigned grid, unsigned threads, cudaStream_t st, const KArgs&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(threads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    if (cooperative) {
+        attr[0].id = cudaLaunchAttributeCooperative;
+        attr[0].val.cooperative = 1;
+    } else {
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = chain_allowed(st) ? 1 : 0;
+    cfg.numAttrs = cooperative || chain_allowed(st) ? 1 : 0;
     void* at[] = {const_cast<void*>(static_cast<const void*>(&args))...};      // the tables are copied once, by the runtime
     return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), at);
+}
+template <typename... KArgs>
+cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, unsigned threads, cudaStream_t st, const KArgs&... args) {
+    return launch_as(false, kernel, grid, threads, st, args...);
 }
 
 // Puts the tensors i = 0 .. n-1 that have chunks (chunks_of(i)) into tables (fill(table, slot, i)) and launches each table that is
@@ -566,11 +638,15 @@ int norm_tables(int n, const director_tensor* g, int per, Run&& run) {
         run);
 }
 
+bool sm_count(int* out) {
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
+}
+
 // Leaves *slots partial sums in the workspace.
 int sum_squares(int n, const director_tensor* g, const Call& q, int* slots, cudaStream_t st) {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return DIRECTOR_ERR_CUDA;
+    int sms = 0;
+    if (!sm_count(&sms)) return DIRECTOR_ERR_CUDA;
     *slots = 0;
     const auto run = [&](auto kernel, const auto& t, int chunks) {
         const int grid = std::max(1, std::min({chunks, kNormCtas * sms, kSlots}));
@@ -586,21 +662,24 @@ int sum_squares(int n, const director_tensor* g, const Call& q, int* slots, cuda
 
 int finish_call(const Call& q, int slots, cudaStream_t st) { return cuda_status(launch(finish_kernel, 1u, kThreads, st, q, slots)); }
 
-// Sums the squares for a call whose elementwise part has chunks of `chunk` elements, and joins the sums unless those do it; *slots: how many
-// they have to join.
-int norm_for(int n, const director_tensor* g, int chunk, const Call& q, int* slots, cudaStream_t st) {
-    long long chunks = 0;
-    for (int i = 0; i < n; ++i) chunks += (g[i].numel + chunk - 1) / chunk;
-    int rc = sum_squares(n, g, q, slots, st);
-    if (rc == DIRECTOR_OK && (n > kFewTensors || chunks == 0 || chunks > kFewChunks)) {
-        rc = finish_call(q, *slots, st);
-        *slots = 0;
-    }
-    return rc;
+// The norm, finished.
+int take_norm(int n, const director_tensor* g, const Call& q, cudaStream_t st) {
+    int slots = 0;
+    const int rc = sum_squares(n, g, q, &slots, st);
+    return rc != DIRECTOR_OK ? rc : finish_call(q, slots, st);
 }
 
-template <int CAP, bool SLOTS>
-int clip_launches(int n, const director_tensor* g, const director_tensor* out, const Call& q, int slots, cudaStream_t st) {
+// Whether the norm and the elementwise part, of chunks of `chunk` elements, go into one launch: all CTAs run at once.
+bool in_one_launch(int n, const director_tensor* g, int chunk) {
+    int sms = 0;
+    if (n > kFewTensors || !sm_count(&sms)) return false;
+    long long chunks = 0;
+    for (int i = 0; i < n; ++i) chunks += (g[i].numel + chunk - 1) / chunk;
+    return chunks > 0 && chunks <= std::min(kSmallCtas * sms, kSlots);
+}
+
+template <int CAP, typename Run>
+int clip_tables(int n, const director_tensor* g, const director_tensor* out, Run&& run) {
     return in_tables<Table<2, CAP>, CAP>(
         n, [&](int i) { return (g[i].numel + kClipChunk - 1) / kClipChunk; },
         [&](Table<2, CAP>& t, int k, int i) {
@@ -612,13 +691,17 @@ int clip_launches(int n, const director_tensor* g, const director_tensor* out, c
                                         ((sb ? whole<__nv_bfloat16>(g[i].data) : whole<float>(g[i].data)) ? kGradWhole : 0) |
                                         ((db ? whole<__nv_bfloat16>(out[i].data) : whole<float>(out[i].data)) ? kOutWhole : 0));
         },
-        [&](const Table<2, CAP>& t, int chunks) {
-            return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(clip_kernel<CAP, SLOTS>, (unsigned)chunks, kThreads, st, t, q, slots));
-        });
+        run);
+}
+template <int CAP>
+int clip_launches(int n, const director_tensor* g, const director_tensor* out, const Call& q, cudaStream_t st) {
+    return clip_tables<CAP>(n, g, out, [&](const Table<2, CAP>& t, int chunks) {
+        return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(clip_kernel<CAP>, (unsigned)chunks, kThreads, st, t, q, out == g));
+    });
 }
 
-template <int CAP, bool SLOTS>
-int update_launches(int n, const director_tensor* g, const director_param* p, const Call& q, const Betas& b, int slots, cudaStream_t st) {
+template <int CAP, typename Run>
+int update_tables(int n, const director_tensor* g, const director_param* p, Run&& run) {
     return in_tables<Table<5, CAP>, CAP>(
         n, [&](int i) { return (g[i].numel + kChunk - 1) / kChunk; },
         [&](Table<5, CAP>& t, int k, int i) {
@@ -634,9 +717,13 @@ int update_launches(int n, const director_tensor* g, const director_param* p, co
             t.kind[k] = (unsigned char)((gb ? kGradBf16 : 0) | (wb ? kOutBf16 : 0) | (state ? kOutWhole : 0) |
                                         ((gb ? whole<__nv_bfloat16>(g[i].data) : whole<float>(g[i].data)) ? kGradWhole : 0));
         },
-        [&](const Table<5, CAP>& t, int chunks) {
-            return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(update_kernel<CAP, SLOTS>, (unsigned)chunks, kThreads, st, t, q, b, slots));
-        });
+        run);
+}
+template <int CAP>
+int update_launches(int n, const director_tensor* g, const director_param* p, const Call& q, const Betas& b, cudaStream_t st) {
+    return update_tables<CAP>(n, g, p, [&](const Table<5, CAP>& t, int chunks) {
+        return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(update_kernel<CAP>, (unsigned)chunks, kThreads, st, t, q, b));
+    });
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -666,9 +753,7 @@ int director_grad_norm(int32_t n, const director_tensor* grads, float* norm, voi
     Call q = {};
     q.ws = static_cast<Workspace*>(workspace);
     q.norm = norm;
-    int slots = 0;
-    const int done = sum_squares(n, grads, q, &slots, st);
-    return done != DIRECTOR_OK ? done : finish_call(q, slots, st);
+    return take_norm(n, grads, q, st);
 }
 
 int director_clip_grads(int32_t n, const director_tensor* grads, const director_tensor* out, float max_norm, float* norm,
@@ -694,12 +779,13 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
     q.ws = static_cast<Workspace*>(workspace);
     q.norm = norm;
     q.max_norm = max_norm;
-    int slots = 0;
-    rc = norm_for(n, grads, kClipChunk, q, &slots, st);
+    if (in_one_launch(n, grads, kClipChunk))
+        return clip_tables<kFewTensors>(n, grads, out, [&](const Table<2, kFewTensors>& t, int chunks) {
+            return cuda_status(launch_as(true, clip_small_kernel, (unsigned)chunks, kThreads, st, t, q));
+        });
+    rc = take_norm(n, grads, q, st);
     if (rc != DIRECTOR_OK) return rc;
-    return slots > 0          ? clip_launches<kFewTensors, true>(n, grads, out, q, slots, st)
-           : n <= kFewTensors ? clip_launches<kFewTensors, false>(n, grads, out, q, 0, st)
-                              : clip_launches<kClipTensors, false>(n, grads, out, q, 0, st);
+    return n <= kFewTensors ? clip_launches<kFewTensors>(n, grads, out, q, st) : clip_launches<kClipTensors>(n, grads, out, q, st);
 }
 
 int director_adamw_step(int32_t n, const director_tensor* grads, const director_param* params, const director_adamw* h,
@@ -743,16 +829,21 @@ int director_adamw_step(int32_t n, const director_tensor* grads, const director_
     q.lr = h->lr, q.beta1 = h->beta1, q.beta2 = h->beta2, q.weight_decay = h->weight_decay;
     q.lr_dev = lr;
     q.status = device_status;
-    int slots = 0;
-    rc = norm != nullptr || std::isfinite(h->max_norm) ? norm_for(n, grads, kChunk, q, &slots, st) : finish_call(q, 0, st);
-    if (rc != DIRECTOR_OK) return rc;
     Betas b = {};
     b.beta1 = (float)h->beta1, b.rest1 = (float)(1.0 - h->beta1);
     b.beta2 = (float)h->beta2, b.rest2 = (float)(1.0 - h->beta2);
     b.eps = (float)h->eps;
-    return slots > 0          ? update_launches<kFewTensors, true>(n, grads, params, q, b, slots, st)
-           : n <= kFewTensors ? update_launches<kFewTensors, false>(n, grads, params, q, b, 0, st)
-                              : update_launches<kUpdateTensors, false>(n, grads, params, q, b, 0, st);
+    if (norm != nullptr || std::isfinite(h->max_norm)) {
+        if (in_one_launch(n, grads, kChunk))
+            return update_tables<kFewTensors>(n, grads, params, [&](const Table<5, kFewTensors>& t, int chunks) {
+                return cuda_status(launch_as(true, update_small_kernel, (unsigned)chunks, kThreads, st, t, q, b));
+            });
+        rc = take_norm(n, grads, q, st);
+    } else {
+        rc = finish_call(q, 0, st);
+    }
+    if (rc != DIRECTOR_OK) return rc;
+    return n <= kFewTensors ? update_launches<kFewTensors>(n, grads, params, q, b, st) : update_launches<kUpdateTensors>(n, grads, params, q, b, st);
 }
 
 }  // extern "C"

@@ -72,9 +72,11 @@ def _begin(device: torch.device):
     return lib, binding._stream()
 
 
-def _workspace(lib, device) -> torch.Tensor:
-    # made anew by each call, on its stream: calls that overlap, captured ones too, never share one
-    return torch.empty(lib.director_grad_workspace_bytes(), dtype=torch.uint8, device=device)
+def _norm_and_workspace(lib, device):
+    """One allocation of the two.  Made anew by each call, on its stream: calls that overlap, captured ones too, never share it."""
+    words = lib.director_grad_workspace_bytes() // 4
+    room = torch.empty(words + 1, dtype=torch.float32, device=device)
+    return room[words], room.data_ptr()
 
 
 def _changed(tensors):
@@ -86,10 +88,11 @@ def grad_norm(grads) -> torch.Tensor:
     """The square root of the sum of squares over all elements of all tensors (a TensorList or a sequence): fp32, no dimensions."""
     grads = _as_list(grads)
     lib, stream = _begin(grads.device)
-    norm = torch.empty((), dtype=torch.float32, device=grads.device)
-    workspace = None if grads.small else _workspace(lib, grads.device)
-    _check(lib.director_grad_norm(len(grads), grads.array, norm.data_ptr(), None if workspace is None else workspace.data_ptr(), stream),
-           "director_grad_norm")
+    if grads.small:
+        norm, workspace = torch.empty((), dtype=torch.float32, device=grads.device), None
+    else:
+        norm, workspace = _norm_and_workspace(lib, grads.device)
+    _check(lib.director_grad_norm(len(grads), grads.array, norm.data_ptr(), workspace, stream), "director_grad_norm")
     return norm
 
 
@@ -106,9 +109,8 @@ def clip_grads(grads, max_norm: float, out=None) -> torch.Tensor:
     if out.device != grads.device:
         raise ValueError(f"clip_grads: the gradients are on {grads.device}, out is on {out.device}")
     lib, stream = _begin(grads.device)
-    norm, workspace = torch.empty((), dtype=torch.float32, device=grads.device), _workspace(lib, grads.device)
-    _check(lib.director_clip_grads(len(grads), grads.array, out.array, max_norm, norm.data_ptr(), workspace.data_ptr(), stream),
-           "director_clip_grads")
+    norm, workspace = _norm_and_workspace(lib, grads.device)
+    _check(lib.director_clip_grads(len(grads), grads.array, out.array, max_norm, norm.data_ptr(), workspace, stream), "director_clip_grads")
     _changed(out.tensors)
     return norm
 
@@ -133,7 +135,7 @@ class AdamW:
         self.steps = torch.zeros((1,), dtype=torch.int64, device=self.device)
         self.status = torch.zeros((1,), dtype=torch.int32, device=self.device)
         self._norm = torch.zeros((), dtype=torch.float32, device=self.device)
-        self._workspace = _workspace(load_library(), self.device)
+        self._workspace = torch.empty(load_library().director_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
         self._hyper, self._shapes = DirectorAdamW(), listed.shapes
         self._params = (DirectorParam * max(1, len(self.weights)))()
         for i, w in enumerate(self.weights):

@@ -217,6 +217,26 @@ def test_steps(wtypes, gtypes, shift, decay, max_norm):
     assert opt.last_status() == 0
 
 
+@pytest.mark.parametrize("extra", [-2049, -1, 0, 1, 2049])
+def test_sizes_where_one_launch_ends(extra):
+    """A call is one launch up to two chunks (2048 weights of a step, 8192 gradients of clip_grads) for every SM."""
+    import torch
+    from paper_2607_08782_b200.training import clip_grads
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for chunk in (2048, 8192):
+        n = 2 * sms * chunk + extra
+        sizes = [n - 3 * chunk, chunk, 2 * chunk]
+        opt, grads = _optimizer(sizes, "bf", "fb", 21, lr=1e-3, max_norm=0.5)
+        for k in range(2):
+            ref, g = _Reference(opt), grads(k)
+            opt.step(g)
+            ref.step(g, 1e-3, 0.5)
+        out = [torch.empty_like(t, dtype=torch.float32) for t in g]
+        want = _norm64(g)
+        assert abs(clip_grads(g, 0.25 * want, out=out).item() - want) <= NORM_TOL * want
+        assert all(((o.double() - 0.25 * t.double()).abs() <= (NORM_TOL + 4 * 2.0 ** -24) * t.double().abs()).all() for o, t in zip(out, g))
+
+
 @pytest.mark.parametrize("count", [17, 160, 163, 500])
 def test_a_step_of_many_tensors(count):
     sizes = [(i * 53) % 2203 for i in range(count)]
