@@ -38,19 +38,33 @@ __device__ __forceinline__ void load_row(const float* __restrict__ row, int E, i
     }
 }
 
-// x -> exp(x - max); returns their sum, NaN for a row with a NaN, a +inf or nothing but -inf.  __expf's error grows with the
-// distance from the maximum, 2^-24 a unit: what it moves is as small as exp(-distance).
+__device__ __forceinline__ float power_of_two(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// x -> exp(x - max), up to a factor that all have in common; returns their sum, NaN for a row with a NaN, a +inf or nothing but
+// -inf.  One product and one power of two: 2^(x log2(e) - max log2(e)).  The second product's rounding is the common factor; the
+// difference's is 2^-24 of the distance from the maximum, in the exponent: what it moves is as small as exp(-distance).
 template <int LPR>
 __device__ __forceinline__ float softmax_terms(float (&x)[kVals]) {
+    constexpr float kLog2E = 1.4426950408889634f;
     float m = x[0];
 #pragma unroll
     for (int i = 1; i < kVals; ++i) m = fmaxf(m, x[i]);
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    if (fabsf(m) > 1e37f) {                                // max log2(e) would leave the range
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) x[i] -= m;
+        m -= m;
+    }
+    m *= kLog2E;
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < kVals; ++i) {
-        x[i] = __expf(x[i] - m);
+        x[i] = power_of_two(fmaf(x[i], kLog2E, -m));
         s += x[i];
     }
 #pragma unroll
@@ -117,7 +131,7 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
         for (int i = 0; i < kVals; ++i) x[i] = next[i];
         next_live = fetch(base + kWarps * kGroups);
         const float s = softmax_terms<LPR>(x);
-        const float inv = 1.0f / s;
+        const float inv = __fdividef(1.0f, s);
         if (live) {
             valid += sub == 0;
             if (s > 0.0f) {
@@ -226,17 +240,20 @@ balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restr
         const int row = r0 + base + lane / LPR;
         const float s = softmax_terms<LPR>(x);
         const bool good = live && s > 0.0f;
-        if (live && !good && sub == 0) director_set_status(status, DIRECTOR_ERR_NONFINITE);
+        if (!good) {                                       // no gradient: padding, or a row that is not finite
+            if (live && sub == 0) director_set_status(status, DIRECTOR_ERR_NONFINITE);
+#pragma unroll
+            for (int i = 0; i < kVals; ++i) x[i] = 0.0f;
+        }
         float mean = 0.0f;
 #pragma unroll
         for (int i = 0; i < kVals; ++i) mean = fmaf(x[i], f[i], mean);
 #pragma unroll
         for (int o = 1; o < LPR; o <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, o);
-        const float inv = 1.0f / s, scale = factor * inv;
-        mean *= inv;
+        const float inv = good ? __fdividef(1.0f, s) : 0.0f, scale = factor * inv, shift = mean * inv * scale;
         float d[kVals];
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) d[i] = good ? scale * x[i] * (f[i] - mean) : 0.0f;
+        for (int i = 0; i < kVals; ++i) d[i] = x[i] * fmaf(f[i], scale, -shift);
         const bool here = base + lane / LPR < n_rows;
         live = fetch(base + kWarps * kGroups);
         if (!here) continue;

@@ -293,24 +293,35 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
+// Elements [lo, hi) of eight, the others zero; `whole`: the address allows whole accesses.
 template <typename T>
-__device__ __forceinline__ void load_some(const T* p, int n, float (&v)[8]) {
+__device__ __forceinline__ void load_some(const T* p, int lo, int hi, bool whole, float (&v)[8]) {
+    if (whole && lo == 0 && hi == 8) {
+        load8(p, v);
+        return;
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_float(p[i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = i >= lo && i < hi ? to_float(p[i]) : 0.0f;
 }
 __device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_one(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 template <typename T>
-__device__ __forceinline__ void store_some(T* p, int n, const float (&v)[8]) {
+__device__ __forceinline__ void store_some(T* p, int lo, int hi, bool whole, const float (&v)[8]) {
+    if (whole && lo == 0 && hi == 8) {
+        store8(p, v);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (i < n) store_one(p + i, v[i]);
+        if (i >= lo && i < hi) store_one(p + i, v[i]);
 }
+// Elements of an array in front of its address that would make whole accesses of it possible from there.
 template <typename T>
-inline bool whole(const void* p) { return (reinterpret_cast<uintptr_t>(p) & (8 * sizeof(T) - 1)) == 0; }
+inline int pad_of(const void* p) { return (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % 8); }
+inline int pad_of(const void* p, int type) { return type == DIRECTOR_BF16 ? pad_of<__nv_bfloat16>(p) : pad_of<float>(p); }
 
-// kind bits of a tensor: its types, and which addresses allow whole accesses
-enum { kGradBf16 = 1, kOutBf16 = 2, kGradWhole = 4, kOutWhole = 8 };
+// kind of a tensor: its types, which addresses allow whole accesses, and how many elements in front of it its first chunk begins
+enum { kGradBf16 = 1, kOutBf16 = 2, kGradWhole = 4, kOutWhole = 8, kStateWhole = 16, kPadShift = 5 };
 
 // What all elements have in common: (scale, decay, rate, root) of the workspace.
 __device__ __forceinline__ float4 common_of(const Call& q) { return *reinterpret_cast<const float4*>(&q.ws->scale); }
@@ -318,12 +329,15 @@ __device__ __forceinline__ float4 common_of(const Call& q) { return *reinterpret
 // The chunks run backwards: the norm has read the last tensors last, and what of them is still in L2 is not fetched again.
 struct Place {
     int k, kind;                 // tensor
-    long long at, left;          // the chunk's first element, and how many are left from there
+    long long at, end;           // the chunk's first element (negative in front of the tensor), and the tensor's end from there
+    __device__ bool full(int chunk) const { return at >= 0 && end >= chunk; }
+    __device__ int lo(int e) const { return at + e >= 0 ? 0 : (int)min(8ll, -(at + e)); }         // of the eight elements at e
+    __device__ int hi(int e) const { return (int)max(0ll, min(8ll, end - e)); }
 };
 template <typename TABLE>
 __device__ __forceinline__ Place place_of(const TABLE& t, int c, int chunk) {
     const int k = tensor_of(t, c);
-    const long long at = (long long)(c - t.first[k]) * chunk;
+    const long long at = (long long)(c - t.first[k]) * chunk - (t.kind[k] >> kPadShift);
     return {k, t.kind[k], at, t.numel[k] - at};
 }
 
@@ -332,19 +346,10 @@ __device__ __forceinline__ Place place_of(const TABLE& t, int c, int chunk) {
 template <typename TABLE>
 __device__ __forceinline__ double norm_in_launch(const TABLE& t, const Call& q, const Place& p, int chunk) {
     double sum = 0.0;
-    for (long long e = threadIdx.x * 8; e < chunk && e < p.left; e += kThreads * 8) {
-        const int some = (int)min(8ll, p.left - e);
-        const bool one = some == 8 && (p.kind & kGradWhole);
+    for (int e = threadIdx.x * 8; e < chunk && e < p.end; e += kThreads * 8) {
         float v[8];
-        if (p.kind & kGradBf16) {
-            const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.at[0][p.k]) + p.at + e;
-            if (one) load8(g, v);
-            else load_some(g, some, v);
-        } else {
-            const float* g = static_cast<const float*>(t.at[0][p.k]) + p.at + e;
-            if (one) load8(g, v);
-            else load_some(g, some, v);
-        }
+        if (p.kind & kGradBf16) load_some(static_cast<const __nv_bfloat16*>(t.at[0][p.k]) + p.at + e, p.lo(e), p.hi(e), p.kind & kGradWhole, v);
+        else load_some(static_cast<const float*>(t.at[0][p.k]) + p.at + e, p.lo(e), p.hi(e), p.kind & kGradWhole, v);
         sum += squares_of(v);
     }
     if (q.steps != nullptr && blockIdx.x == gridDim.x - 1 && threadIdx.x == kThreads - 1) start_step(q);
@@ -358,36 +363,37 @@ __device__ __forceinline__ double norm_in_launch(const TABLE& t, const Call& q, 
 
 // ---- clipping ------------------------------------------------------------------------------------------------------
 
-// A chunk: kClipUnroll x eight elements a thread, asked for together.  FULL: all of them exist; SW, DW: whole accesses.
-template <bool FULL, bool SW, bool DW, typename S, typename D>
-__device__ __forceinline__ void clip_chunk(const S* src, D* dst, long long left, float scale) {
+// A chunk: kClipUnroll x eight elements a thread, asked for together.  FULL: all of them exist, and go out whole; SW: and come in whole.
+template <bool FULL, bool SW, typename S, typename D>
+__device__ __forceinline__ void clip_chunk(const S* src, D* dst, const Place& p, float scale) {
     float v[kClipUnroll][8];
 #pragma unroll
     for (int u = 0; u < kClipUnroll; ++u) {
-        const int e = (u * kThreads + threadIdx.x) * 8, some = FULL ? 8 : (int)max(0ll, min(8ll, left - e));
-        if (SW) load8(src + e, v[u]);
-        else load_some(src + e, some, v[u]);
+        const int e = (u * kThreads + threadIdx.x) * 8;
+        if (FULL && SW) load8(src + e, v[u]);
+        else if (FULL) load_some(src + e, 0, 8, false, v[u]);
+        else load_some(src + e, p.lo(e), p.hi(e), p.kind & kGradWhole, v[u]);
     }
     const bool same = scale == kNotFinite || scale == 1.0f;
     if (same && static_cast<const void*>(src) == dst) return;
 #pragma unroll
     for (int u = 0; u < kClipUnroll; ++u) {
-        const int e = (u * kThreads + threadIdx.x) * 8, some = FULL ? 8 : (int)max(0ll, min(8ll, left - e));
+        const int e = (u * kThreads + threadIdx.x) * 8;
         if (!same)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[u][i] *= scale;
-        if (DW) store8(dst + e, v[u]);
-        else store_some(dst + e, some, v[u]);
+        if (FULL) store8(dst + e, v[u]);
+        else store_some(dst + e, p.lo(e), p.hi(e), p.kind & kOutWhole, v[u]);
     }
 }
 template <typename S, typename D>
 __device__ __forceinline__ void clip_any(const void* src, void* dst, const Place& p, float scale) {
     const S* s = static_cast<const S*>(src) + p.at;
     D* d = static_cast<D*>(dst) + p.at;
-    const bool full = p.left >= kClipChunk;
-    if (full && (p.kind & kGradWhole) && (p.kind & kOutWhole)) clip_chunk<true, true, true>(s, d, p.left, scale);
-    else if (full && (p.kind & kOutWhole)) clip_chunk<true, false, true>(s, d, p.left, scale);
-    else clip_chunk<false, false, false>(s, d, p.left, scale);
+    const bool full = p.full(kClipChunk) && (p.kind & kOutWhole);
+    if (full && (p.kind & kGradWhole)) clip_chunk<true, true>(s, d, p, scale);
+    else if (full) clip_chunk<true, false>(s, d, p, scale);
+    else clip_chunk<false, false>(s, d, p, scale);
 }
 
 template <typename TABLE>
@@ -430,28 +436,22 @@ struct Arrays {
     float *master, *exp_avg, *exp_avg_sq;
 };
 
-// A chunk: eight elements a thread.  FULL: all of them exist and the weight and its state allow whole accesses; GW: the gradient does.
-template <bool FULL, bool GW, typename G, typename W>
+// A chunk: eight elements a thread.  FULL: all of them exist and the state's addresses allow whole accesses; GW, WW: the gradient's and
+// the weight's do.
+template <bool FULL, bool GW, bool WW, typename G, typename W>
 __device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, float4 common, const Betas& b) {
     constexpr bool kMaster = sizeof(W) == 2;
-    const long long at = p.at + threadIdx.x * 8;
-    const int some = FULL ? 8 : (int)max(0ll, min(8ll, p.left - threadIdx.x * 8));
-    const G* const grad = static_cast<const G*>(a.grad) + at;
-    W* const weight = static_cast<W*>(a.weight) + at;
-    float* const w32 = kMaster ? a.master + at : reinterpret_cast<float*>(weight);
-    float g[8], w[8], m[8], v[8];
-    if (FULL) {
-        load8(a.exp_avg + at, m);
-        load8(a.exp_avg_sq + at, v);
-        load8(w32, w);
-    } else {
-        load_some(a.exp_avg + at, some, m);
-        load_some(a.exp_avg_sq + at, some, v);
-        load_some(w32, some, w);
-    }
-    if (GW) load8(grad, g);
-    else load_some(grad, some, g);
+    const int e = threadIdx.x * 8;
+    const long long at = p.at + e;
+    const int hi = FULL ? 8 : p.hi(e);
+    const bool state = FULL || (p.kind & kStateWhole), grad = FULL ? GW : (p.kind & kGradWhole) != 0, weight = FULL ? WW : (p.kind & kOutWhole) != 0;
     const float scale = common.x, decay = common.y, rate = common.z, root = common.w;
+    float g[8], w[8], m[8], v[8];
+    load_some(a.exp_avg + at, 0, hi, state, m);
+    load_some(a.exp_avg_sq + at, 0, hi, state, v);
+    if (kMaster) load_some(a.master + at, 0, hi, state, w);
+    else load_some(static_cast<const float*>(a.weight) + at, 0, hi, weight, w);
+    load_some(static_cast<const G*>(a.grad) + at, 0, hi, grad, g);
     if (scale == kNotFinite) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -460,24 +460,19 @@ __device__ __forceinline__ void update_chunk(const Arrays& a, const Place& p, fl
         v[i] = fmaf(b.beta2, v[i], b.rest2 * x * x);
         w[i] = fmaf(-decay, w[i], w[i]) - rate * m[i] / fmaf(sqrtf(v[i]), root, b.eps);
     }
-    if (FULL) {
-        store8(a.exp_avg + at, m);
-        store8(a.exp_avg_sq + at, v);
-        store8(w32, w);
-        if (kMaster) store8(weight, w);
-    } else {
-        store_some(a.exp_avg + at, some, m);
-        store_some(a.exp_avg_sq + at, some, v);
-        store_some(w32, some, w);
-        if (kMaster) store_some(weight, some, w);
-    }
+    store_some(a.exp_avg + at, 0, hi, state, m);
+    store_some(a.exp_avg_sq + at, 0, hi, state, v);
+    if (kMaster) store_some(a.master + at, 0, hi, state, w);
+    store_some(static_cast<W*>(a.weight) + at, 0, hi, weight, w);
 }
 template <typename G, typename W>
 __device__ __forceinline__ void update_any(const Arrays& a, const Place& p, float4 common, const Betas& b) {
-    const bool full = p.left >= kChunk && (p.kind & kOutWhole);
-    if (full && (p.kind & kGradWhole)) update_chunk<true, true, G, W>(a, p, common, b);
-    else if (full) update_chunk<true, false, G, W>(a, p, common, b);
-    else update_chunk<false, false, G, W>(a, p, common, b);
+    const bool gw = p.kind & kGradWhole, ww = p.kind & kOutWhole;
+    if (!p.full(kChunk) || !(p.kind & kStateWhole)) update_chunk<false, false, false, G, W>(a, p, common, b);
+    else if (gw && ww) update_chunk<true, true, true, G, W>(a, p, common, b);
+    else if (ww) update_chunk<true, false, true, G, W>(a, p, common, b);
+    else if (gw) update_chunk<true, true, false, G, W>(a, p, common, b);
+    else update_chunk<true, false, false, G, W>(a, p, common, b);
 }
 
 template <typename TABLE>
@@ -504,7 +499,7 @@ update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas
 __global__ void __launch_bounds__(kThreads, kSmallCtas)
 update_small_kernel(const __grid_constant__ Table<5, kFewTensors> t, const Call q, const Betas b) {
     const Place p = place_of(t, blockIdx.x, kChunk);
-    if (threadIdx.x * 8 < p.left) {
+    if (threadIdx.x * 8 < p.end) {
         const long long at = p.at + threadIdx.x * 8;
         const int w32 = (p.kind & kOutBf16) ? 2 : 1;
 #pragma unroll
@@ -669,27 +664,31 @@ int take_norm(int n, const director_tensor* g, const Call& q, cudaStream_t st) {
     return rc != DIRECTOR_OK ? rc : finish_call(q, slots, st);
 }
 
-// Whether the norm and the elementwise part, of chunks of `chunk` elements, go into one launch: all CTAs run at once.
-bool in_one_launch(int n, const director_tensor* g, int chunk) {
+// Whether the norm and the elementwise part, of chunks_of(i) chunks a tensor, go into one launch: all CTAs run at once.
+template <typename Chunks>
+bool in_one_launch(int n, Chunks&& chunks_of) {
     int sms = 0;
     if (n > kFewTensors || !sm_count(&sms)) return false;
     long long chunks = 0;
-    for (int i = 0; i < n; ++i) chunks += (g[i].numel + chunk - 1) / chunk;
+    for (int i = 0; i < n; ++i) chunks += chunks_of(i);
     return chunks > 0 && chunks <= std::min(kSmallCtas * sms, kSlots);
 }
 
+// Chunks of a gradient to be clipped into `out`: they begin where that allows whole accesses.
+long long clip_chunks(const director_tensor& out) {
+    return out.numel == 0 ? 0 : (out.numel + pad_of(out.data, out.type) + kClipChunk - 1) / kClipChunk;
+}
 template <int CAP, typename Run>
 int clip_tables(int n, const director_tensor* g, const director_tensor* out, Run&& run) {
     return in_tables<Table<2, CAP>, CAP>(
-        n, [&](int i) { return (g[i].numel + kClipChunk - 1) / kClipChunk; },
+        n, [&](int i) { return clip_chunks(out[i]); },
         [&](Table<2, CAP>& t, int k, int i) {
             t.at[0][k] = g[i].data;
             t.at[1][k] = out[i].data;
             t.numel[k] = g[i].numel;
-            const bool sb = g[i].type == DIRECTOR_BF16, db = out[i].type == DIRECTOR_BF16;
-            t.kind[k] = (unsigned char)((sb ? kGradBf16 : 0) | (db ? kOutBf16 : 0) |
-                                        ((sb ? whole<__nv_bfloat16>(g[i].data) : whole<float>(g[i].data)) ? kGradWhole : 0) |
-                                        ((db ? whole<__nv_bfloat16>(out[i].data) : whole<float>(out[i].data)) ? kOutWhole : 0));
+            const int pad = pad_of(out[i].data, out[i].type);
+            t.kind[k] = (unsigned char)((g[i].type == DIRECTOR_BF16 ? kGradBf16 : 0) | (out[i].type == DIRECTOR_BF16 ? kOutBf16 : 0) |
+                                        (pad_of(g[i].data, g[i].type) == pad ? kGradWhole : 0) | kOutWhole | pad << kPadShift);
         },
         run);
 }
@@ -700,10 +699,11 @@ int clip_launches(int n, const director_tensor* g, const director_tensor* out, c
     });
 }
 
+long long update_chunks(const director_tensor& g) { return (g.numel + kChunk - 1) / kChunk; }
 template <int CAP, typename Run>
 int update_tables(int n, const director_tensor* g, const director_param* p, Run&& run) {
     return in_tables<Table<5, CAP>, CAP>(
-        n, [&](int i) { return (g[i].numel + kChunk - 1) / kChunk; },
+        n, [&](int i) { return update_chunks(g[i]); },
         [&](Table<5, CAP>& t, int k, int i) {
             t.at[0][k] = g[i].data;
             t.at[1][k] = p[i].weight;
@@ -711,11 +711,10 @@ int update_tables(int n, const director_tensor* g, const director_param* p, Run&
             t.at[3][k] = p[i].exp_avg;
             t.at[4][k] = p[i].exp_avg_sq;
             t.numel[k] = g[i].numel;
-            const bool gb = g[i].type == DIRECTOR_BF16, wb = p[i].type == DIRECTOR_BF16;
-            const bool state = whole<float>(p[i].exp_avg) && whole<float>(p[i].exp_avg_sq) &&
-                               (wb ? whole<__nv_bfloat16>(p[i].weight) && whole<float>(p[i].master) : whole<float>(p[i].weight));
-            t.kind[k] = (unsigned char)((gb ? kGradBf16 : 0) | (wb ? kOutBf16 : 0) | (state ? kOutWhole : 0) |
-                                        ((gb ? whole<__nv_bfloat16>(g[i].data) : whole<float>(g[i].data)) ? kGradWhole : 0));
+            const bool wb = p[i].type == DIRECTOR_BF16;
+            const bool state = pad_of<float>(p[i].exp_avg) == 0 && pad_of<float>(p[i].exp_avg_sq) == 0 && (!wb || pad_of<float>(p[i].master) == 0);
+            t.kind[k] = (unsigned char)((g[i].type == DIRECTOR_BF16 ? kGradBf16 : 0) | (wb ? kOutBf16 : 0) | (state ? kStateWhole : 0) |
+                                        (pad_of(p[i].weight, p[i].type) == 0 ? kOutWhole : 0) | (pad_of(g[i].data, g[i].type) == 0 ? kGradWhole : 0));
         },
         run);
 }
@@ -779,7 +778,7 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
     q.ws = static_cast<Workspace*>(workspace);
     q.norm = norm;
     q.max_norm = max_norm;
-    if (in_one_launch(n, grads, kClipChunk))
+    if (in_one_launch(n, [&](int i) { return clip_chunks(out[i]); }))
         return clip_tables<kFewTensors>(n, grads, out, [&](const Table<2, kFewTensors>& t, int chunks) {
             return cuda_status(launch_as(true, clip_small_kernel, (unsigned)chunks, kThreads, st, t, q));
         });
@@ -834,7 +833,7 @@ int director_adamw_step(int32_t n, const director_tensor* grads, const director_
     b.beta2 = (float)h->beta2, b.rest2 = (float)(1.0 - h->beta2);
     b.eps = (float)h->eps;
     if (norm != nullptr || std::isfinite(h->max_norm)) {
-        if (in_one_launch(n, grads, kChunk))
+        if (in_one_launch(n, [&](int i) { return update_chunks(grads[i]); }))
             return update_tables<kFewTensors>(n, grads, params, [&](const Table<5, kFewTensors>& t, int chunks) {
                 return cuda_status(launch_as(true, update_small_kernel, (unsigned)chunks, kThreads, st, t, q, b));
             });
