@@ -25,7 +25,9 @@ namespace director {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kNormCtas = 5, kSlots = 1024;      // CTAs of the norm's grid: an SM's, and at most, one partial sum each
+// CTAs of the norm's grid: as many as an SM holds (five leave room for the next kernel's, which then fill the SMs unevenly: back to
+// back, the norm of 336 tensors takes 52 instead of 46 us), and at most, one partial sum each.
+constexpr int kNormCtas = 6, kSlots = 1024;
 constexpr int kNormUnroll = 4;                   // 16-byte loads of a thread and chunk of the norm
 constexpr int kClusterCtas = 16, kClusterThreads = 1024, kClusterUnroll = 8;
 constexpr int kChunk = kThreads * 8;             // elements of a chunk of the update
@@ -135,7 +137,25 @@ inline long long norm_chunks(const void* p, long long n, int per) {
     return n == 0 ? 0 : vecs == 0 ? 1 : (vecs + per - 1) / per;
 }
 
-// What a thread of a CTA of THREADS adds for chunk `chunk` of a tensor: UNROLL 16-byte loads.
+// The same four vectors once more in fp64, all zeros apart (an expert without tokens, the places behind a tensor's end).  They are
+// read again and out of line, so that the common way has the registers.
+template <typename T>
+__device__ __noinline__ double far_squares(const uint4* q, long long v, int step, long long vecs) {
+    constexpr uint32_t kMagnitude = sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu;
+    double sum = 0.0;
+    for (int u = 0; u < 4 && v < vecs; ++u, v += step) {
+        const uint4 x = __ldg(q + v);
+        if (((x.x | x.y | x.z | x.w) & kMagnitude) == 0) continue;
+#pragma unroll
+        for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
+            const double e = (double)element<T>(x, i);
+            sum = fma(e, e, sum);
+        }
+    }
+    return sum;
+}
+
+// What a thread of a CTA of THREADS adds for chunk `chunk` of a tensor: UNROLL 16-byte loads, a multiple of four.
 template <typename T, int THREADS, int UNROLL>
 __device__ __forceinline__ double squares_of_chunk(const T* __restrict__ p, long long n, int chunk) {
     constexpr int kPer = 16 / sizeof(T);
@@ -155,22 +175,22 @@ __device__ __forceinline__ double squares_of_chunk(const T* __restrict__ p, long
         else if (tid >= 32 && tid < 32 + tail) v = to_float(p[n - tail + tid - 32]);
         sum = (double)v * (double)v;
     }
-    float s = 0.0f;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u)
+    for (int u0 = 0; u0 < UNROLL; u0 += 4) {               // up to 32 elements
+        float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const float v = element<T>(x[u], i);
-            s = fmaf(v, v, s);
+        for (int u = u0; u < u0 + 4; ++u)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const float v = element<T>(x[u], i);
+                s = fmaf(v, v, s);
+            }
+        if (s >= kSquaresLowest && s <= kSquaresHighest) {
+            sum += (double)s;
+            continue;
         }
-    if (s >= kSquaresLowest && s <= kSquaresHighest) return sum + (double)s;
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u)
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const double v = (double)element<T>(x[u], i);
-            sum = fma(v, v, sum);
-        }
+        sum += far_squares<T>(q, v0 + u0 * THREADS, THREADS, vecs);
+    }
     return sum;
 }
 
@@ -495,16 +515,10 @@ update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas
     update_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kChunk), common_of(q), b);
 }
 
-// Few chunks: norm and step in one cooperative launch, the state on its way to L2 while the norm is taken.
+// Few chunks: norm and step in one cooperative launch.
 __global__ void __launch_bounds__(kThreads, kSmallCtas)
 update_small_kernel(const __grid_constant__ Table<5, kFewTensors> t, const Call q, const Betas b) {
     const Place p = place_of(t, blockIdx.x, kChunk);
-    if (threadIdx.x * 8 < p.end) {
-        const long long at = p.at + threadIdx.x * 8;
-        const int w32 = (p.kind & kOutBf16) ? 2 : 1;
-#pragma unroll
-        for (int i = 2; i < 5; ++i) asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const float*>(t.at[i == 2 ? w32 : i][p.k]) + at));
-    }
     const double norm = norm_in_launch(t, q, p, kChunk);
     float4 common = common_of(q);
     common.x = scale_of(q, norm);
