@@ -310,7 +310,7 @@ int director_balance_loss_backward(director_ctx* ctx, int32_t T, const float* lo
  * the call returns.  workspace: dev, director_grad_workspace_bytes() bytes, 16-byte aligned, contents irrelevant; calls that may
  * overlap on the GPU need one each.  The results have the same bits on every run on the same kind of GPU.
  * Errors: DIRECTOR_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, negative lengths, tensors that are written
- * and overlap another of the call; DIRECTOR_ERR_UNSUPPORTED for more than 2^40 elements in a tensor. */
+ * and overlap another of the call; DIRECTOR_ERR_UNSUPPORTED for more than 2^40 elements in a tensor or 2^24 tensors. */
 enum { DIRECTOR_FP32 = 0, DIRECTOR_BF16 = 1 };
 typedef struct {
     void* data;          /* dev */
@@ -342,7 +342,7 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
  * so far, advanced by one.  norm: dev fp32 [1] or NULL.
  * Where max_norm is finite or norm is not NULL the norm is taken, and where it is infinite or NaN the step is skipped: nothing
  * changes, steps neither, and device_status (dev int32 [1] or NULL) receives DIRECTOR_ERR_NONFINITE if it was 0.
- * 0 <= beta1, beta2 < 1, eps >= 0, max_norm > 0 (infinity: no clipping); lr and weight_decay finite. */
+ * 0 <= beta1, beta2 < 1, eps >= 0 (with 0, a weight whose gradients have all been zero becomes 0/0), max_norm > 0 (infinity: no clipping); lr and weight_decay finite. */
 typedef struct {
     void* weight;                              /* dev bf16 or fp32 [numel] */
     float *master, *exp_avg, *exp_avg_sq;      /* dev fp32 [numel] */

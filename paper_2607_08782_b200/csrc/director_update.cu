@@ -32,11 +32,12 @@ constexpr int kNormUnroll = 4;                   // 16-byte loads of a thread an
 constexpr int kClusterCtas = 16, kClusterThreads = 1024, kClusterUnroll = 8;
 constexpr int kChunk = kThreads * 8;             // elements of a chunk of the update
 constexpr int kClipUnroll = 4, kClipChunk = kThreads * 8 * kClipUnroll;
-// CTAs of an SM, and so chunks, up to which norm and elementwise part are one cooperative launch.  Against two launches or three, four
-// tensors: a step of 0.26 M weights 8.2 and 11.8 us a call, of 0.5 M 10.3 and 11.8, of 1 M (512 chunks) 12.3 and 11.7; clipping of
-// 1 M 11.4 and 15.7, of 4 M (512 chunks) 13.5 and 15.8, but 12.4 and 9.3 without the host, in a graph.
+// CTAs of an SM, and so chunks, up to which norm and elementwise part are one cooperative launch.  Against three launches, four tensors:
+// a step of 0.26 M weights 8.2 and 11.8 us a call, of 0.5 M 9.3 and 11.8, but of 1 M (512 chunks) 12.3 and 11.7; clipping of 1 M
+// 10.4 and 14.8.
 constexpr int kSmallCtas = 2;
-constexpr long long kMostElements = 1ll << 40;
+constexpr long long kMostElements = 1ll << 40;   // of a tensor
+constexpr int kMostTensors = 1 << 24;            // of a call
 
 // What a call keeps between its launches, in the caller's workspace.
 struct Workspace {
@@ -105,7 +106,7 @@ __device__ __forceinline__ double squares_of(const float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
     if (s >= kSquaresLowest && s <= kSquaresHighest) return (double)s;
-    double d = 0.0;
+    double d = 0.0;                                        // as in far_squares
 #pragma unroll
     for (int i = 0; i < 8; ++i) d = fma((double)v[i], (double)v[i], d);
     return d;
@@ -363,15 +364,29 @@ __device__ __forceinline__ Place place_of(const TABLE& t, int c, int chunk) {
 
 // The norm inside a cooperative launch: a CTA sums the squares of its chunk, and every CTA joins the partial sums behind the grid's
 // barrier.  Array 0 of the table holds the gradients.
-template <typename TABLE>
-__device__ __forceinline__ double norm_in_launch(const TABLE& t, const Call& q, const Place& p, int chunk) {
-    double sum = 0.0;
-    for (int e = threadIdx.x * 8; e < chunk && e < p.end; e += kThreads * 8) {
-        float v[8];
-        if (p.kind & kGradBf16) load_some(static_cast<const __nv_bfloat16*>(t.at[0][p.k]) + p.at + e, p.lo(e), p.hi(e), p.kind & kGradWhole, v);
-        else load_some(static_cast<const float*>(t.at[0][p.k]) + p.at + e, p.lo(e), p.hi(e), p.kind & kGradWhole, v);
-        sum += squares_of(v);
+template <typename T, int UNROLL>
+__device__ __forceinline__ double squares_of_place(const void* grad, const Place& p) {
+    const T* g = static_cast<const T*>(grad) + p.at;
+    const bool whole = p.kind & kGradWhole, full = whole && p.full(UNROLL * kThreads * 8);
+    float v[UNROLL][8];
+    if (full) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) load8(g + (u * kThreads + threadIdx.x) * 8, v[u]);
+    } else {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int e = (u * kThreads + threadIdx.x) * 8;
+            load_some(g + e, p.lo(e), p.hi(e), whole, v[u]);
+        }
     }
+    double sum = 0.0;
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) sum += squares_of(v[u]);
+    return sum;
+}
+template <int UNROLL, typename TABLE>
+__device__ __forceinline__ double norm_in_launch(const TABLE& t, const Call& q, const Place& p) {
+    double sum = (p.kind & kGradBf16) ? squares_of_place<__nv_bfloat16, UNROLL>(t.at[0][p.k], p) : squares_of_place<float, UNROLL>(t.at[0][p.k], p);
     if (q.steps != nullptr && blockIdx.x == gridDim.x - 1 && threadIdx.x == kThreads - 1) start_step(q);
     sum = block_sum<kThreads>(sum);
     if (threadIdx.x == 0) q.ws->partial[blockIdx.x] = sum;
@@ -442,7 +457,7 @@ clip_kernel(const __grid_constant__ Table<2, CAP> t, const Call q, bool in_place
 __global__ void __launch_bounds__(kThreads, kSmallCtas)
 clip_small_kernel(const __grid_constant__ Table<2, kFewTensors> t, const Call q) {
     const Place p = place_of(t, blockIdx.x, kClipChunk);
-    clip_place(t, p, scale_of(q, norm_in_launch(t, q, p, kClipChunk)));
+    clip_place(t, p, scale_of(q, norm_in_launch<kClipUnroll>(t, q, p)));
 }
 
 // ---- AdamW ---------------------------------------------------------------------------------------------------------
@@ -519,7 +534,7 @@ update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas
 __global__ void __launch_bounds__(kThreads, kSmallCtas)
 update_small_kernel(const __grid_constant__ Table<5, kFewTensors> t, const Call q, const Betas b) {
     const Place p = place_of(t, blockIdx.x, kChunk);
-    const double norm = norm_in_launch(t, q, p, kChunk);
+    const double norm = norm_in_launch<1>(t, q, p);
     float4 common = common_of(q);
     common.x = scale_of(q, norm);
     update_place(t, p, common, b);
@@ -567,6 +582,7 @@ private:
 
 int check_tensors(int32_t n, const director_tensor* g) {
     if (n < 0 || (n > 0 && g == nullptr)) return DIRECTOR_ERR_INVALID_ARG;
+    if (n > kMostTensors) return DIRECTOR_ERR_UNSUPPORTED;
     for (int i = 0; i < n; ++i) {
         if (!valid_array(g[i].data, g[i].numel, g[i].type)) return DIRECTOR_ERR_INVALID_ARG;
         if (g[i].numel > kMostElements) return DIRECTOR_ERR_UNSUPPORTED;
@@ -816,6 +832,7 @@ int director_adamw_step(int32_t n, const director_tensor* grads, const director_
     for (int i = 0; i < n; ++i) {
         const director_param& p = params[i];
         const bool wb = p.type == DIRECTOR_BF16;
+        if (p.numel > kMostElements) return DIRECTOR_ERR_UNSUPPORTED;
         if (!valid_array(p.weight, p.numel, p.type) || !valid_array(p.exp_avg, p.numel, DIRECTOR_FP32) ||
             !valid_array(p.exp_avg_sq, p.numel, DIRECTOR_FP32) || (wb && !valid_array(p.master, p.numel, DIRECTOR_FP32)) ||
             (!wb && p.master != nullptr))

@@ -16,7 +16,7 @@ import math
 import torch
 
 from . import binding
-from .binding import BF16, FP32, DirectorAdamW, DirectorError, DirectorParam, DirectorTensor, _check, load_library
+from .binding import BF16, FP32, SMALL_BYTES, SMALL_TENSORS, DirectorAdamW, DirectorError, DirectorParam, DirectorTensor, _check, load_library
 
 _TYPES = {torch.float32: FP32, torch.bfloat16: BF16}
 
@@ -45,9 +45,9 @@ class TensorList:
                 raise ValueError(f"tensor {i} is on {t.device}, the ones before it on {self.device}")
             a = self.array[i]
             a.data, a.numel, a.type = t.data_ptr(), t.numel(), kind
+        self.live = [t for t in self.tensors if t is not None and not t.is_inference()]
         self.numels = [a.numel for a in self.array[:len(self.tensors)]]
-        # what the library's norm needs no workspace for
-        self.small = len(self.tensors) <= 16 and sum(a.numel * (4 if a.type == FP32 else 2) for a in self.array) <= 4 << 20
+        self.small = len(self.tensors) <= SMALL_TENSORS and sum(a.numel * (4 if a.type == FP32 else 2) for a in self.array) <= SMALL_BYTES
         if self.device is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
 
@@ -79,11 +79,6 @@ def _norm_and_workspace(lib, device):
     return room[words], room.data_ptr()
 
 
-def _changed(tensors):
-    """Tells autograd that the tensors were changed in place."""
-    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
-
-
 def grad_norm(grads) -> torch.Tensor:
     """The square root of the sum of squares over all elements of all tensors (a TensorList or a sequence): fp32, no dimensions."""
     grads = _as_list(grads)
@@ -111,16 +106,17 @@ def clip_grads(grads, max_norm: float, out=None) -> torch.Tensor:
     lib, stream = _begin(grads.device)
     norm, workspace = _norm_and_workspace(lib, grads.device)
     _check(lib.director_clip_grads(len(grads), grads.array, out.array, max_norm, norm.data_ptr(), workspace, stream), "director_clip_grads")
-    _changed(out.tensors)
+    torch.autograd.graph.increment_version(out.live)          # autograd is told that they were changed in place
     return norm
 
 
 class AdamW:
-    """AdamW over bf16 weights, each with an fp32 master, and fp32 weights (contiguous CUDA tensors, kept by reference and updated
-    in place); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to it.  A step whose norm is infinite or NaN is skipped
-    (with max_norm = infinity the norm is not taken, and such gradients reach the weights).  `lr` may be changed between steps; in a captured step, pass an
-    fp32 CUDA tensor of one element instead, which the step reads when it runs.  One optimizer serves one stream at a time; its workspace
-    and the norm that a step returns are its own."""
+    """AdamW over bf16 weights, each with an fp32 master, and fp32 weights (contiguous CUDA tensors that share no memory, kept by
+    reference and updated in place); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to
+    it on the way (the gradients themselves stay as they are).  A step whose norm is infinite or NaN is skipped; with max_norm =
+    infinity the norm is not taken, and such gradients reach the weights.  `lr` and the other numbers may be changed between steps; for
+    a captured step, give `lr` as an fp32 CUDA tensor of one element, which the step reads when it runs.  One optimizer serves one
+    stream at a time: its workspace and the norm that a step returns are its own."""
 
     def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, max_norm=math.inf):
         self.weights = list(weights)
@@ -136,7 +132,7 @@ class AdamW:
         self.status = torch.zeros((1,), dtype=torch.int32, device=self.device)
         self._norm = torch.zeros((), dtype=torch.float32, device=self.device)
         self._workspace = torch.empty(load_library().director_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
-        self._hyper, self._shapes = DirectorAdamW(), listed.shapes
+        self._hyper, self._shapes, self._live = DirectorAdamW(), listed.shapes, listed.live
         self._params = (DirectorParam * max(1, len(self.weights)))()
         for i, w in enumerate(self.weights):
             p = self._params[i]
@@ -170,7 +166,7 @@ class AdamW:
         _check(lib.director_adamw_step(len(self._shapes), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(),
                                        None if norm is None else norm.data_ptr(), self.status.data_ptr(), self._workspace.data_ptr(), stream),
                "director_adamw_step")
-        _changed(self.weights)
+        torch.autograd.graph.increment_version(self._live)         # autograd is told that they were changed in place
         return norm
 
     def last_status(self) -> int:

@@ -2,31 +2,14 @@
 import numpy as np
 import pytest
 
+from oracle import director_training_oracle as tro
+
 pytestmark = pytest.mark.gpu
 
 
 def _director(T, E, K):
     from paper_2607_08782_b200.binding import Director
     return Director(T, 256, 128, E, K, 0, 16, 16)
-
-
-def _oracle(logits, idx, mask, K):
-    """loss, counts [E+1], and per token p and the difference f_e - sum_j f_j p_j (zeros for tokens without one)."""
-    T, E = logits.shape
-    valid = np.ones(T, bool) if mask is None else mask.astype(bool)
-    x = np.where(valid[:, None], logits.astype(np.float64), 0.0)
-    with np.errstate(invalid="ignore"):
-        z = np.exp(x - x.max(1, keepdims=True))
-        p = z / z.sum(1, keepdims=True)
-    good = valid & np.isfinite(p).all(1)
-    p = np.where(good[:, None], p, 0.0)
-    chosen = idx[valid].reshape(-1)
-    counts = np.bincount(chosen[(chosen >= 0) & (chosen < E)], minlength=E)
-    N = int(valid.sum())
-    f = counts / (K * max(N, 1))
-    loss = E * float(f @ p.sum(0)) / max(N, 1)
-    f = (E * counts - counts.sum()) / (E * K * max(N, 1))
-    return loss, np.append(counts, N), p, np.where(good[:, None], f - (p @ f)[:, None], 0.0), np.abs(f).max(), max(N, 1)
 
 
 def _inputs(T, E, K, masked, seed, spread=1.0):
@@ -40,20 +23,22 @@ def _inputs(T, E, K, masked, seed, spread=1.0):
 
 
 def _p_tolerance(logits):
-    """Relative error of a score.  The exponential: its argument d = x - max is rounded (2^-24 |d|) and so is d log2(e) (2^-24 |d| again),
-    2 ulp of the power of two; the sum over E <= 256 terms: 16 in a lane, one after another, and 4 shuffles; the division."""
+    """Relative error of a score.  The exponential: its argument, d log2(e) with d = x - max, is rounded once (2^-24 |d| log2(e), so
+    2^-24 |d| of the score; twice that allowed), 2 ulp of the power of two; the sum over E <= 256 terms: 16 in a lane, one after another,
+    and 4 shuffles; the division."""
     x = logits.double()
     x = x[x.isfinite().all(1)]
     d = float((x.amax(1) - x.amin(1)).max()) if x.numel() else 0.0
     return 2 * (2 * min(d, 90.0) + 4 + 20 + 2) * 2.0 ** -24
 
 
-def _check(d, T, E, K, logits, idx, mask, added, dloss=0.37, loss=None, counts=None):
+def _check(d, T, E, K, logits, idx, mask, added, dloss=0.37):
     import torch
     loss = torch.full((1,), 7.0, device="cuda")
     counts = torch.full((E + 1,), -7, dtype=torch.int64, device="cuda")
     d.balance_loss(T, logits, idx, mask, loss, counts)
-    want, want_counts, p, diff, f_max, N = _oracle(logits.cpu().numpy(), idx.cpu().numpy(), None if mask is None else mask.cpu().numpy(), K)
+    want, want_counts, p, diff, f = tro.balance(logits.cpu().numpy(), idx.cpu().numpy(), None if mask is None else mask.cpu().numpy(), K)
+    f_max, N = np.abs(f).max(), max(int(want_counts[-1]), 1)
     assert np.array_equal(counts.cpu().numpy(), want_counts)
     tol = _p_tolerance(logits if mask is None else logits[mask.bool()])
     # the sum over tokens: up to 64 of a lane one after another, 5 shuffles; all terms positive

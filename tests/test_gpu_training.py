@@ -419,6 +419,11 @@ def test_refusals():
     assert int(opt.steps) == 0 and len(TensorList([t, None])) == 2
 
 
+def test_the_c_entry_points_from_a_c_program(tmp_path):
+    from test_gpu_c_abi import _build_and_run
+    assert "0 mismatches" in _build_and_run(tmp_path, "step_from_c")
+
+
 # ---- together ------------------------------------------------------------------------------------------------------
 
 

@@ -46,6 +46,8 @@ def test_tensors_of_the_wrong_kind(bad):
 def test_a_tensor_that_is_too_long():
     n, a = _tensors((A, (1 << 40) + 1, BF16))
     assert _norm(n, a) == UNSUPPORTED and _clip(n, a, None) == UNSUPPORTED
+    assert _norm((1 << 24) + 1, a) == UNSUPPORTED
+    assert _step(_tensors((None, 0, BF16))[1], (DirectorParam * 1)(_param(numel=(1 << 40) + 1))) == UNSUPPORTED
 
 
 def test_missing_and_misaligned_buffers():
@@ -135,3 +137,12 @@ def test_python_refusals_that_need_no_gpu():
     from paper_2607_08782_b200.finetune import train
     with pytest.raises(ValueError):
         train(optimizer="sgd")
+
+
+def test_the_header_and_the_binding_agree_on_the_small_norm():
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(__file__), "..", "include", "director.h")).read()
+    assert int(re.search(r"DIRECTOR_SMALL_TENSORS (\d+)", text)[1]) == binding.SMALL_TENSORS
+    assert eval(re.search(r"DIRECTOR_SMALL_BYTES \((.*?)\)", text)[1]) == binding.SMALL_BYTES
+    assert ctypes.sizeof(DirectorTensor) == 24 and ctypes.sizeof(DirectorParam) == 48 and ctypes.sizeof(DirectorAdamW) == 48
