@@ -323,7 +323,7 @@ int64_t director_grad_workspace_bytes(void);
 /* norm = sqrt of the sum of squares over all elements of all tensors.  norm: dev fp32 [1].  Squares that leave fp32's range
  * do not harm it; an infinity or a NaN among the elements does.  At most DIRECTOR_SMALL_TENSORS tensors of DIRECTOR_SMALL_BYTES
  * bytes altogether take one launch and no workspace (NULL). */
-#define DIRECTOR_SMALL_TENSORS 16
+#define DIRECTOR_SMALL_TENSORS 64
 #define DIRECTOR_SMALL_BYTES (4 << 20)
 int director_grad_norm(int32_t n, const director_tensor* grads, float* norm, void* workspace, void* stream);
 

@@ -55,7 +55,7 @@ class DirectorAdamW(ctypes.Structure):
 
 
 FP32, BF16 = 0, 1
-SMALL_TENSORS, SMALL_BYTES = 16, 4 << 20          # what director_grad_norm needs no workspace for
+SMALL_TENSORS, SMALL_BYTES = 64, 4 << 20          # what director_grad_norm needs no workspace for
 
 
 class DirectorError(RuntimeError):

@@ -63,7 +63,7 @@ constexpr int kFewTensors = DIRECTOR_SMALL_TENSORS, kNormTensors = 480, kClipTen
 
 // The tensor that chunk c lies in.
 template <typename TABLE>
-__device__ __forceinline__ int tensor_of(const TABLE& t, int c) {
+__host__ __device__ __forceinline__ int tensor_of(const TABLE& t, int c) {
     int lo = 0, hi = t.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -214,7 +214,8 @@ __device__ __forceinline__ double squares_of_table(const TABLE& t, int cta, int 
     return sum;
 }
 
-// What a call makes of the norm.  Its first launch starts the step (AdamW), one thread behind the norm finishes it.
+// What a call makes of the norm.  A step (AdamW) is started by the call's first launch and counted by its last one, so that a call
+// whose later launches fail has not counted it.
 struct Call {
     Workspace* ws;
     float* norm;                 // or NULL
@@ -227,7 +228,6 @@ struct Call {
 
 __device__ __forceinline__ void start_step(const Call& q) {
     const long long t = *q.steps + 1;
-    *q.steps = t;
     const double lr = q.lr_dev != nullptr ? (double)*q.lr_dev : q.lr;
     q.ws->decay = (float)(lr * q.weight_decay);
     q.ws->rate = (float)(lr / (1.0 - pow(q.beta1, (double)t)));
@@ -238,16 +238,16 @@ __device__ __forceinline__ float scale_of(const Call& q, double norm) {
 }
 __device__ __forceinline__ void finish(const Call& q, double norm) {
     if (q.norm != nullptr) *q.norm = (float)norm;
-    if (q.steps != nullptr && !isfinite((float)norm)) {    // the step is not taken
-        *q.steps -= 1;
-        if (q.status != nullptr) director_set_status(q.status, DIRECTOR_ERR_NONFINITE);
-    }
+    if (q.steps != nullptr && q.status != nullptr && !isfinite((float)norm)) director_set_status(q.status, DIRECTOR_ERR_NONFINITE);
+}
+// One thread of the call's last launch, which nobody else reads *q.steps in; a norm that is not finite: the step is not taken.
+__device__ __forceinline__ void count_step(const Call& q, float scale) {
+    if (scale != kNotFinite) *q.steps += 1;
 }
 
 // Partial sum blockIdx.x of the workspace, added to it where an earlier launch of the call has written it (blockIdx.x < filled).
-template <int CAP>
 __global__ void __launch_bounds__(kThreads, kNormCtas)
-norm_kernel(const __grid_constant__ Table<1, CAP> t, const Call q, int filled) {
+norm_kernel(const __grid_constant__ Table<1, kNormTensors> t, const Call q, int filled) {
     chain_prologue();
     if (filled == 0 && q.steps != nullptr && blockIdx.x == gridDim.x - 1 && threadIdx.x == kThreads - 1) start_step(q);
     const double sum = block_sum<kThreads>(squares_of_table<kThreads, kNormUnroll>(t, blockIdx.x, gridDim.x));
@@ -261,14 +261,16 @@ __device__ __forceinline__ double norm_of_slots(const Workspace* ws, int slots) 
     return sqrt(block_sum<kThreads>(v));
 }
 
-// The norm from the partial sums; with none of them: a norm of 0, and the step is started here.
-__global__ void __launch_bounds__(kThreads) finish_kernel(const Call q, int slots) {
+// The norm from the partial sums; with none of them: a norm of 0, and the step is started here.  last: no launch of the call follows.
+__global__ void __launch_bounds__(kThreads) finish_kernel(const Call q, int slots, bool last) {
     chain_prologue();
     const double norm = norm_of_slots(q.ws, slots);
     if (threadIdx.x != 0) return;
     if (slots == 0 && q.steps != nullptr) start_step(q);
-    q.ws->scale = scale_of(q, norm);
+    const float scale = scale_of(q, norm);
+    q.ws->scale = scale;
     finish(q, norm);
+    if (last && q.steps != nullptr) count_step(q, scale);
 }
 
 // The norm alone of small tensors: the CTAs of one cluster hand their sums to its first through distributed shared memory - one
@@ -351,12 +353,13 @@ __device__ __forceinline__ float4 common_of(const Call& q) { return *reinterpret
 struct Place {
     int k, kind;                 // tensor
     long long at, end;           // the chunk's first element (negative in front of the tensor), and the tensor's end from there
-    __device__ bool full(int chunk) const { return at >= 0 && end >= chunk; }
-    __device__ int lo(int e) const { return at + e >= 0 ? 0 : (int)min(8ll, -(at + e)); }         // of the eight elements at e
-    __device__ int hi(int e) const { return (int)max(0ll, min(8ll, end - e)); }
+    __host__ __device__ bool full(int chunk) const { return at >= 0 && end >= chunk; }
+    // of the eight elements at e, those of the tensor: [lo, hi)
+    __host__ __device__ int lo(int e) const { return at + e >= 0 ? 0 : at + e > -8 ? (int)-(at + e) : 8; }
+    __host__ __device__ int hi(int e) const { return end - e >= 8 ? 8 : end > e ? (int)(end - e) : 0; }
 };
 template <typename TABLE>
-__device__ __forceinline__ Place place_of(const TABLE& t, int c, int chunk) {
+__host__ __device__ __forceinline__ Place place_of(const TABLE& t, int c, int chunk) {
     const int k = tensor_of(t, c);
     const long long at = (long long)(c - t.first[k]) * chunk - (t.kind[k] >> kPadShift);
     return {k, t.kind[k], at, t.numel[k] - at};
@@ -444,9 +447,8 @@ __device__ __forceinline__ void clip_place(const TABLE& t, const Place& p, float
     }
 }
 
-template <int CAP>
 __global__ void __launch_bounds__(kThreads, 4)
-clip_kernel(const __grid_constant__ Table<2, CAP> t, const Call q, bool in_place) {
+clip_kernel(const __grid_constant__ Table<2, kClipTensors> t, const Call q, bool in_place) {
     chain_prologue();
     const float scale = common_of(q).x;
     if (in_place && (scale == kNotFinite || scale == 1.0f)) return;
@@ -523,11 +525,12 @@ __device__ __forceinline__ void update_place(const TABLE& t, const Place& p, flo
     }
 }
 
-template <int CAP>
 __global__ void __launch_bounds__(kThreads, 4)
-update_kernel(const __grid_constant__ Table<5, CAP> t, const Call q, const Betas b) {
+update_kernel(const __grid_constant__ Table<5, kUpdateTensors> t, const Call q, const Betas b, bool last) {
     chain_prologue();
-    update_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kChunk), common_of(q), b);
+    const float4 common = common_of(q);
+    if (last && blockIdx.x == 0 && threadIdx.x == 0) count_step(q, common.x);
+    update_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kChunk), common, b);
 }
 
 // Few chunks: norm and step in one cooperative launch.
@@ -537,6 +540,7 @@ update_small_kernel(const __grid_constant__ Table<5, kFewTensors> t, const Call 
     const double norm = norm_in_launch<1>(t, q, p);
     float4 common = common_of(q);
     common.x = scale_of(q, norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0) count_step(q, common.x);
     update_place(t, p, common, b);
 }
 
@@ -615,7 +619,7 @@ cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, unsigned threads, cu
 }
 
 // Puts the tensors i = 0 .. n-1 that have chunks (chunks_of(i)) into tables (fill(table, slot, i)) and launches each table that is
-// full, and the last one even if it is empty: run(table, chunks).
+// full, and the last one even if it is empty: run(table, chunks, last).
 template <typename TABLE, int CAP, typename Chunks, typename Fill, typename Run>
 int in_tables(int n, Chunks&& chunks_of, Fill&& fill, Run&& run) {
     TABLE t;
@@ -625,7 +629,7 @@ int in_tables(int n, Chunks&& chunks_of, Fill&& fill, Run&& run) {
         const long long chunks = chunks_of(i);
         if (chunks == 0) continue;
         if (t.n == CAP || t.first[t.n] + chunks > (1ll << 30)) {
-            const int rc = run(t, t.first[t.n]);
+            const int rc = run(t, t.first[t.n], false);
             if (rc != DIRECTOR_OK) return rc;
             t.n = 0;
         }
@@ -633,7 +637,7 @@ int in_tables(int n, Chunks&& chunks_of, Fill&& fill, Run&& run) {
         t.first[t.n + 1] = (int)(t.first[t.n] + chunks);
         ++t.n;
     }
-    return run(t, t.first[t.n]);
+    return run(t, t.first[t.n], true);
 }
 
 // Whether one cluster takes the sum of squares.
@@ -673,25 +677,23 @@ int sum_squares(int n, const director_tensor* g, const Call& q, int* slots, cuda
     int sms = 0;
     if (!sm_count(&sms)) return DIRECTOR_ERR_CUDA;
     *slots = 0;
-    const auto run = [&](auto kernel, const auto& t, int chunks) {
+    return norm_tables<kNormTensors>(n, g, kThreads * kNormUnroll, [&](const Table<1, kNormTensors>& t, int chunks, bool) {
         const int grid = std::max(1, std::min({chunks, kNormCtas * sms, kSlots}));
-        const cudaError_t e = launch(kernel, (unsigned)grid, kThreads, st, t, q, *slots);
+        const cudaError_t e = launch(norm_kernel, (unsigned)grid, kThreads, st, t, q, *slots);
         *slots = std::max(*slots, grid);
         return cuda_status(e);
-    };
-    constexpr int kPer = kThreads * kNormUnroll;
-    return n <= kFewTensors
-        ? norm_tables<kFewTensors>(n, g, kPer, [&](const Table<1, kFewTensors>& t, int chunks) { return run(norm_kernel<kFewTensors>, t, chunks); })
-        : norm_tables<kNormTensors>(n, g, kPer, [&](const Table<1, kNormTensors>& t, int chunks) { return run(norm_kernel<kNormTensors>, t, chunks); });
+    });
 }
 
-int finish_call(const Call& q, int slots, cudaStream_t st) { return cuda_status(launch(finish_kernel, 1u, kThreads, st, q, slots)); }
+int finish_call(const Call& q, int slots, bool last, cudaStream_t st) {
+    return cuda_status(launch(finish_kernel, 1u, kThreads, st, q, slots, last));
+}
 
 // The norm, finished.
-int take_norm(int n, const director_tensor* g, const Call& q, cudaStream_t st) {
+int take_norm(int n, const director_tensor* g, const Call& q, bool last, cudaStream_t st) {
     int slots = 0;
     const int rc = sum_squares(n, g, q, &slots, st);
-    return rc != DIRECTOR_OK ? rc : finish_call(q, slots, st);
+    return rc != DIRECTOR_OK ? rc : finish_call(q, slots, last, st);
 }
 
 // Whether the norm and the elementwise part, of chunks_of(i) chunks a tensor, go into one launch: all CTAs run at once.
@@ -722,13 +724,6 @@ int clip_tables(int n, const director_tensor* g, const director_tensor* out, Run
         },
         run);
 }
-template <int CAP>
-int clip_launches(int n, const director_tensor* g, const director_tensor* out, const Call& q, cudaStream_t st) {
-    return clip_tables<CAP>(n, g, out, [&](const Table<2, CAP>& t, int chunks) {
-        return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(clip_kernel<CAP>, (unsigned)chunks, kThreads, st, t, q, out == g));
-    });
-}
-
 long long update_chunks(const director_tensor& g) { return (g.numel + kChunk - 1) / kChunk; }
 template <int CAP, typename Run>
 int update_tables(int n, const director_tensor* g, const director_param* p, Run&& run) {
@@ -748,13 +743,6 @@ int update_tables(int n, const director_tensor* g, const director_param* p, Run&
         },
         run);
 }
-template <int CAP>
-int update_launches(int n, const director_tensor* g, const director_param* p, const Call& q, const Betas& b, cudaStream_t st) {
-    return update_tables<CAP>(n, g, p, [&](const Table<5, CAP>& t, int chunks) {
-        return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(update_kernel<CAP>, (unsigned)chunks, kThreads, st, t, q, b));
-    });
-}
-
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 }  // namespace
@@ -772,17 +760,29 @@ int director_grad_norm(int32_t n, const director_tensor* grads, float* norm, voi
     if (rc != DIRECTOR_OK) return rc;
     if (norm == nullptr || !aligned4(norm) || !aligned16(workspace) || (workspace == nullptr && !in_one_cluster(n, grads)))
         return DIRECTOR_ERR_INVALID_ARG;
+    const auto apart = [](const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+        return x + a_bytes <= y || y + b_bytes <= x;
+    };
+    const size_t room = workspace == nullptr ? 0 : sizeof(Workspace);
+    if (room > 0 && !apart(norm, sizeof(float), workspace, room)) return DIRECTOR_ERR_INVALID_ARG;
+    for (int i = 0; i < n; ++i) {
+        const size_t bytes = (size_t)grads[i].numel * width_of(grads[i].type);
+        if (bytes == 0) continue;
+        if (!apart(grads[i].data, bytes, norm, sizeof(float)) || (room > 0 && !apart(grads[i].data, bytes, workspace, room)))
+            return DIRECTOR_ERR_INVALID_ARG;
+    }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (in_one_cluster(n, grads)) {
         if (cudaFuncSetAttribute(norm_cluster_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return DIRECTOR_ERR_CUDA;
-        return norm_tables<kFewTensors>(n, grads, kClusterThreads * kClusterUnroll, [&](const Table<1, kFewTensors>& t, int) {
+        return norm_tables<kFewTensors>(n, grads, kClusterThreads * kClusterUnroll, [&](const Table<1, kFewTensors>& t, int, bool) {
             return cuda_status(launch(norm_cluster_kernel, kClusterCtas, kClusterThreads, st, t, norm));
         });
     }
     Call q = {};
     q.ws = static_cast<Workspace*>(workspace);
     q.norm = norm;
-    return take_norm(n, grads, q, st);
+    return take_norm(n, grads, q, true, st);
 }
 
 int director_clip_grads(int32_t n, const director_tensor* grads, const director_tensor* out, float max_norm, float* norm,
@@ -809,12 +809,14 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
     q.norm = norm;
     q.max_norm = max_norm;
     if (in_one_launch(n, [&](int i) { return clip_chunks(out[i]); }))
-        return clip_tables<kFewTensors>(n, grads, out, [&](const Table<2, kFewTensors>& t, int chunks) {
+        return clip_tables<kFewTensors>(n, grads, out, [&](const Table<2, kFewTensors>& t, int chunks, bool) {
             return cuda_status(launch_as(true, clip_small_kernel, (unsigned)chunks, kThreads, st, t, q));
         });
-    rc = take_norm(n, grads, q, st);
+    rc = take_norm(n, grads, q, false, st);
     if (rc != DIRECTOR_OK) return rc;
-    return n <= kFewTensors ? clip_launches<kFewTensors>(n, grads, out, q, st) : clip_launches<kClipTensors>(n, grads, out, q, st);
+    return clip_tables<kClipTensors>(n, grads, out, [&](const Table<2, kClipTensors>& t, int chunks, bool) {
+        return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(clip_kernel, (unsigned)chunks, kThreads, st, t, q, out == grads));
+    });
 }
 
 int director_adamw_step(int32_t n, const director_tensor* grads, const director_param* params, const director_adamw* h,
@@ -863,17 +865,21 @@ int director_adamw_step(int32_t n, const director_tensor* grads, const director_
     b.beta1 = (float)h->beta1, b.rest1 = (float)(1.0 - h->beta1);
     b.beta2 = (float)h->beta2, b.rest2 = (float)(1.0 - h->beta2);
     b.eps = (float)h->eps;
+    bool none = true;                                      // no weight has a gradient
+    for (int i = 0; i < n && none; ++i) none = grads[i].numel == 0;
     if (norm != nullptr || std::isfinite(h->max_norm)) {
         if (in_one_launch(n, [&](int i) { return update_chunks(grads[i]); }))
-            return update_tables<kFewTensors>(n, grads, params, [&](const Table<5, kFewTensors>& t, int chunks) {
+            return update_tables<kFewTensors>(n, grads, params, [&](const Table<5, kFewTensors>& t, int chunks, bool) {
                 return cuda_status(launch_as(true, update_small_kernel, (unsigned)chunks, kThreads, st, t, q, b));
             });
-        rc = take_norm(n, grads, q, st);
+        rc = take_norm(n, grads, q, none, st);
     } else {
-        rc = finish_call(q, 0, st);
+        rc = finish_call(q, 0, none, st);
     }
     if (rc != DIRECTOR_OK) return rc;
-    return n <= kFewTensors ? update_launches<kFewTensors>(n, grads, params, q, b, st) : update_launches<kUpdateTensors>(n, grads, params, q, b, st);
+    return update_tables<kUpdateTensors>(n, grads, params, [&](const Table<5, kUpdateTensors>& t, int chunks, bool last) {
+        return chunks == 0 ? DIRECTOR_OK : cuda_status(launch(update_kernel, (unsigned)chunks, kThreads, st, t, q, b, last));
+    });
 }
 
 }  // extern "C"

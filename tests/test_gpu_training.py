@@ -42,7 +42,7 @@ def test_norm(types, shift):
     assert abs(grad_norm(t).item() - want) <= NORM_TOL * want
 
 
-@pytest.mark.parametrize("count", [15, 16, 17, 160, 161, 321, 1000])
+@pytest.mark.parametrize("count", [15, 63, 64, 65, 480, 481, 1000])
 def test_norm_of_many_tensors_and_the_same_bits_again(count):
     import torch
     from paper_2607_08782_b200.training import TensorList, grad_norm
@@ -120,6 +120,19 @@ def test_clip(src, dst, shift, fraction):
                 assert torch.equal(t, b)
         if out is not None:
             assert all(torch.equal(a, b) for a, b in zip(g, before))
+
+
+@pytest.mark.parametrize("count", [64, 65, 361, 800])
+def test_clip_of_many_tensors(count):
+    import torch
+    from paper_2607_08782_b200.training import clip_grads
+    g = _tensors([(i * 61) % 2701 for i in range(count)], "fbb", count, shift=count % 3)
+    want = _norm64(g)
+    out = [torch.full_like(t, 7.0, dtype=torch.float32) for t in g]
+    assert abs(clip_grads(g, 0.5 * want, out=out).item() - want) <= NORM_TOL * want
+    for o, t in zip(out, g):
+        ref = 0.5 * t.double()
+        assert ((o.double() - ref).abs() <= (NORM_TOL + 4 * 2.0 ** -24) * ref.abs()).all()
 
 
 def test_clip_in_place_into_itself_and_without_a_limit():
@@ -237,7 +250,7 @@ def test_sizes_where_one_launch_ends(extra):
         assert all(((o.double() - 0.25 * t.double()).abs() <= (NORM_TOL + 4 * 2.0 ** -24) * t.double().abs()).all() for o, t in zip(out, g))
 
 
-@pytest.mark.parametrize("count", [17, 160, 163, 500])
+@pytest.mark.parametrize("count", [17, 64, 65, 200, 203, 500])
 def test_a_step_of_many_tensors(count):
     sizes = [(i * 53) % 2203 for i in range(count)]
     opt, grads = _optimizer(sizes, "bbf", "bf", 2, lr=1e-3, max_norm=0.1)

@@ -57,6 +57,8 @@ def test_missing_and_misaligned_buffers():
     for bad in (None, WORK + 8):
         assert _norm(n, a, work=bad) == INVALID and _clip(n, a, None, work=bad) == INVALID
     assert _norm(1, None) == INVALID and _norm(-1, a) == INVALID
+    assert _norm(n, a, norm=A + 400) == INVALID and _norm(n, a, work=A + 1600) == INVALID       # inside the gradient
+    assert _norm(n, a, norm=WORK + 16) == INVALID
 
 
 @pytest.mark.parametrize("max_norm", [0.0, -1.0, -math.inf, math.nan])
