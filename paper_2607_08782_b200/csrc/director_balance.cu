@@ -6,7 +6,10 @@
 //
 // A row of up to 256 logits lies in the registers of LPR lanes, sixteen values each, so that a pass over the logits is one read;
 // max and sum of the softmax take log2(LPR) shuffles for the 32 / LPR rows that a warp has at a time, and a lane keeps its columns from
-// row to row, so that the sums over tokens are adds in registers.  HBM bounds the large batches, the launch the small ones.
+// row to row, so that the sums over tokens are adds in registers.  Sixteen and not eight values a lane: half the shuffles (131072 x
+// 256, the forward 28 and 30 us).  HBM bounds the large batches, the call the small ones: 131072 tokens, 256 experts, 28 us the forward
+// (138 MB, 5.0 TB/s, of which 3 us are the last CTAs' sums and 2 us the counts) and 45 us the gradient (268 MB, 6.0 TB/s); 8192
+// tokens, 64 experts, 5.9 and 3.1 us; 48 tokens, 8 experts, 3.1 and 2.5 us.
 #include "director_common.cuh"
 
 #include <cmath>
@@ -164,12 +167,14 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
             if (count) atomicAdd(&sums->count[tid], (unsigned long long)count);
         }
         if (tid == 0 && n) atomicAdd(&sums->count[kMaxE], (unsigned long long)n);
-        __threadfence();
         __syncthreads();
-        if (tid == 0) s_last = atomicAdd(&sums->ticket, 1u) == gridDim.x - 1;
+        if (tid == 0) {                                    // one fence behind the barrier covers what the whole CTA has added
+            __threadfence();
+            s_last = atomicAdd(&sums->ticket, 1u) == gridDim.x - 1;
+            __threadfence();
+        }
         __syncthreads();
         if (!s_last) return;
-        __threadfence();
         if (tid < E) {
             p = ldexp((double)(long long)__ldcg(&sums->p[tid]), -shift);
             count = (long long)__ldcg(&sums->count[tid]);
@@ -196,7 +201,8 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
     }
 }
 
-// The gradient.  f enters less its mean, (E counts_e - sum counts) / (E K N) from whole numbers: the difference f_e - sum_j f_j p_tj is
+// The gradient.  A row is read, its softmax taken again (keeping it would cost the forward another array) and its gradient written.
+// f enters less its mean, (E counts_e - sum counts) / (E K N) from whole numbers: the difference f_e - sum_j f_j p_tj is
 // the same, and a router that is nearly balanced does not lose it to the rounding of two nearly equal numbers.
 template <int LPR, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? 4 : 3)

@@ -245,6 +245,8 @@ __device__ __forceinline__ void count_step(const Call& q, float scale) {
     if (scale != kNotFinite) *q.steps += 1;
 }
 
+// The sum of squares: one read of the gradients, HBM-bound.  Four 16-byte loads a thread are under way, a chunk of 16 KB a CTA; 1.41 G
+// bf16 gradients take 390 us, 7.2 TB/s (a CTA to a chunk would take 2 % less, but leave 172 thousand sums to join).
 // Partial sum blockIdx.x of the workspace, added to it where an earlier launch of the call has written it (blockIdx.x < filled).
 __global__ void __launch_bounds__(kThreads, kNormCtas)
 norm_kernel(const __grid_constant__ Table<1, kNormTensors> t, const Call q, int filled) {
@@ -274,7 +276,8 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const Call q, int slot
 }
 
 // The norm alone of small tensors: the CTAs of one cluster hand their sums to its first through distributed shared memory - one
-// launch instead of two, and no workspace.
+// launch instead of two, and no workspace.  Sixteen SMs read 2 TB/s: 1 MB in 4.2 us and 4 MB in 5.9 us on the device, where the two
+// launches take 3.8 and 4.5, but 7.0 instead of 11.4 us a call.
 __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterThreads, 1)
 norm_cluster_kernel(const __grid_constant__ Table<1, kFewTensors> t, float* norm) {
     __shared__ double s_sums[kClusterCtas];
@@ -401,6 +404,8 @@ __device__ __forceinline__ double norm_in_launch(const TABLE& t, const Call& q, 
 
 // ---- clipping ------------------------------------------------------------------------------------------------------
 
+// One read and one write, HBM-bound, with the norm's read before it: 571 M bf16 gradients to fp32 in 680 us, 156 of them the norm's; the
+// rest moves 3.43 GB at 6.5 TB/s.  Chunks of 4096 elements 692 us, of 2048 892: a CTA then has too few bytes under way.
 // A chunk: kClipUnroll x eight elements a thread, asked for together.  FULL: all of them exist, and go out whole; SW: and come in whole.
 template <bool FULL, bool SW, typename S, typename D>
 __device__ __forceinline__ void clip_chunk(const S* src, D* dst, const Place& p, float scale) {
@@ -473,6 +478,8 @@ struct Arrays {
     float *master, *exp_avg, *exp_avg_sq;
 };
 
+// Four arrays read, four written, 28 bytes a bf16 weight, HBM-bound: 604 M weights in 2635 us with the norm (168 us), 6.85 TB/s.  Eight
+// elements a thread and not more: 112 bytes under way are enough at 1024 threads an SM, and the registers are full.
 // A chunk: eight elements a thread.  FULL: all of them exist and the state's addresses allow whole accesses; GW, WW: the gradient's and
 // the weight's do.
 template <bool FULL, bool GW, bool WW, typename G, typename W>
