@@ -67,26 +67,32 @@ def _begin(device: torch.device):
     lib = load_library()
     if binding._raw_stream is None:
         binding._bind_torch()
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    current = binding._current_device()
+    if device.index != current:
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{current}")
     return lib, binding._stream()
 
 
-def _norm_and_workspace(lib, device):
-    """One allocation of the two.  Made anew by each call, on its stream: calls that overlap, captured ones too, never share it."""
-    words = lib.director_grad_workspace_bytes() // 4
-    room = torch.empty(words + 1, dtype=torch.float32, device=device)
-    return room[words], room.data_ptr()
+_words = 0        # of a workspace, in fp32
+
+
+def _norm_and_workspace(lib, device, small=False):
+    """A place for the norm and, unless the call is small, the address of a workspace, in one allocation.  Made anew by each call, on its
+    stream: calls that overlap, captured ones too, never share it."""
+    if small:
+        return torch.empty_strided((), (), dtype=torch.float32, device=device), None        # 0.9 us less than torch.empty(())
+    global _words
+    if _words == 0:
+        _words = lib.director_grad_workspace_bytes() // 4
+    room = torch.empty(_words + 1, dtype=torch.float32, device=device)
+    return room[_words], room.data_ptr()
 
 
 def grad_norm(grads) -> torch.Tensor:
     """The square root of the sum of squares over all elements of all tensors (a TensorList or a sequence): fp32, no dimensions."""
     grads = _as_list(grads)
     lib, stream = _begin(grads.device)
-    if grads.small:
-        norm, workspace = torch.empty((), dtype=torch.float32, device=grads.device), None
-    else:
-        norm, workspace = _norm_and_workspace(lib, grads.device)
+    norm, workspace = _norm_and_workspace(lib, grads.device, grads.small)
     _check(lib.director_grad_norm(len(grads), grads.array, norm.data_ptr(), workspace, stream), "director_grad_norm")
     return norm
 

@@ -85,6 +85,41 @@ def test_a_long_batch_and_the_same_bits_again(E, K):
     assert d.last_status() == 0
 
 
+def test_offsets_past_31_bits():
+    """More logits than 31 bits count: the loss in pieces, the gradient of the first and the last tokens."""
+    import torch
+    T, E, K = 8_400_011, 256, 1
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GB")
+    d = _director(T, E, K)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    logits = torch.randn((T, E), generator=g, device="cuda")
+    idx = torch.randint(0, E // 2, (T, K), generator=g, device="cuda").int()
+    mask = (torch.arange(T, device="cuda") % 7 != 0)
+    loss, counts = torch.empty(1, device="cuda"), torch.empty(E + 1, dtype=torch.int64, device="cuda")
+    d.balance_loss(T, logits, idx, mask, loss, counts)
+    N = int(mask.sum())
+    want = torch.bincount(idx[mask].view(-1).long(), minlength=E)
+    assert torch.equal(counts[:E], want) and int(counts[E]) == N
+    P = torch.zeros(E, dtype=torch.float64, device="cuda")
+    for lo in range(0, T, 400_000):
+        p = logits[lo:lo + 400_000].double().softmax(1)
+        P += p[mask[lo:lo + 400_000]].sum(0)
+    f = want.double() / N
+    ref = E * float(f @ P) / N
+    tol = _p_tolerance(logits[:100_000])
+    assert abs(loss.item() - ref) <= (tol + 2.0 ** -24 * (64 + 5 + 2)) * ref
+    out = torch.full((T, E), 7.0, device="cuda")
+    d.balance_loss_backward(T, logits, counts, mask, torch.ones(1, device="cuda"), None, out)
+    f = (E * want - want.sum()).double() / (E * N)
+    for rows in (slice(0, 3000), slice((1 << 31) // E - 1500, (1 << 31) // E + 1500), slice(T - 3000, T)):
+        p = logits[rows].double().softmax(1) * mask[rows].unsqueeze(1)
+        diff = f - (p @ f).unsqueeze(1)
+        bound = E / N * p * (2 * tol + 2.0 ** -21) * (diff.abs() + f.abs().max()) + 1e-37
+        assert ((out[rows].double() - E / N * p * diff).abs() <= bound).all()
+    assert d.last_status() == 0
+
+
 def test_every_expert_chosen_by_every_token_has_no_gradient():
     import torch
     d = _director(500, 8, 8)

@@ -260,6 +260,42 @@ def test_a_step_of_many_tensors(count):
         ref.step(g, 1e-3, 0.1)
 
 
+def test_offsets_past_31_bits():
+    """A weight with more elements than 31 bits count, next to a small one: its first, middle and last elements."""
+    import torch
+    from paper_2607_08782_b200.training import AdamW, clip_grads
+    n = (1 << 31) + 5003
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    ends = [slice(0, 4099), slice((1 << 31) - 3000, (1 << 31) + 3000), slice(n - 4099, n)]
+    g = [torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.randn(1000, device="cuda")]
+    w = [torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.randn(1000, device="cuda")]
+    for s in ends:
+        g[0][s], w[0][s] = torch.randn(s.stop - s.start, device="cuda").bfloat16(), torch.randn(s.stop - s.start, device="cuda").bfloat16()
+    opt = AdamW(w, lr=1e-2, max_norm=1.0)
+
+    class Part:                                              # the optimizer as _Reference sees it, at some of the elements
+        betas, eps, weight_decay = opt.betas, opt.eps, opt.weight_decay
+
+        def __init__(self, s):
+            self.weights, self.masters, self.exp_avg, self.exp_avg_sq = ([t[s]] for t in (w[0], opt.masters[0], opt.exp_avg[0], opt.exp_avg_sq[0]))
+            self.steps = opt.steps
+    parts = [(_Reference(Part(s)), s) for s in ends]
+    want = _norm64([g[0][ends[0]], g[0][ends[1].start:], g[1]])          # the last two overlap
+    got = opt.step(g)
+    assert abs(got.item() - want) <= NORM_TOL * want
+    for ref, s in parts:                                     # clipped by the norm of all
+        part = g[0][s]
+        ref.step([part], 1e-2, _norm64([part]) / want)
+        ref.opt.steps = opt.steps
+    assert not opt.exp_avg[0][5000:9000].any() and not w[0][5000:9000].any()
+    before = [g[0][s].clone() for s in ends]
+    clip_grads(g, 0.25 * want)
+    for b, s in zip(before, ends):
+        ref = b.double() * 0.25
+        assert ((g[0][s].double() - ref).abs() <= (HALF["b"] + NORM_TOL + 2.0 ** -22) * ref.abs()).all()
+
+
 def test_states_at_odd_addresses():
     """Weights that are views of one buffer, back to back."""
     import torch
