@@ -110,22 +110,33 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
     };
     bool next_live = fetch(warp * kGroups);
 
-    // the counts, while the first rows are on their way; r0 is a multiple of four, so that a CTA's indices start on 16 bytes
+    // The counts, four choices a thread and pass, fetched a pass ahead like the rows.  r0 is a multiple of four, so that a CTA's
+    // choices start on 16 bytes.
+    const unsigned n_chosen = (unsigned)n_rows * K;
+    const int32_t* const chosen = topk_idx + (size_t)r0 * K;
+    unsigned at = 4 * tid;
+    int4 four = make_int4(0, 0, 0, 0);
+    const auto fetch_four = [&] {
+        if (at + 4 <= n_chosen) {
+            four = __ldg(reinterpret_cast<const int4*>(chosen + at));
+        } else if (at < n_chosen) {
+            four.x = __ldg(chosen + at);
+            if (at + 1 < n_chosen) four.y = __ldg(chosen + at + 1);
+            if (at + 2 < n_chosen) four.z = __ldg(chosen + at + 2);
+        }
+    };
     const auto count_one = [&](unsigned a, int e) {
-        if (mask != nullptr && __ldg(mask + r0 + a / (unsigned)K) == 0) return;
+        if (a >= n_chosen || (mask != nullptr && __ldg(mask + r0 + a / (unsigned)K) == 0)) return;
         if ((unsigned)e < (unsigned)E) atomicAdd(&s_count[e], 1);
         else director_set_status(status, DIRECTOR_ERR_BAD_INDEX);
     };
-    const unsigned n_chosen = (unsigned)n_rows * K;
-    const int32_t* const chosen = topk_idx + (size_t)r0 * K;
-    for (unsigned a = 4 * tid; a < n_chosen; a += 4 * kThreads) {
-        if (a + 4 <= n_chosen) {
-            const int4 e = __ldg(reinterpret_cast<const int4*>(chosen + a));
-            count_one(a, e.x), count_one(a + 1, e.y), count_one(a + 2, e.z), count_one(a + 3, e.w);
-        } else {
-            for (unsigned b = a; b < n_chosen; ++b) count_one(b, __ldg(chosen + b));
-        }
-    }
+    const auto count_four = [&] {
+        if (at >= n_chosen) return;
+        count_one(at, four.x), count_one(at + 1, four.y), count_one(at + 2, four.z), count_one(at + 3, four.w);
+        at += 4 * kThreads;
+        fetch_four();
+    };
+    fetch_four();
 
     for (int base = warp * kGroups; base < n_rows; base += kWarps * kGroups) {
         const bool live = next_live;
@@ -144,7 +155,9 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
                 director_set_status(status, DIRECTOR_ERR_NONFINITE);
             }
         }
+        count_four();
     }
+    while (at < n_chosen) count_four();
 #pragma unroll
     for (int o = LPR; o < 32; o <<= 1)
 #pragma unroll
