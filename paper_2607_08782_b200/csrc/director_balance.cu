@@ -7,9 +7,9 @@
 // A row of up to 256 logits lies in the registers of LPR lanes, sixteen values each, so that a pass over the logits is one read;
 // max and sum of the softmax take log2(LPR) shuffles for the 32 / LPR rows that a warp has at a time, and a lane keeps its columns from
 // row to row, so that the sums over tokens are adds in registers.  Sixteen and not eight values a lane: half the shuffles (131072 x
-// 256, the forward 28 and 30 us).  HBM bounds the large batches, the call the small ones: 131072 tokens, 256 experts, 28 us the forward
-// (138 MB, 5.0 TB/s, of which 3 us are the last CTAs' sums and 2 us the counts) and 45 us the gradient (268 MB, 6.0 TB/s); 8192
-// tokens, 64 experts, 5.9 and 3.1 us; 48 tokens, 8 experts, 3.1 and 2.5 us.
+// 256, the forward 28 and 30 us).  HBM bounds the large batches, the call the small ones: 131072 tokens, 256 experts, 27 us the forward
+// (138 MB, 5.2 TB/s; 3 us of them are the last CTAs' sums) and 44 us the gradient (268 MB, 6.1 TB/s); 8192 tokens, 64 experts, 5.6
+// and 3.1 us; 48 tokens, 8 experts, 3.1 and 2.5 us.
 #include "director_common.cuh"
 
 #include <cmath>
@@ -21,9 +21,9 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32, kVals = 16;
 constexpr int kMostPasses = 64;      // rows that a lane sees in one CTA at most: the forward's fp32 sums stay short
 // CTAs of the forward that an SM holds, and that the batch is cut for: they all run at once (131072 x 256: 28 us; four and 64 registers
-// 28, five 41).  The backward sums nothing, and many small CTAs keep the addresses that are under way close together: 45 us with 16
-// an SM of which four run, 46 with 8, 50 with 4.
-constexpr int kForwardCtas = 3, kBackwardCtas = 16;
+// 28, five 41).  The backward sums nothing, and many small CTAs keep the addresses that are under way close together: 43.8 us with 24
+// an SM of which four run, 44.8 with 16, 45.8 with 8, 50 with 4, 47 with 64.
+constexpr int kForwardCtas = 3, kBackwardCtas = 24;
 
 // The sixteen values of lane `sub` of its row: groups of four, LPR groups apart.  -inf behind the last expert.
 template <int LPR, bool VEC>
