@@ -48,8 +48,9 @@ __device__ __forceinline__ float power_of_two(float x) {
 }
 
 // x -> exp(x - max), up to a factor that all have in common; returns their sum, NaN for a row with a NaN, a +inf or nothing but
-// -inf.  One product and one power of two: 2^(x log2(e) - max log2(e)).  The second product's rounding is the common factor; the
-// difference's is 2^-24 of the distance from the maximum, in the exponent: what it moves is as small as exp(-distance).
+// -inf.  One product and one power of two: 2^(x log2(e) - max log2(e)).  The second product's rounding, 2^-24 of it, is the common
+// factor's exponent, which has to stay small; the difference's is 2^-24 of the distance from the maximum, in the exponent: what it moves
+// is as small as exp(-distance).
 template <int LPR>
 __device__ __forceinline__ float softmax_terms(float (&x)[kVals]) {
     constexpr float kLog2E = 1.4426950408889634f;
@@ -58,7 +59,7 @@ __device__ __forceinline__ float softmax_terms(float (&x)[kVals]) {
     for (int i = 1; i < kVals; ++i) m = fmaxf(m, x[i]);
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    if (fabsf(m) > 1e37f) {                                // max log2(e) would leave the range
+    if (fabsf(m) > 1e6f) {                                 // the common factor would be more than 2^0.1 from one
 #pragma unroll
         for (int i = 0; i < kVals; ++i) x[i] -= m;
         m -= m;

@@ -190,6 +190,23 @@ def test_large_logits_do_not_overflow():
     _check(d, T, E, K, *_inputs(T, E, K, False, 7, spread=1e-6))
 
 
+@pytest.mark.parametrize("E", [8, 61, 256])
+@pytest.mark.parametrize("at", [1e3, 9e5, 2e6, 1e9, 1e12, 1e30, 1e37, 3e38])
+def test_logits_far_from_zero(E, at):
+    """Rows around `at` and -`at`, one step of fp32 or a few units apart."""
+    import torch
+    T, K = 64, 2
+    d = _director(T, E, K)
+    logits, idx, _, added = _inputs(T, E, K, False, 12)
+    logits[:32] = at + logits[:32]
+    logits[32:] = -at + logits[32:]
+    logits[5, 1] = torch.nextafter(logits[5, 1], torch.tensor(0.0, device="cuda"))
+    logits[40, 2] = logits[40].max() - 3.0
+    assert torch.isfinite(logits).all()
+    _check(d, T, E, K, logits, idx, None, added)
+    assert d.last_status() == 0
+
+
 def test_indices_of_no_expert_are_skipped_and_reported():
     T, E, K = 120, 60, 4
     d = _director(T, E, K)
