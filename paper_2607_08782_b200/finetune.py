@@ -32,18 +32,21 @@ class _Layer(torch.autograd.Function):
         ctx.layer = layer
         # What the backward pass reads of the caller's: autograd then notices where it was changed in place (x itself is read by
         # the shared experts alone, the routed experts' rows are copies).  The pass's number goes the same way, so that under
-        # activation checkpointing it comes back as that of the pass that was run again.
-        # The balance term reads the logits and the mask again.
-        ctx.save_for_backward(torch.tensor(layer.passes, device="cpu"), *weights, *((x,) if layer.dims["S"] > 0 else ()),
+        # activation checkpointing it comes back as that of the pass that was run again.  The balance term, which has a number of
+        # its own, reads the logits and the mask again.
+        ctx.balance = balance
+        ctx.save_for_backward(torch.tensor([layer.passes, layer.balances], device="cpu"), *weights, *((x,) if layer.dims["S"] > 0 else ()),
                               *((logits, *((token_mask,) if token_mask is not None else ())) if balance else ()))
         return (y, loss) if balance else y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dbalance=None):
-        kept, layer = int(ctx.saved_tensors[0]), ctx.layer         # the first access raises if a tensor was changed
+        (kept, balanced), layer = ctx.saved_tensors[0].tolist(), ctx.layer         # the first access raises if a tensor was changed
         if layer.trained is None or layer.trained[3] != kept:
             raise RuntimeError("the layer keeps one forward pass: run its backward before the layer's next pass")
+        if ctx.balance and layer.balances != balanced:
+            raise RuntimeError("the layer keeps one balance term: its balance_loss() was called between the passes")
         g = layer.backward(dy.shape[0], dy.contiguous(), dbalance.contiguous() if dbalance is not None else None)
         weights = [g[n] for n in _WEIGHTS if n in g]
         return (None, None, None, None, *(t.clone() if need else None for t, need in zip([g["x"], g["logits"], *weights], ctx.needs_input_grad[4:])))
@@ -55,7 +58,7 @@ def moe_layer(layer: MoELayer, x: torch.Tensor, logits: torch.Tensor, token_src_
     weights (those that require a gradient).  Between the passes the experts' gate and up values are kept in 8 bits, which moves the
     gradients by under 1 %; the weights' come out in bf16.  The layer's placement has to be set.  One forward pass at a time is kept: the
     backward pass of a call has to run before the layer's next call (torch.utils.checkpoint lifts this: it runs the call again
-    when its backward pass comes), and before the weights (with shared experts, x too) are changed
+    when its backward pass comes), and before the weights (with shared experts, x too; with balance, the logits and the mask) are changed
     in place.  token_src_rank (int32 [T]): the tokens' home ranks, for the locality-first choice of replicas (see MoELayer.dispatch).
     balance: returns (y, loss) with the router's balance term, fp32 [1], over the tokens that token_mask (uint8 or bool [T], 0 for padding)
     leaves; it is 1 for an even load and is to be added to the training loss with a small weight.  Padded tokens go through the

@@ -40,7 +40,9 @@ class MoELayer:
         # the layer have the same number.
         self.trained = None
         self.passes = 0
-        self.balanced = None         # (T, logits, token_mask, pass) of the balance_loss() whose counts are intact
+        # (T, logits, token_mask, pass, number) of the balance_loss() whose counts are intact; no two of them have the same number.
+        self.balanced = None
+        self.balances = 0
         self.w = (w_gate, w_up, w_down)
         self.ws = (ws_gate, ws_up, ws_down)
         A, G = T_max * K, R * C_max
@@ -174,7 +176,8 @@ class MoELayer:
             self.balance = (torch.empty((1,), dtype=torch.float32, device=dev), torch.empty((self.dims["E"] + 1,), dtype=torch.int64, device=dev))
         self.balanced = None
         self.d.balance_loss(T, logits, self.topk_idx, token_mask, *self.balance)
-        self.balanced = (T, logits.detach(), token_mask, self.passes)
+        self.balances += 1
+        self.balanced = (T, logits.detach(), token_mask, self.passes, self.balances)
         return self.balance
 
     def backward(self, T, dy, dbalance=None):
@@ -202,7 +205,7 @@ class MoELayer:
         self.d.dispatch_backward(T, self.dxp, self.inv_row, self.dx_shared if with_shared else None, g["x"])
         self.d.route_backward(T, self.topk_idx, self.topk_w, self.dtopk_w, g["logits"])
         if dbalance is not None:
-            _, logits, mask, _ = self.balanced
+            logits, mask = self.balanced[1:3]
             self.d.balance_loss_backward(T, logits, self.balance[1], mask, dbalance, g["logits"], g["logits"])
         return {n: t[:T] if n in ("x", "logits") else t for n, t in g.items()}
 

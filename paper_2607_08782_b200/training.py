@@ -118,7 +118,7 @@ def clip_grads(grads, max_norm: float, out=None) -> torch.Tensor:
 
 class AdamW:
     """AdamW over bf16 weights, each with an fp32 master, and fp32 weights (contiguous CUDA tensors that share no memory, kept by
-    reference and updated in place); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to
+    reference and updated in place, at the addresses that they and the state have now); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to
     it on the way (the gradients themselves stay as they are).  A step whose norm is infinite or NaN is skipped; with max_norm =
     infinity the norm is not taken, and such gradients reach the weights.  `lr` and the other numbers may be changed between steps; for
     a captured step, give `lr` as an fp32 CUDA tensor of one element, which the step reads when it runs.  One optimizer serves one
@@ -139,6 +139,7 @@ class AdamW:
         self._norm = torch.zeros((), dtype=torch.float32, device=self.device)
         self._workspace = torch.empty(load_library().director_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
         self._hyper, self._shapes, self._live = DirectorAdamW(), listed.shapes, listed.live
+        self._addresses = [w.data_ptr() for w in self.weights]
         self._params = (DirectorParam * max(1, len(self.weights)))()
         for i, w in enumerate(self.weights):
             p = self._params[i]
@@ -150,6 +151,8 @@ class AdamW:
         """One step on `grads` (a TensorList or a sequence, a tensor or None for each weight; default: the weights' .grad), with
         `lr` in place of the optimizer's if given (a number or an fp32 CUDA tensor of one element).  Returns the gradients' norm before
         clipping (fp32, no dimensions, overwritten by the next step), None where max_norm is infinite."""
+        if [w.data_ptr() for w in self.weights] != self._addresses:
+            raise RuntimeError("AdamW.step: a weight has moved to other memory since the optimizer was made")
         grads = _as_list([w.grad for w in self.weights] if grads is None else grads)
         if grads.shapes != self._shapes:
             if len(grads) != len(self._shapes):

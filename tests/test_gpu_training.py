@@ -465,6 +465,12 @@ def test_refusals():
         AdamW([t]).step([t])
     with pytest.raises(DirectorError):
         AdamW([t], betas=(1.0, 0.9)).step([t.clone()])
+    moved = [t.clone(), t.clone()]
+    other = AdamW(moved)
+    moved[1].data = t.clone()
+    with pytest.raises(RuntimeError):
+        other.step([t, t])
+    assert int(other.steps) == 0
     assert int(opt.steps) == 0 and len(TensorList([t, None])) == 2
 
 
@@ -546,6 +552,13 @@ def test_autograd_with_the_balance_term():
         logits.add_(1.0)
     with pytest.raises(RuntimeError):                        # the logits were changed in between
         loss.sum().backward()
+    y, loss = moe_layer(layer, x, logits, balance=True)
+    layer.balance_loss(96, logits, mask)
+    with pytest.raises(RuntimeError):                        # the counts are no longer that term's
+        loss.sum().backward()
+    y = moe_layer(layer, x, logits)
+    layer.balance_loss(96, logits, mask)                     # a pass without the term does not mind
+    y.float().sum().backward()
     for bad in (dict(token_mask=mask), dict(balance=True, token_mask=mask[:5]), dict(balance=True, token_mask=mask.float())):
         with pytest.raises(ValueError):
             moe_layer(layer, x, logits, **bad)
