@@ -25,18 +25,28 @@ constexpr int kMostPasses = 64;      // rows that a lane sees in one CTA at most
 // an SM of which four run, 44.8 with 16, 45.8 with 8, 50 with 4, 47 with 64.
 constexpr int kForwardCtas = 3, kBackwardCtas = 24;
 
-// The sixteen values of lane `sub` of its row: groups of four, LPR groups apart.  -inf behind the last expert.
+// The expert of a lane's value i: groups of four LPR groups apart where a row can be read in 16-byte words, values LPR apart where
+// it cannot, so that the lanes of a row touch neighbours in either case.
+template <int LPR, bool VEC>
+__device__ __forceinline__ int expert_of(int i, int sub) {
+    return VEC ? 4 * ((i / 4) * LPR + sub) + i % 4 : i * LPR + sub;
+}
+
+// The sixteen values of lane `sub` of its row, -inf behind the last expert.
 template <int LPR, bool VEC>
 __device__ __forceinline__ void load_row(const float* __restrict__ row, int E, int sub, float (&x)[kVals]) {
 #pragma unroll
     for (int j = 0; j < kVals / 4; ++j) {
-        const int e = 4 * (j * LPR + sub);
         if (VEC) {
+            const int e = 4 * (j * LPR + sub);
             const float4 v = e < E ? __ldg(reinterpret_cast<const float4*>(row + e)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
             x[4 * j] = v.x, x[4 * j + 1] = v.y, x[4 * j + 2] = v.z, x[4 * j + 3] = v.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * j + i] = e + i < E ? __ldg(row + e + i) : -INFINITY;
+            for (int i = 4 * j; i < 4 * j + 4; ++i) {
+                const int e = expert_of<LPR, VEC>(i, sub);
+                x[i] = e < E ? __ldg(row + e) : -INFINITY;
+            }
         }
     }
 }
@@ -165,7 +175,7 @@ balance_loss_kernel(const float* __restrict__ logits, const int32_t* __restrict_
         for (int i = 0; i < kVals; ++i) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], o);
     if (lane < LPR)
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) s_p[warp][4 * ((i / 4) * LPR + sub) + i % 4] = acc[i];
+        for (int i = 0; i < kVals; ++i) s_p[warp][expert_of<LPR, VEC>(i, sub)] = acc[i];
     valid = __reduce_add_sync(0xFFFFFFFFu, valid);
     if (lane == 0 && valid) atomicAdd(&s_count[kMaxE], valid);
     __syncthreads();
@@ -253,7 +263,7 @@ balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restr
     __syncthreads();
     float f[kVals];
 #pragma unroll
-    for (int i = 0; i < kVals; ++i) f[i] = s_f[4 * ((i / 4) * LPR + sub) + i % 4];
+    for (int i = 0; i < kVals; ++i) f[i] = s_f[expert_of<LPR, VEC>(i, sub)];
     const float factor = n > 0 ? (float)((double)__ldg(dloss) * E / n) : 0.0f;
 
     for (int base = warp * kGroups; base < n_rows; base += kWarps * kGroups) {
@@ -279,10 +289,10 @@ balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restr
         if (!here) continue;
 #pragma unroll
         for (int j = 0; j < kVals / 4; ++j) {
-            const int e = 4 * (j * LPR + sub);
-            const size_t at = (size_t)row * E + e;
             if (VEC) {
+                const int e = 4 * (j * LPR + sub);
                 if (e >= E) continue;
+                const size_t at = (size_t)row * E + e;
                 float4 v = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
                 if (added != nullptr) {
                     const float4 a = *reinterpret_cast<const float4*>(added + at);
@@ -291,8 +301,12 @@ balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restr
                 *reinterpret_cast<float4*>(dlogits + at) = v;
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (e + i < E) dlogits[at + i] = added != nullptr ? added[at + i] + d[4 * j + i] : d[4 * j + i];
+                for (int i = 4 * j; i < 4 * j + 4; ++i) {
+                    const int e = expert_of<LPR, VEC>(i, sub);
+                    if (e >= E) continue;
+                    const size_t at = (size_t)row * E + e;
+                    dlogits[at] = added != nullptr ? added[at] + d[i] : d[i];
+                }
             }
         }
     }
