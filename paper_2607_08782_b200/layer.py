@@ -171,6 +171,8 @@ class MoELayer:
         experts' counts, int64 [E+1], the last entry the number of valid tokens (see director_balance_loss): buffers of the layer,
         overwritten by the next call.  logits: as for forward_train(); they and token_mask (uint8 or bool [T], 0 for padding) have
         to stay as they are until backward()."""
+        if self.trained is not None and self.trained[0] != T:
+            raise RuntimeError(f"balance_loss() of {T} tokens after a forward_train() of {self.trained[0]}")
         if getattr(self, "balance", None) is None:
             dev = self.y.device
             self.balance = (torch.empty((1,), dtype=torch.float32, device=dev), torch.empty((self.dims["E"] + 1,), dtype=torch.int64, device=dev))

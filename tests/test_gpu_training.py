@@ -414,6 +414,32 @@ def test_captured_steps_advance_and_follow_the_learning_rate():
     assert norm0.item() > 0
 
 
+@pytest.mark.parametrize("sizes", [[4000, 17], [3_000_000, 5, 1_000_000], [(i * 37) % 901 for i in range(100)]])
+def test_every_call_replayed_from_a_graph(sizes):
+    """One launch, three, many tensors: norm, clipping in place and apart, a step, on inputs that changed since the capture."""
+    import torch
+    from paper_2607_08782_b200.training import TensorList, clip_grads, grad_norm
+    g, h = TensorList(_tensors(sizes, "bf", 1)), TensorList(_tensors(sizes, "bf", 2))
+    out = TensorList([torch.empty_like(t, dtype=torch.float32) for t in g])
+    (opt, _), (twin, _) = (_optimizer(sizes, "bf", "bf", 16, lr=1e-3, max_norm=0.7) for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norms = [grad_norm(g), clip_grads(g, 0.9, out=out), clip_grads(h, 0.8), opt.step(g), grad_norm(h)]
+    for k in range(3):
+        new = [_tensors(sizes, "bf", 30 + k, 10.0 ** -k), _tensors(sizes, "bf", 40 + k)]
+        for lst, values in zip((g, h), new):
+            for t, v in zip(lst, values):
+                t.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        other = [torch.empty_like(t, dtype=torch.float32) for t in g]
+        want = [grad_norm(new[0]), clip_grads(new[0], 0.9, out=other), clip_grads(new[1], 0.8), twin.step(new[0]), grad_norm(new[1])]
+        assert all(torch.equal(a, b) for a, b in zip(norms, want))
+        for mine, theirs in ((out, other), (h, new[1]), (opt.weights, twin.weights), (opt.exp_avg, twin.exp_avg), (opt.exp_avg_sq, twin.exp_avg_sq)):
+            assert all(torch.equal(a, b) for a, b in zip(mine, theirs))
+    assert int(opt.steps) == 3
+
+
 def test_on_another_stream():
     import torch
     opt, grads = _optimizer([4000, 17, 700000], "bf", "bf", 15, lr=1e-3, max_norm=1.0)
@@ -519,6 +545,8 @@ def test_the_layers_gradients_with_the_balance_term():
         layer.backward(96, dy, weight)
     with pytest.raises(ValueError):
         layer.balance_loss(96, logits[:95])
+    with pytest.raises(RuntimeError):                        # the choices of the pass are 96 tokens'
+        layer.balance_loss(95, logits)
 
 
 def test_autograd_with_the_balance_term():
