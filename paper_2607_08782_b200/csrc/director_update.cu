@@ -25,8 +25,8 @@ namespace director {
 namespace {
 
 constexpr int kThreads = 256;
-// CTAs of the norm's grid: as many as an SM holds (five leave room for the next kernel's, which then fill the SMs unevenly: back to
-// back, the norm of 336 tensors takes 52 instead of 46 us), and at most, one partial sum each.
+// CTAs of an SM in the norm's grid (eight, as many as an SM holds, read 1.41 G bf16 gradients in 414 us, six in 393), and CTAs of a grid
+// at most, one partial sum each.
 constexpr int kNormCtas = 6, kSlots = 1024;
 constexpr int kNormUnroll = 4;                   // 16-byte loads of a thread and chunk of the norm
 constexpr int kClusterCtas = 16, kClusterThreads = 1024, kClusterUnroll = 8;
@@ -49,6 +49,13 @@ struct Workspace {
 };
 
 constexpr float kNotFinite = -1.0f;
+
+// chain_prologue() in two halves, for the kernels that come before a norm: they let the next kernel come when their own work is done (at
+// their end, where they do not say so themselves), not when it begins.  The CTAs of a norm that comes earlier go where some of its
+// predecessor's have left first, more than kNormCtas to an SM and fewer to others, and the SMs stay unevenly filled as long as it runs
+// (back to back, 336 tensors 56 us instead of 43, as from a graph; 1.41 G elements 419 instead of 387).
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chain_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // The tensors of one launch: P arrays of CAP tensors, and the first chunk of each tensor.
 template <int P, int CAP>
@@ -267,9 +274,10 @@ __device__ __forceinline__ void count_step(const Call& q, float scale) {
 // Partial sum blockIdx.x of the workspace, added to it where an earlier launch of the call has written it (blockIdx.x < filled).
 __global__ void __launch_bounds__(kThreads, kNormCtas)
 norm_kernel(const __grid_constant__ Table<1, kNormTensors> t, const Call q, int filled) {
-    chain_prologue();
+    chain_wait();
     if (filled == 0 && q.steps != nullptr && blockIdx.x == gridDim.x - 1 && threadIdx.x == kThreads - 1) start_step(q);
     const double sum = block_sum<kThreads>(squares_of_table<kThreads, kNormUnroll>(t, blockIdx.x, gridDim.x));
+    chain_release();
     double* const mine = q.ws->partial + blockIdx.x;
     if (threadIdx.x == 0) *mine = (int)blockIdx.x < filled ? *mine + sum : sum;
 }
@@ -282,7 +290,7 @@ __device__ __forceinline__ double norm_of_slots(const Workspace* ws, int slots) 
 
 // The norm from the partial sums; with none of them: a norm of 0, and the step is started here.  last: no launch of the call follows.
 __global__ void __launch_bounds__(kThreads) finish_kernel(const Call q, int slots, bool last) {
-    chain_prologue();
+    chain_wait();
     const double norm = norm_of_slots(q.ws, slots);
     if (threadIdx.x != 0) return;
     if (slots == 0 && q.steps != nullptr) start_step(q);
@@ -470,7 +478,7 @@ __device__ __forceinline__ void clip_place(const TABLE& t, const Place& p, float
 
 __global__ void __launch_bounds__(kThreads, 4)
 clip_kernel(const __grid_constant__ Table<2, kClipTensors> t, const Call q, bool in_place) {
-    chain_prologue();
+    chain_wait();
     const float scale = common_of(q).x;
     if (in_place && (scale == kNotFinite || scale == 1.0f)) return;
     clip_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kClipChunk), scale);
@@ -550,7 +558,7 @@ __device__ __forceinline__ void update_place(const TABLE& t, const Place& p, flo
 
 __global__ void __launch_bounds__(kThreads, 4)
 update_kernel(const __grid_constant__ Table<5, kUpdateTensors> t, const Call q, const Betas b, bool last) {
-    chain_prologue();
+    chain_wait();
     const float4 common = common_of(q);
     if (last && blockIdx.x == 0 && threadIdx.x == 0) count_step(q, common.x);
     update_place(t, place_of(t, gridDim.x - 1 - blockIdx.x, kChunk), common, b);
