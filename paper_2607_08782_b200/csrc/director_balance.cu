@@ -280,7 +280,8 @@ balance_backward_kernel(const float* __restrict__ logits, const int64_t* __restr
         for (int i = 0; i < kVals; ++i) mean = fmaf(x[i], f[i], mean);
 #pragma unroll
         for (int o = 1; o < LPR; o <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, o);
-        const float inv = good ? __fdividef(1.0f, s) : 0.0f, scale = factor * inv, shift = mean * inv * scale;
+        // chosen, not multiplied by zero: a factor that is not finite (a scaled loss that overflowed) leaves such rows alone
+        const float inv = good ? __fdividef(1.0f, s) : 0.0f, scale = good ? factor * inv : 0.0f, shift = mean * inv * scale;
         float d[kVals];
 #pragma unroll
         for (int i = 0; i < kVals; ++i) d[i] = x[i] * fmaf(f[i], scale, -shift);
