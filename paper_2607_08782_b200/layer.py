@@ -21,9 +21,11 @@ def tensor_to_bf16_bits(t: torch.Tensor) -> np.ndarray:
 class LayerGraph(torch.cuda.CUDAGraph):
     """A captured pass of a layer.  Its replays write to the layer's buffers, as the pass itself does."""
     layer = None
+    T = 0
 
     def replay(self):
         self.layer.trained = None
+        self.layer.routed = self.T
         super().replay()
 
 
@@ -40,6 +42,7 @@ class MoELayer:
         # the layer have the same number.
         self.trained = None
         self.passes = 0
+        self.routed = 0            # tokens whose choices topk_idx and topk_w hold
         # (T, logits, token_mask, pass, number) of the balance_loss() whose counts are intact; no two of them have the same number.
         self.balanced = None
         self.balances = 0
@@ -74,6 +77,7 @@ class MoELayer:
     def route(self, T, logits):
         self.trained = None
         self.d.route(T, logits, self.topk_idx, self.topk_w)
+        self.routed = T
 
     def set_replica_policy(self, policy: int):
         """0: round-robin over an expert's replicas; 1: locality first (see director_set_replica_policy)."""
@@ -170,9 +174,11 @@ class MoELayer:
         """The router's balance term over the batch that forward_train() (or route()) just took, E sum_e f_e P_e, fp32 [1], and the
         experts' counts, int64 [E+1], the last entry the number of valid tokens (see director_balance_loss): buffers of the layer,
         overwritten by the next call.  logits: as for forward_train(); they and token_mask (uint8 or bool [T], 0 for padding) have
-        to stay as they are until backward()."""
+        to stay as they are until backward().  For more tokens than the layer routed last it raises a RuntimeError."""
         if self.trained is not None and self.trained[0] != T:
             raise RuntimeError(f"balance_loss() of {T} tokens after a forward_train() of {self.trained[0]}")
+        if T > self.routed:                               # the places behind hold another batch's choices, or nothing
+            raise RuntimeError(f"balance_loss() of {T} tokens, but the layer has routed {self.routed}")
         if getattr(self, "balance", None) is None:
             dev = self.y.device
             self.balance = (torch.empty((1,), dtype=torch.float32, device=dev), torch.empty((self.dims["E"] + 1,), dtype=torch.int64, device=dev))
@@ -228,6 +234,7 @@ class MoELayer:
             self.d.route_dispatch_cost(T, logits, x, self.topk_idx, self.topk_w, None if gather else self.xp,
                                        self.row_token, self.inv_row, self.dest_rank, self.seg_offsets, self.workload,
                                        self.rank_load, self.dispatch_tokens, self.dispatch_bytes)
+            self.routed = T
         else:
             self.route(T, logits)
             self.dispatch(T, x, indices_only=gather)
@@ -251,7 +258,7 @@ class MoELayer:
             self.forward(T, logits, x, with_cost, fused, fused_combine)
         torch.cuda.current_stream().wait_stream(side)
         graph = LayerGraph()
-        graph.layer = self
+        graph.layer, graph.T = self, T
         with torch.cuda.graph(graph):
             self.forward(T, logits, x, with_cost, fused, fused_combine)
         return graph
