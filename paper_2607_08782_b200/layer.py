@@ -24,7 +24,7 @@ class LayerGraph(torch.cuda.CUDAGraph):
     T = 0
 
     def replay(self):
-        self.layer.trained = None
+        self.layer._give_up_pass()
         self.layer.routed = self.T
         super().replay()
 
@@ -43,7 +43,7 @@ class MoELayer:
         self.trained = None
         self.passes = 0
         self.routed = 0            # tokens whose choices topk_idx and topk_w hold
-        # (T, logits, token_mask, pass, number) of the balance_loss() whose counts are intact; no two of them have the same number.
+        # (T, logits, token_mask, pass, number) of the pass's balance_loss() whose counts are intact; no two of them have the same number.
         self.balanced = None
         self.balances = 0
         self.w = (w_gate, w_up, w_down)
@@ -66,6 +66,10 @@ class MoELayer:
         self.dispatch_tokens = torch.empty((R, R), **i64)
         self.dispatch_bytes = torch.empty((R, R), **i64)     # bit pattern of uint64
 
+    def _give_up_pass(self):
+        """No backward pass of the last training forward may run any more; what it would have read of the caller's is let go."""
+        self.trained = self.balanced = None
+
     def set_placement(self, X: np.ndarray):
         self.d.set_placement(X)
 
@@ -75,7 +79,7 @@ class MoELayer:
         self.ffn_variant = variant
 
     def route(self, T, logits):
-        self.trained = None
+        self._give_up_pass()
         self.d.route(T, logits, self.topk_idx, self.topk_w)
         self.routed = T
 
@@ -84,7 +88,7 @@ class MoELayer:
         self.d.set_replica_policy(policy)
 
     def dispatch(self, T, x, indices_only=False, token_src_rank=None):
-        self.trained = None
+        self._give_up_pass()
         xp = None if indices_only else self.xp
         if token_src_rank is None:
             self.d.dispatch(T, x, self.topk_idx, xp, self.row_token, self.inv_row, self.dest_rank, self.seg_offsets)
@@ -103,13 +107,13 @@ class MoELayer:
     def expert_ffn_gather(self, T, x):
         """The routed experts read their rows from x through row_token (no permuted copy)."""
         S = self.dims["S"]
-        self.trained = None
+        self._give_up_pass()
         self.d.expert_ffn_gather(T, x, self.row_token, self.seg_offsets, *self.w, self.yp,
                                  *(self.ws if S > 0 else (None, None, None)), self.y_shared if S > 0 else None)
 
     def expert_ffn(self, T, x=None):
         S = self.dims["S"]
-        self.trained = None
+        self._give_up_pass()
         self.d.expert_ffn(T, self.xp, self.seg_offsets, *self.w, self.yp,
                           x if S > 0 else None, *(self.ws if S > 0 else (None, None, None)),
                           self.y_shared if S > 0 else None)
@@ -185,7 +189,8 @@ class MoELayer:
         self.balanced = None
         self.d.balance_loss(T, logits, self.topk_idx, token_mask, *self.balance)
         self.balances += 1
-        self.balanced = (T, logits.detach(), token_mask, self.passes, self.balances)
+        if self.trained is not None:                      # else there is no backward pass to keep them for
+            self.balanced = (T, logits.detach(), token_mask, self.passes, self.balances)
         return self.balance
 
     def backward(self, T, dy, dbalance=None):
@@ -200,10 +205,11 @@ class MoELayer:
             raise RuntimeError("backward() needs the placement that forward_train() ran under, which has been changed since")
         if dbalance is not None and (self.balanced is None or self.balanced[0] != T or self.balanced[3] != number):
             raise RuntimeError("backward() with dbalance needs a balance_loss() of the pass")
+        balanced = self.balanced
         _need("backward", ("dy", dy, torch.bfloat16, T * self.dims["H"]))
         if dbalance is not None:
             _need("backward", ("dbalance", dbalance, torch.float32, 1))
-        self.trained = None
+        self._give_up_pass()
         g = self.grads
         self.d.combine_backward(T, dy, self.yp, self.inv_row, self.topk_w, self.dyp, self.dtopk_w)
         with_shared = self.dims["S"] > 0
@@ -213,7 +219,7 @@ class MoELayer:
         self.d.dispatch_backward(T, self.dxp, self.inv_row, self.dx_shared if with_shared else None, g["x"])
         self.d.route_backward(T, self.topk_idx, self.topk_w, self.dtopk_w, g["logits"])
         if dbalance is not None:
-            logits, mask = self.balanced[1:3]
+            logits, mask = balanced[1:3]
             self.d.balance_loss_backward(T, logits, self.balance[1], mask, dbalance, g["logits"], g["logits"])
         return {n: t[:T] if n in ("x", "logits") else t for n, t in g.items()}
 
@@ -229,7 +235,7 @@ class MoELayer:
         # a batch small enough for the weight-streaming FFN kernels needs no permuted copy either: they stage a
         # segment's few rows from x themselves
         gather = (fused and self.ffn_variant == 2) or (self.d.batch_streams_weights(T) and not fused_combine)
-        self.trained = None
+        self._give_up_pass()
         if with_cost:          # front end in one call (a single launch for decode-sized batches)
             self.d.route_dispatch_cost(T, logits, x, self.topk_idx, self.topk_w, None if gather else self.xp,
                                        self.row_token, self.inv_row, self.dest_rank, self.seg_offsets, self.workload,

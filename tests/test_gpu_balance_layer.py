@@ -47,3 +47,39 @@ def test_a_batch_is_not_larger_than_what_was_routed(how):
     layer.forward_train(96, large, x)
     assert torch.equal(layer.balance_loss(96, large)[1][:8], _counts(large))
     layer.d.check_device_status()
+
+
+@pytest.mark.parametrize("end", ["backward", "backward without the term", "route", "forward", "forward_train", "graph", "nothing to keep"])
+def test_the_batch_is_let_go_with_its_pass(end):
+    """Logits and mask are held for the backward pass and not beyond it."""
+    import gc
+    import weakref
+
+    import torch
+    layer = _layer()
+    (other, xo), (logits, x) = _batch(40, 3), _batch(96, 4)
+    dy, weight = torch.randn((96, 256), device="cuda").bfloat16(), torch.full((1,), 0.1, device="cuda")
+    graph = layer.capture(40, other, xo) if end == "graph" else None
+    mask = torch.ones(96, dtype=torch.uint8, device="cuda")
+    if end == "nothing to keep":
+        layer.route(96, logits)
+    else:
+        layer.forward_train(96, logits, x)
+    layer.balance_loss(96, logits, mask)
+    held = weakref.ref(mask)
+    del mask
+    gc.collect()
+    assert (held() is not None) == (end != "nothing to keep"), "the backward pass reads it"
+    if end.startswith("backward"):
+        layer.backward(96, dy, weight if end == "backward" else None)
+    elif end == "route":
+        layer.route(40, other)
+    elif end == "forward":
+        layer.forward(40, other, xo)
+    elif end == "forward_train":
+        layer.forward_train(40, other, xo)
+    elif end == "graph":
+        graph.replay()
+    gc.collect()
+    assert held() is None and layer.balanced is None
+    layer.d.check_device_status()
