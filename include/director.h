@@ -336,8 +336,8 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
 /* One step of AdamW (Adam where weight_decay is 0) on the gradients g' = g * min(1, max_norm / norm), t = *steps + 1:
  *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
  *   w = w - lr weight_decay w - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
- * in fp32.  A bf16 weight has an fp32 master, which is what w is above, and becomes the master rounded; an fp32 weight has none
- * (master NULL).  grads: n tensors as long as the weights; one with data NULL and numel 0 leaves its weight and moments as they are.
+ * in fp32.  A bf16 weight has an fp32 master, which is what w is above, and becomes the master rounded, whatever it held before (who
+ * writes a weight between steps has to write its master too); an fp32 weight has none (master NULL).  grads: n tensors as long as the weights; one with data NULL and numel 0 leaves its weight and moments as they are.
  * params: host.  lr: dev fp32 [1] that takes the place of h->lr (for captured steps), or NULL.  steps: dev int64 [1], the steps done
  * so far, advanced by one.  norm: dev fp32 [1] or NULL.
  * Where max_norm is finite or norm is not NULL the norm is taken, and where it is infinite or NaN the step is skipped: nothing

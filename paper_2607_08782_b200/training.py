@@ -118,11 +118,16 @@ def clip_grads(grads, max_norm: float, out=None) -> torch.Tensor:
 
 class AdamW:
     """AdamW over bf16 weights, each with an fp32 master, and fp32 weights (contiguous CUDA tensors that share no memory, kept by
-    reference and updated in place, at the addresses that they and the state have now); Adam where weight_decay is 0.  Gradients above max_norm in their global norm are scaled down to
-    it on the way (the gradients themselves stay as they are).  A step whose norm is infinite or NaN is skipped; with max_norm =
-    infinity the norm is not taken, and such gradients reach the weights.  `lr` and the other numbers may be changed between steps; for
-    a captured step, give `lr` as an fp32 CUDA tensor of one element, which the step reads when it runs.  One optimizer serves one
-    stream at a time: its workspace and the norm that a step returns are its own."""
+    reference and updated in place, at the addresses that they and the state have now); Adam where weight_decay is 0.  Gradients above
+    max_norm in their global norm are scaled down to it on the way (the gradients themselves stay as they are).  A step whose norm is
+    infinite or NaN is skipped; with max_norm = infinity the norm is not taken, and such gradients reach the weights.  `lr` and the other
+    numbers may be changed between steps; for a captured step, give `lr` as an fp32 CUDA tensor of one element, which the step reads when
+    it runs.  One optimizer serves one stream at a time: its workspace and the norm that a step returns are its own.
+
+    A step writes a bf16 weight from its master.  Weights that are given other values after the optimizer was made (a checkpoint is loaded)
+    need masters_from_weights(): until then a step raises a RuntimeError.  It goes by autograd's count of in-place changes, so that it does not
+    notice changes through .data, to weights that are part of a larger tensor (which has one count for all of it) or to inference tensors,
+    nor by graph replays; those would be lost."""
 
     def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, max_norm=math.inf):
         self.weights = list(weights)
@@ -140,6 +145,12 @@ class AdamW:
         self._workspace = torch.empty(load_library().director_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
         self._hyper, self._shapes, self._live = DirectorAdamW(), listed.shapes, listed.live
         self._addresses = [w.data_ptr() for w in self.weights]
+        self._workspace_at, self._norm_at = self._workspace.data_ptr(), self._norm.data_ptr()
+        # bf16 weights that have their memory, and so their count of in-place changes, to themselves; the counts' sum as of the last
+        # time that weights and masters agreed.  The counts only grow.
+        self._counted = [w for w, m in zip(self.weights, self.masters)
+                         if m is not None and not w.is_inference() and w.untyped_storage().nbytes() == w.numel() * w.element_size()]
+        self._changes = self._count_changes()
         self._params = (DirectorParam * max(1, len(self.weights)))()
         for i, w in enumerate(self.weights):
             p = self._params[i]
@@ -147,12 +158,39 @@ class AdamW:
             p.exp_avg, p.exp_avg_sq = self.exp_avg[i].data_ptr(), self.exp_avg_sq[i].data_ptr()
             p.master = self.masters[i].data_ptr() if self.masters[i] is not None else None
 
+    def _count_changes(self) -> int:
+        return sum([w._version for w in self._counted])
+
+    def _check_weights(self):
+        """Some bf16 weight was written since the last step: raises unless all are what their masters say (swapped out and back)."""
+        advice = ("call masters_from_weights() to go on from the weights as they are, or load_state_dict(state_dict()) to go on from "
+                  "the masters")
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError(f"AdamW.step: a bf16 weight was written since the last step, before this capture: {advice}")
+        with torch.no_grad():
+            for i, (w, m) in enumerate(zip(self.weights, self.masters)):
+                for a, b in zip(w.view(-1).split(1 << 26), m.view(-1).split(1 << 26)) if m is not None else ():
+                    b = b.to(torch.bfloat16)
+                    if not ((a == b) | (a.isnan() & b.isnan())).all():
+                        raise RuntimeError(f"AdamW.step: weight {i} was written since the last step, and would be overwritten from its master: {advice}")
+        self._changes = self._count_changes()
+
+    def masters_from_weights(self):
+        """The masters become the bf16 weights as they are now (weights that were loaded into them); moments and step count stay."""
+        with torch.no_grad():
+            for w, m in zip(self.weights, self.masters):
+                if m is not None:
+                    m.copy_(w)
+        self._changes = self._count_changes()
+
     def step(self, grads=None, lr=None) -> torch.Tensor | None:
         """One step on `grads` (a TensorList or a sequence, a tensor or None for each weight; default: the weights' .grad), with
         `lr` in place of the optimizer's if given (a number or an fp32 CUDA tensor of one element).  Returns the gradients' norm before
         clipping (fp32, no dimensions, overwritten by the next step), None where max_norm is infinite."""
         if [w.data_ptr() for w in self.weights] != self._addresses:
             raise RuntimeError("AdamW.step: a weight has moved to other memory since the optimizer was made")
+        if sum([w._version for w in self._counted]) != self._changes:
+            self._check_weights()
         grads = _as_list([w.grad for w in self.weights] if grads is None else grads)
         if grads.shapes != self._shapes:
             if len(grads) != len(self._shapes):
@@ -171,11 +209,12 @@ class AdamW:
             lr_dev, lr = lr.data_ptr(), 0.0
         h = self._hyper
         h.lr, (h.beta1, h.beta2), h.eps, h.weight_decay, h.max_norm = lr, self.betas, self.eps, self.weight_decay, self.max_norm
-        norm = self._norm if self.max_norm != math.inf else None
-        _check(lib.director_adamw_step(len(self._shapes), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(),
-                                       None if norm is None else norm.data_ptr(), self.status.data_ptr(), self._workspace.data_ptr(), stream),
+        norm, norm_at = (self._norm, self._norm_at) if self.max_norm != math.inf else (None, None)
+        _check(lib.director_adamw_step(len(self._shapes), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(), norm_at,
+                                       self.status.data_ptr(), self._workspace_at, stream),
                "director_adamw_step")
         torch.autograd.graph.increment_version(self._live)         # autograd is told that they were changed in place
+        self._changes += len(self._counted)
         return norm
 
     def last_status(self) -> int:
@@ -209,3 +248,4 @@ class AdamW:
                 if m is not None:
                     w.copy_(m)
             self.steps.copy_(state["steps"])
+        self._changes = self._count_changes()
