@@ -143,7 +143,8 @@ class AdamW:
         self.status = torch.zeros((1,), dtype=torch.int32, device=self.device)
         self._norm = torch.zeros((), dtype=torch.float32, device=self.device)
         self._workspace = torch.empty(load_library().director_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
-        self._hyper, self._shapes, self._live = DirectorAdamW(), listed.shapes, listed.live
+        self._hyper, self._numbers, self._shapes, self._live = DirectorAdamW(), None, listed.shapes, listed.live
+        self._hyper_at = ctypes.byref(self._hyper)
         self._addresses = [w.data_ptr() for w in self.weights]
         self._workspace_at, self._norm_at = self._workspace.data_ptr(), self._norm.data_ptr()
         # bf16 weights that have their memory, and so their count of in-place changes, to themselves; the counts' sum as of the last
@@ -203,14 +204,18 @@ class AdamW:
         lib, stream = _begin(self.device)
         lr = self.lr if lr is None else lr
         lr_dev = None
-        if isinstance(lr, torch.Tensor):
+        if type(lr) is not float and isinstance(lr, torch.Tensor):
             if lr.dtype is not torch.float32 or lr.numel() != 1 or lr.device != self.device:
                 raise ValueError("AdamW.step: lr has to be a number or an fp32 tensor of one element on the weights' device")
             lr_dev, lr = lr.data_ptr(), 0.0
-        h = self._hyper
-        h.lr, (h.beta1, h.beta2), h.eps, h.weight_decay, h.max_norm = lr, self.betas, self.eps, self.weight_decay, self.max_norm
+        beta1, beta2 = self.betas
+        numbers = (lr, beta1, beta2, self.eps, self.weight_decay, self.max_norm)
+        if numbers != self._numbers:                          # 0.2 us less than writing them each time
+            h = self._hyper
+            h.lr, h.beta1, h.beta2, h.eps, h.weight_decay, h.max_norm = numbers
+            self._numbers = numbers
         norm, norm_at = (self._norm, self._norm_at) if self.max_norm != math.inf else (None, None)
-        _check(lib.director_adamw_step(len(self._shapes), grads.array, self._params, ctypes.byref(h), lr_dev, self.steps.data_ptr(), norm_at,
+        _check(lib.director_adamw_step(len(self._shapes), grads.array, self._params, self._hyper_at, lr_dev, self.steps.data_ptr(), norm_at,
                                        self.status.data_ptr(), self._workspace_at, stream),
                "director_adamw_step")
         torch.autograd.graph.increment_version(self._live)         # autograd is told that they were changed in place
