@@ -291,7 +291,8 @@ int director_expert_ffn_backward(director_ctx* ctx, int32_t T, const void* xp, c
  * does not count (padding), or NULL.  loss: dev fp32 [1].  counts: dev int64 [E+1], the last entry is N.  N = 0: loss 0.
  * A masked token's logits and indices are not looked at.  An index outside [0,E) is skipped and reported as
  * DIRECTOR_ERR_BAD_INDEX.  A logit of -inf scores 0; a row with a NaN, a +inf or nothing but -inf adds no scores (its assignments
- * and the token itself count) and is reported as DIRECTOR_ERR_NONFINITE.  The results have the same bits on every run. */
+ * and the token itself count) and is reported as DIRECTOR_ERR_NONFINITE.  The results have the same bits on every run.  Calls on one context share
+ * its sums: they (and replays of graphs that hold them) must not overlap on the GPU. */
 int director_balance_loss(director_ctx* ctx, int32_t T, const float* logits, const int32_t* topk_idx, const uint8_t* token_mask,
                           float* loss, int64_t* counts, void* stream);
 
@@ -308,7 +309,9 @@ int director_balance_loss_backward(director_ctx* ctx, int32_t T, const float* lo
 /* Norm, clipping and update of the gradients of a whole model: no context, any number of tensors, each contiguous, of any length
  * (0 too) and at any address that is a multiple of its element's size.  The tables of tensors are host memory and may be reused when
  * the call returns.  workspace: dev, director_grad_workspace_bytes() bytes, 16-byte aligned, contents irrelevant; calls that may
- * overlap on the GPU need one each.  The results have the same bits on every run on the same kind of GPU.
+ * overlap on the GPU need one each.  The results have the same bits on every run on the same kind of GPU.  Small calls are one launch
+ * of CTAs that wait for one another, as many as the device's SM count allows: on a stream with only part of the SMs (a green
+ * context's) they may be turned down with DIRECTOR_ERR_CUDA.
  * Errors: DIRECTOR_ERR_INVALID_ARG for NULL or misaligned pointers, unknown types, negative lengths, tensors that are written
  * and overlap another of the call; DIRECTOR_ERR_UNSUPPORTED for more than 2^40 elements in a tensor or 2^24 tensors. */
 enum { DIRECTOR_FP32 = 0, DIRECTOR_BF16 = 1 };
@@ -337,7 +340,8 @@ int director_clip_grads(int32_t n, const director_tensor* grads, const director_
  *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
  *   w = w - lr weight_decay w - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
  * in fp32.  A bf16 weight has an fp32 master, which is what w is above, and becomes the master rounded, whatever it held before (who
- * writes a weight between steps has to write its master too); an fp32 weight has none (master NULL).  grads: n tensors as long as the weights; one with data NULL and numel 0 leaves its weight and moments as they are.
+ * writes a weight between steps has to write its master too); an fp32 weight has none (master NULL).  grads: n tensors as long as the
+ * weights; one with data NULL and numel 0 leaves its weight and moments as they are.
  * params: host.  lr: dev fp32 [1] that takes the place of h->lr (for captured steps), or NULL.  steps: dev int64 [1], the steps done
  * so far, advanced by one.  norm: dev fp32 [1] or NULL.
  * Where max_norm is finite or norm is not NULL the norm is taken, and where it is infinite or NaN the step is skipped: nothing

@@ -33,8 +33,8 @@ constexpr int kClusterCtas = 16, kClusterThreads = 1024, kClusterUnroll = 8;
 constexpr int kChunk = kThreads * 8;             // elements of a chunk of the update
 constexpr int kClipUnroll = 4, kClipChunk = kThreads * 8 * kClipUnroll;
 // CTAs of an SM, and so chunks, up to which norm and elementwise part are one cooperative launch.  Against three launches, four tensors:
-// a step of 0.26 M weights 8.2 and 11.8 us a call, of 0.5 M 8.3 and 11.8, but of 1 M (512 chunks) 12.3 and 11.7; clipping of 1 M
-// 9.4 and 14.8.
+// a step of 0.26 M weights 7.9 and 13.1 us a call (6.5 and 7.2 from a graph), of 0.5 M 8.6 and 13.2 (7.9 both); clipping of 1 M 9.7 and
+// 15.5.  With four CTAs an SM a step of 1 M (512 chunks) would take 10.3 instead of 13.1 us a call, but 9.4 instead of 9.3 from a graph.
 constexpr int kSmallCtas = 2;
 constexpr long long kMostElements = 1ll << 40;   // of a tensor
 constexpr int kMostTensors = 1 << 24;            // of a call
@@ -270,7 +270,7 @@ __device__ __forceinline__ void count_step(const Call& q, float scale) {
 }
 
 // The sum of squares: one read of the gradients, HBM-bound.  Four 16-byte loads a thread are under way, a chunk of 16 KB a CTA; 1.41 G
-// bf16 gradients take 390 us, 7.2 TB/s (a CTA to a chunk would take 2 % less, but leave 172 thousand sums to join).
+// bf16 gradients take 387 us, 7.3 TB/s (a CTA to a chunk would leave 172 thousand sums to join).
 // Partial sum blockIdx.x of the workspace, added to it where an earlier launch of the call has written it (blockIdx.x < filled).
 __global__ void __launch_bounds__(kThreads, kNormCtas)
 norm_kernel(const __grid_constant__ Table<1, kNormTensors> t, const Call q, int filled) {
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const Call q, int slot
 }
 
 // The norm alone of small tensors: the CTAs of one cluster hand their sums to its first through distributed shared memory - one
-// launch instead of two, and no workspace.  Sixteen SMs read 2 TB/s: 1 MB in 4.0 us and 4 MB in 5.6 us on the device, where the two
-// launches take 3.8 and 4.5, but 6.3 instead of 10.4 us a call.
+// launch instead of two, and no workspace.  Sixteen SMs read little: 1 MB takes 4.5 us and 4 MB 5.9 us from a graph, where the two
+// launches take 3.8 and 4.2, but 6.6 instead of 11.1 us a call.
 __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterThreads, 1)
 norm_cluster_kernel(const __grid_constant__ Table<1, kFewTensors> t, float* norm) {
     __shared__ double s_sums[kClusterCtas];
@@ -502,7 +502,7 @@ struct Arrays {
     float *master, *exp_avg, *exp_avg_sq;
 };
 
-// Four arrays read, four written, 28 bytes a bf16 weight, HBM-bound: 604 M weights in 2635 us with the norm (168 us), 6.85 TB/s.  Eight
+// Four arrays read, four written, 28 bytes a bf16 weight, HBM-bound: 604 M weights in 2630 us with the norm (170 us), 6.87 TB/s.  Eight
 // elements a thread and not more: 112 bytes under way are enough at 1024 threads an SM, and the registers are full.
 // A chunk: eight elements a thread.  FULL: all of them exist and the state's addresses allow whole accesses; GW, WW: the gradient's and
 // the weight's do.
